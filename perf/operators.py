@@ -367,7 +367,7 @@ def _clip(s):
         import paper_2505_20524_b200 as fp8
         if "items" not in s:
             s["items"] = fp8.fp8_grad_items(s["grads"], s["outs"])
-            s["ws"] = torch.empty(fp8.fp8_grad_norm_workspace_bytes(len(s["grads"])), dtype=torch.uint8, device=DEVICE)
+            s["ws"] = torch.empty(fp8.fp8_grad_norm_workspace_bytes(s["items"]), dtype=torch.uint8, device=DEVICE)
         fp8.fp8_grad_norm(s["items"], s["norm"], s["ws"])
         fp8.fp8_grad_clip(s["items"], s["norm"], s["max_norm"])
         return {"norm": s["norm"], "bucket": s["bucket"]}
