@@ -322,6 +322,102 @@ FP8_API int fp8_linear_dgrad_blockwise(const uint8_t *dY8, const uint8_t *W8, co
 FP8_API int fp8_linear_wgrad_blockwise(const uint8_t *dY8, const uint8_t *X8, const float *sdy_inv_t,
                                const float *sx_inv_t, void *dW_bf16, int T, int N, int K, void *stream);
 
+/* ---- token embedding ----------------------------------------------------------------------------------
+ * Section 3 / Appendix B (architecture table, column "input scaling"): the block's input is the token embedding times
+ * sigma_0^-1, and without a pre-normalisation it is the operand of the first FP8 GEMM.
+ *
+ * fp8_embedding_fwd: out[t, :] = bf16(scale * table[ids[t], :]), one binary32 product and one rounding; *amax_out
+ * (nullable) is overwritten with amax(out).  table [V, D] BF16 or FP32 (table_is_fp32), ids [T] int32 or int64
+ * (ids_are_int64), out [T, D] BF16.  An id outside [0, V) (padding) gives a row of zeros.
+ * fp8_embedding_fwd_q: the producer form under delayed scaling: also out8 = FP8cast(*q_scale * out) of the BF16-rounded
+ * values (bit-identical to fp8_cast of out_bf16); out_bf16 may be NULL when only the codes are wanted.
+ * fp8_embedding_bwd: dtable[v, :] (+)= scale * sum over t with ids[t] = v of dy[t, :], dy [T, D] BF16, dtable [V, D] BF16 or
+ * FP32.  Sums are FP32 in ascending t within runs of 32 equal ids and then over the runs in order, rounded once: the
+ * result is the same from call to call.  Without `accumulate` every row is overwritten (zeros where no token points);
+ * with it only the rows that a token points at are read and written.  Ids outside [0, V) contribute nothing.
+ * ws: scratch of fp8_embedding_bwd_workspace_bytes(T, V, D), 256-byte aligned, contents need no preparation; calls that
+ * share it must be ordered.  D % 8 == 0, D <= 2^20, T and V <= 2^30.  Outputs must not overlap inputs. */
+FP8_API int fp8_embedding_fwd(const void *table, int table_is_fp32, size_t V, size_t D, const void *ids, int ids_are_int64,
+                      size_t T, float scale, void *out_bf16, float *amax_out, void *stream);
+FP8_API int fp8_embedding_fwd_q(const void *table, int table_is_fp32, size_t V, size_t D, const void *ids, int ids_are_int64,
+                        size_t T, float scale, const float *q_scale, int fmt, void *out_bf16, uint8_t *out8,
+                        float *amax_out, void *stream);
+FP8_API size_t fp8_embedding_bwd_workspace_bytes(size_t T, size_t V, size_t D);
+FP8_API int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_are_int64, size_t T, size_t V, size_t D, float scale,
+                      void *dtable, int out_is_fp32, int accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- layer norm ---------------------------------------------------------------------------------------
+ * The centred counterpart of fp8_postnorm_residual, with its gradient.  Per row of D columns:
+ *   mean = sum(x) / D, rstd = 1 / sqrt(sum((x - mean)^2) / D + eps), out = residual + gamma (x - mean) rstd + beta
+ * in FP32 (the squares are of the distances from the mean), rounded once.  x, residual (nullable), out: [T, D] BF16; gamma,
+ * beta: D binary32; mean, rstd (nullable): T binary32, what the backward pass reads; *amax_out (nullable) is overwritten with
+ * amax(out).  out may be x or residual itself.  fp8_layernorm_fwd_q also writes out8 = FP8cast(*q_scale * out) of the
+ * BF16-rounded values (bit-identical to fp8_cast of out_bf16).
+ * fp8_layernorm_bwd: from dout [T, D] BF16 and the forward's x, mean, rstd, with xh = (x - mean) rstd and g = gamma dout:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),  dgamma (+)= sum over rows of dout xh,  dbeta (+)= sum over rows of dout
+ * (the residual's gradient is dout).  dx [T, D] BF16, may be dout or x itself; dgamma, dbeta: D binary32, added to with
+ * `accumulate`.  The sums over rows are FP32 in a fixed order.  ws: scratch of fp8_layernorm_bwd_workspace_bytes(T, D),
+ * 256-byte aligned; calls that share it must be ordered.  D % 8 == 0, D <= 16384, T < 2^31. */
+FP8_API int fp8_layernorm_fwd(const void *x_bf16, const float *gamma, const float *beta, const void *residual_bf16, size_t T,
+                      size_t D, float eps, void *out_bf16, float *mean, float *rstd, float *amax_out, void *stream);
+FP8_API int fp8_layernorm_fwd_q(const void *x_bf16, const float *gamma, const float *beta, const void *residual_bf16, size_t T,
+                        size_t D, float eps, const float *q_scale, int fmt, void *out_bf16, uint8_t *out8, float *mean,
+                        float *rstd, float *amax_out, void *stream);
+FP8_API size_t fp8_layernorm_bwd_workspace_bytes(size_t T, size_t D);
+FP8_API int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, const float *gamma, const float *mean, const float *rstd,
+                      size_t T, size_t D, void *dx_bf16, float *dgamma, float *dbeta, int accumulate, void *ws,
+                      size_t ws_bytes, void *stream);
+
+/* ---- router of the grouped products -------------------------------------------------------------------
+ * What fp8_grouped_linear_* calls the router's output, and its gradient (Appendix D: sparse FFNs, 8 experts of which 2 are
+ * active; balance through an auxiliary loss, z-loss and an expert bias).  logits [T, E] BF16 or FP32 (is_fp32).  For token
+ * t, with p = softmax(logits[t]) in FP32 and the score s_e = logits[t, e] + bias[e] (bias: E binary32, nullable; it
+ * decides the choice only):
+ *   expert[t, 0..k)  the experts of the k largest scores in falling order, equal scores in rising order of e
+ *   weight[t, j]     p of that expert; with `normalize` the softmax over the k chosen logits
+ * Experts of score -inf are never chosen; free slots hold expert -1 and weight 0.  A token whose logits are all -inf (padding)
+ * is not routed: it takes no part in the sums below.  A token with a NaN or +inf logit gets expert -1 and weight NaN, and the
+ * losses become NaN.
+ *   counts[e]        chosen slots of expert e;  offsets[0..E]: their running sums (the group_offsets of the products)
+ *   rows             (nullable) [T k]: the flat slots t k + j sorted by expert, equal experts in rising order: row r of the
+ *                    sorted copies is token rows[r] / k; entries behind offsets[E] are -1
+ *   *n_routed        n, the tokens that take part
+ *   loss[0]          balance_coef * E * sum_e (counts[e] / (k n)) * (sum_t p[t, e] / n)      (1 * balance_coef when even)
+ *   loss[1]          z_coef * sum_t logsumexp(logits[t])^2 / n
+ * fp8_moe_route_bwd: dlogits [T, E] (type of logits) of dloss * (loss[0] + loss[1]) + sum dweight * weight, the choice and the
+ * counts held fixed; dloss (nullable: 1) a device scalar, dweight [T, k] FP32 (nullable: 0).  Rows that are not routed get 0;
+ * rows with a NaN or +inf logit get NaN.  expert, counts, n_routed as the forward left them.
+ * ws: scratch of fp8_moe_route_workspace_bytes(T, E), 256-byte aligned; calls that share it must be ordered.
+ * E <= 256, k <= min(E, 16), T <= 2^26. */
+FP8_API size_t fp8_moe_route_workspace_bytes(size_t T, int E);
+FP8_API int fp8_moe_route(const void *logits, int is_fp32, const float *bias, size_t T, int E, int k, int normalize,
+                  float balance_coef, float z_coef, int *expert, float *weight, int *counts, int *offsets, int *rows,
+                  int *n_routed, float *loss, void *ws, size_t ws_bytes, void *stream);
+FP8_API int fp8_moe_route_bwd(const void *logits, int is_fp32, const int *expert, const int *counts, const int *n_routed, size_t T,
+                      int E, int k, int normalize, float balance_coef, float z_coef, const float *dloss,
+                      const float *dweight, void *dlogits, void *stream);
+
+/* ---- gradient norm and clipping -----------------------------------------------------------------------
+ * Over all gradients of a model, e.g. the dW of the weight-gradient products (the paper trains with a clip of 1.0).
+ * `items` is a HOST array, read during the call; every pointer inside it is a device pointer, 16-byte aligned; items
+ * of n = 0 are skipped.
+ * fp8_grad_norm: *norm = sqrt(sum of all squares).  Squares are binary32 (values above 1.8e19 in size give inf, squares
+ * below 2^-149 vanish), sums of 32 of them too, everything above binary64; fixed order.  `out` is not read.
+ * fp8_grad_clip: out_i = g_i * c with c = min(1, max_norm / (*norm + 1e-6)), one binary32 product rounded to the type of
+ * out; out may be g itself (same type), and then nothing is touched when c = 1.  A NaN norm gives NaN, an infinite one 0
+ * (NaN for infinite entries).  *norm may have been combined over ranks in between.  max_norm > 0, finite.
+ * ws: scratch of fp8_grad_norm_workspace_bytes(items, n_items) (which reads the n only), 256-byte aligned; calls that
+ * share it must be ordered. */
+typedef struct {
+    const void *g;        /* device: n gradients, BF16 or FP32 */
+    void *out;            /* device: where fp8_grad_clip writes (may be NULL for fp8_grad_norm) */
+    size_t n;
+    int g_is_fp32, out_is_fp32;
+} fp8_grad_item;
+FP8_API size_t fp8_grad_norm_workspace_bytes(const fp8_grad_item *items, int n_items);
+FP8_API int fp8_grad_norm(const fp8_grad_item *items, int n_items, float *norm, void *ws, size_t ws_bytes, void *stream);
+FP8_API int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *norm, float max_norm, void *stream);
+
 /* ---- attention ------------------------------------------------------------------------------------
  * Appendix B, Eq. (P): P = Softmax(s Q K^T + M), output P V, grouped-query heads; Appendix E table: both
  * products in FP8, forward and backward.  Tensors are [B, N, H, d] row-major; query head h reads KV head

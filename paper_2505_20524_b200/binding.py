@@ -24,6 +24,10 @@ SYMBOLS = ["fp8_last_error", "fp8_device_status", "fp8_selftest_wait_timeout", "
            "fp8_quantize", "fp8_quantize_multi", "fp8_quantize_delayed_multi", "fp8_swiglu_cast", "fp8_act_cast", "fp8_postnorm_residual", "fp8_postnorm_residual_q", "fp8_qk_norm_rope", "fp8_qk_norm_rope_q", "fp8_kurtosis", "fp8_amax_kurtosis",
            "fp8_linear_fwd", "fp8_linear_dgrad", "fp8_linear_wgrad", "fp8_linear_fwd_q", "fp8_linear_dgrad_q", "fp8_linear_dgrad_rm", "fp8_linear_wgrad_rm", "fp8_grouped_linear_fwd", "fp8_grouped_linear_dgrad", "fp8_grouped_linear_wgrad", "fp8_grouped_linear_wgrad_workspace_bytes", "fp8_grouped_linear_wgrad_dev", "fp8_quantize_blockwise", "fp8_linear_fwd_blockwise", "fp8_linear_dgrad_blockwise", "fp8_linear_wgrad_blockwise", "fp8_attention_workspace_bytes",
            "fp8_attention_fwd", "fp8_attention_fwd_q", "fp8_attention_bwd", "fp8_attention_bwd_static",
+           "fp8_embedding_fwd", "fp8_embedding_fwd_q", "fp8_embedding_bwd_workspace_bytes", "fp8_embedding_bwd",
+           "fp8_layernorm_fwd", "fp8_layernorm_fwd_q", "fp8_layernorm_bwd_workspace_bytes", "fp8_layernorm_bwd",
+           "fp8_moe_route_workspace_bytes", "fp8_moe_route", "fp8_moe_route_bwd",
+           "fp8_grad_norm_workspace_bytes", "fp8_grad_norm", "fp8_grad_clip",
            "fp8_linear_step_host_workspace_bytes", "fp8_linear_step_host", "fp8_attention_step_host_workspace_bytes",
            "fp8_attention_step_host", "fp8_host_sync"]
 
@@ -45,6 +49,26 @@ class AttnScales(C.Structure):
                 ("ds_scale", C.c_void_p), ("ds_amax", C.c_void_p), ("max_slack", C.c_float)]
 
 
+# prototypes of the calls whose arguments go through as plain numbers (addresses, sizes, flags)
+_P, _Z, _I, _F = C.c_void_p, C.c_size_t, C.c_int, C.c_float
+_PROTOTYPES = {
+    "fp8_embedding_fwd": (_I, [_P, _I, _Z, _Z, _P, _I, _Z, _F, _P, _P, _P]),
+    "fp8_embedding_fwd_q": (_I, [_P, _I, _Z, _Z, _P, _I, _Z, _F, _P, _I, _P, _P, _P, _P]),
+    "fp8_embedding_bwd_workspace_bytes": (_Z, [_Z, _Z, _Z]),
+    "fp8_embedding_bwd": (_I, [_P, _P, _I, _Z, _Z, _Z, _F, _P, _I, _I, _P, _Z, _P]),
+    "fp8_layernorm_fwd": (_I, [_P, _P, _P, _P, _Z, _Z, _F, _P, _P, _P, _P, _P]),
+    "fp8_layernorm_fwd_q": (_I, [_P, _P, _P, _P, _Z, _Z, _F, _P, _I, _P, _P, _P, _P, _P, _P]),
+    "fp8_layernorm_bwd_workspace_bytes": (_Z, [_Z, _Z]),
+    "fp8_layernorm_bwd": (_I, [_P, _P, _P, _P, _P, _Z, _Z, _P, _P, _P, _I, _P, _Z, _P]),
+    "fp8_moe_route_workspace_bytes": (_Z, [_Z, _I]),
+    "fp8_moe_route": (_I, [_P, _I, _P, _Z, _I, _I, _I, _F, _F, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]),
+    "fp8_moe_route_bwd": (_I, [_P, _I, _P, _P, _P, _Z, _I, _I, _I, _F, _F, _P, _P, _P, _P]),
+    "fp8_grad_norm_workspace_bytes": (_Z, [_P, _I]),
+    "fp8_grad_norm": (_I, [_P, _I, _P, _P, _Z, _P]),
+    "fp8_grad_clip": (_I, [_P, _I, _P, _F, _P]),
+}
+
+
 def load() -> C.CDLL:
     """Loads the CUDA library; raises if it has not been built (there is nothing to fall back to)."""
     global _lib
@@ -64,6 +88,9 @@ def load() -> C.CDLL:
             lib.fp8_linear_step_host_workspace_bytes.argtypes = [C.c_int] * 3
             lib.fp8_attention_step_host_workspace_bytes.restype = C.c_size_t
             lib.fp8_attention_step_host_workspace_bytes.argtypes = [C.c_int] * 5
+        for name, (res, args) in _PROTOTYPES.items():
+            if hasattr(lib, name):
+                getattr(lib, name).restype, getattr(lib, name).argtypes = res, args
         _lib = lib
     return _lib
 
@@ -237,6 +264,208 @@ def fp8_amax_kurtosis(x, amax, kurtosis, stream=None):
     rows, cols = _rows_cols(x)
     _check(load().fp8_amax_kurtosis(_ptr(x), C.c_size_t(rows), C.c_size_t(cols), _ptr(amax), _ptr(kurtosis),
                                     _stream(stream)))
+
+
+def _addr(name, t, dtype, shape, dev):
+    """Address of a contiguous tensor of the given type (or one of several) and shape on device `dev`; ValueError otherwise."""
+    if not t.is_cuda or t.get_device() != dev:
+        raise ValueError(f"{name}: expects a CUDA tensor on the current device, cuda:{dev}, got one on {t.device}")
+    if t.dtype not in dtype if isinstance(dtype, tuple) else t.dtype != dtype:
+        raise ValueError(f"{name}: unexpected type {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: unexpected shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expects a contiguous tensor")
+    return t.data_ptr()
+
+
+def _opt(name, t, dtype, shape, dev):
+    return None if t is None else _addr(name, t, dtype, shape, dev)
+
+
+def _scratch(ws, dev):
+    return _addr("ws", ws, torch.uint8, ws.shape, dev), ws.numel()
+
+
+def _here(stream):
+    """(current device, address of the stream that the call goes to)."""
+    s = torch.cuda.current_stream() if stream is None else stream
+    dev = torch.cuda.current_device()
+    if s.device_index != dev:
+        raise ValueError(f"stream of cuda:{s.device_index} while cuda:{dev} is current")
+    return dev, s.cuda_stream
+
+
+_BF16, _F32, _U8, _I32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
+_FLOATS, _INTS, _ONE = (torch.bfloat16, torch.float32), (torch.int32, torch.int64), (1,)
+
+
+def _matrix(name, t):
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expects a matrix, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def fp8_embedding_fwd(table, ids, scale, out, amax_out=None, stream=None):
+    """out[t] = scale * table[ids[t]]; table [V, D] BF16 / FP32, ids [T] int32 / int64, out [T, D] BF16, amax of out optional.
+    An id outside [0, V) gives a row of zeros."""
+    (V, D), T = _matrix("table", table), ids.numel()
+    dev, st = _here(stream)
+    _check(load().fp8_embedding_fwd(_addr("table", table, _FLOATS, table.shape, dev), table.dtype is _F32, V, D,
+                                    _addr("ids", ids, _INTS, ids.shape, dev), ids.dtype is torch.int64, T, scale,
+                                    _addr("out", out, _BF16, (T, D), dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_embedding_fwd_q(table, ids, scale, q_scale, fmt, out, out8, amax_out=None, stream=None):
+    """fp8_embedding_fwd that also writes the FP8 codes of its (BF16-rounded) result under the delayed scale `q_scale`
+    (out may be None when only the codes are wanted)."""
+    (V, D), T = _matrix("table", table), ids.numel()
+    dev, st = _here(stream)
+    _check(load().fp8_embedding_fwd_q(_addr("table", table, _FLOATS, table.shape, dev), table.dtype is _F32, V, D,
+                                      _addr("ids", ids, _INTS, ids.shape, dev), ids.dtype is torch.int64, T, scale,
+                                      _addr("q_scale", q_scale, _F32, _ONE, dev), fmt, _opt("out", out, _BF16, (T, D), dev),
+                                      _addr("out8", out8, _U8, (T, D), dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_embedding_bwd_workspace_bytes(T, V, D) -> int:
+    return load().fp8_embedding_bwd_workspace_bytes(T, V, D)
+
+
+def fp8_embedding_bwd(dy, ids, scale, dtable, ws, accumulate=False, stream=None):
+    """dtable[v] (+)= scale * sum of dy[t] over ids[t] = v; dy [T, D] BF16, dtable [V, D] BF16 / FP32, overwritten whole
+    without `accumulate`; ws: a uint8 CUDA tensor of fp8_embedding_bwd_workspace_bytes(T, V, D)."""
+    (V, D), T = _matrix("dtable", dtable), ids.numel()
+    dev, st = _here(stream)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_embedding_bwd(_addr("dy", dy, _BF16, (T, D), dev), _addr("ids", ids, _INTS, ids.shape, dev),
+                                    ids.dtype is torch.int64, T, V, D, scale, _addr("dtable", dtable, _FLOATS, dtable.shape, dev),
+                                    dtable.dtype is _F32, bool(accumulate), w, nw, st))
+
+
+def fp8_layernorm_fwd(x, gamma, beta, eps, out, mean=None, rstd=None, residual=None, amax_out=None, stream=None):
+    """out = residual + gamma * (x - mean) * rstd + beta per row; x, residual, out [T, D] BF16, gamma, beta [D] FP32; mean
+    and rstd [T] FP32 for the backward pass."""
+    T, D = _matrix("x", x)
+    dev, st = _here(stream)
+    _check(load().fp8_layernorm_fwd(_addr("x", x, _BF16, x.shape, dev), _addr("gamma", gamma, _F32, (D,), dev),
+                                    _addr("beta", beta, _F32, (D,), dev), _opt("residual", residual, _BF16, x.shape, dev), T, D,
+                                    eps, _addr("out", out, _BF16, x.shape, dev), _opt("mean", mean, _F32, (T,), dev),
+                                    _opt("rstd", rstd, _F32, (T,), dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_layernorm_fwd_q(x, gamma, beta, eps, q_scale, fmt, out, out8, mean=None, rstd=None, residual=None, amax_out=None,
+                        stream=None):
+    """fp8_layernorm_fwd that also writes the FP8 codes of its (BF16-rounded) result under the delayed scale `q_scale`."""
+    T, D = _matrix("x", x)
+    dev, st = _here(stream)
+    _check(load().fp8_layernorm_fwd_q(_addr("x", x, _BF16, x.shape, dev), _addr("gamma", gamma, _F32, (D,), dev),
+                                      _addr("beta", beta, _F32, (D,), dev), _opt("residual", residual, _BF16, x.shape, dev), T,
+                                      D, eps, _addr("q_scale", q_scale, _F32, _ONE, dev), fmt,
+                                      _addr("out", out, _BF16, x.shape, dev), _addr("out8", out8, _U8, x.shape, dev),
+                                      _opt("mean", mean, _F32, (T,), dev), _opt("rstd", rstd, _F32, (T,), dev),
+                                      _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_layernorm_bwd_workspace_bytes(T, D) -> int:
+    return load().fp8_layernorm_bwd_workspace_bytes(T, D)
+
+
+def fp8_layernorm_bwd(dout, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, accumulate=False, stream=None):
+    """dx, dgamma and dbeta from dout [T, D] BF16 and the forward's x, mean, rstd; dgamma, dbeta [D] FP32, added to with
+    `accumulate`; ws: a uint8 CUDA tensor of fp8_layernorm_bwd_workspace_bytes(T, D)."""
+    T, D = _matrix("x", x)
+    dev, st = _here(stream)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_layernorm_bwd(_addr("dout", dout, _BF16, x.shape, dev), _addr("x", x, _BF16, x.shape, dev),
+                                    _addr("gamma", gamma, _F32, (D,), dev), _addr("mean", mean, _F32, (T,), dev),
+                                    _addr("rstd", rstd, _F32, (T,), dev), T, D, _addr("dx", dx, _BF16, x.shape, dev),
+                                    _addr("dgamma", dgamma, _F32, (D,), dev), _addr("dbeta", dbeta, _F32, (D,), dev),
+                                    bool(accumulate), w, nw, st))
+
+
+def fp8_moe_route_workspace_bytes(T, E) -> int:
+    return load().fp8_moe_route_workspace_bytes(T, E)
+
+
+def fp8_moe_route(logits, bias, normalize, balance_coef, z_coef, expert, weight, counts, offsets, rows, n_routed, loss, ws,
+                  stream=None):
+    """Router: logits [T, E] BF16 / FP32, bias [E] FP32 or None -> expert [T, k] int32, weight [T, k] FP32, counts [E],
+    offsets [E + 1], rows [T k] (or None), n_routed [1] int32, loss [2] FP32 (balance, z); k is the width of `expert`;
+    ws: a uint8 CUDA tensor of fp8_moe_route_workspace_bytes(T, E)."""
+    (T, E), (_, k) = _matrix("logits", logits), _matrix("expert", expert)
+    dev, st = _here(stream)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_moe_route(_addr("logits", logits, _FLOATS, logits.shape, dev), logits.dtype is _F32,
+                                _opt("bias", bias, _F32, (E,), dev), T, E, k, bool(normalize), balance_coef, z_coef,
+                                _addr("expert", expert, _I32, (T, k), dev), _addr("weight", weight, _F32, (T, k), dev),
+                                _addr("counts", counts, _I32, (E,), dev), _addr("offsets", offsets, _I32, (E + 1,), dev),
+                                _opt("rows", rows, _I32, (T * k,), dev), _addr("n_routed", n_routed, _I32, _ONE, dev),
+                                _addr("loss", loss, _F32, (2,), dev), w, nw, st))
+
+
+def fp8_moe_route_bwd(logits, expert, counts, n_routed, normalize, balance_coef, z_coef, dloss, dweight, dlogits, stream=None):
+    """Gradient of the router: dlogits (shape and type of logits) of dloss * (balance + z loss) + sum of dweight * weight;
+    dloss [1] or None (1), dweight [T, k] or None (0); expert, counts, n_routed as fp8_moe_route left them."""
+    (T, E), (_, k) = _matrix("logits", logits), _matrix("expert", expert)
+    dev, st = _here(stream)
+    _check(load().fp8_moe_route_bwd(_addr("logits", logits, _FLOATS, logits.shape, dev), logits.dtype is _F32,
+                                    _addr("expert", expert, _I32, (T, k), dev), _addr("counts", counts, _I32, (E,), dev),
+                                    _addr("n_routed", n_routed, _I32, _ONE, dev), T, E, k, bool(normalize), balance_coef, z_coef,
+                                    _opt("dloss", dloss, _F32, _ONE, dev), _opt("dweight", dweight, _F32, (T, k), dev),
+                                    _addr("dlogits", dlogits, logits.dtype, logits.shape, dev), st))
+
+
+class GradItem(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_size_t), ("g_is_fp32", C.c_int), ("out_is_fp32", C.c_int)]
+
+
+class GradItems:
+    """The gradients of a model as fp8_grad_norm and fp8_grad_clip take them: built once, used every step (it keeps the
+    tensors alive; they have to stay where they are)."""
+
+    def __init__(self, grads, outs):
+        self.tensors = (list(grads), list(outs))
+        if not self.tensors[0] or len(self.tensors[0]) != len(self.tensors[1]):
+            raise ValueError(f"{len(self.tensors[0])} gradients and {len(self.tensors[1])} outputs")
+        self.device = self.tensors[0][0].get_device()
+        self.array = (GradItem * len(self.tensors[0]))()
+        for i, (g, o) in enumerate(zip(*self.tensors)):
+            self.array[i] = GradItem(_addr(f"grads[{i}]", g, _FLOATS, g.shape, self.device),
+                                     _addr(f"outs[{i}]", o, _FLOATS, g.shape, self.device), g.numel(), g.dtype is _F32,
+                                     o.dtype is _F32)
+
+    def __len__(self):
+        return len(self.array)
+
+
+def fp8_grad_items(grads, outs=None) -> GradItems:
+    """The list for fp8_grad_norm / fp8_grad_clip: BF16 or FP32 gradients, and where the clipped ones go (None: in place)."""
+    grads = list(grads)
+    return GradItems(grads, grads if outs is None else outs)
+
+
+def _items(items, dev):
+    if items.device != dev:
+        raise ValueError(f"gradients on cuda:{items.device} while cuda:{dev} is current")
+    return items.array, len(items.array)
+
+
+def fp8_grad_norm_workspace_bytes(items) -> int:
+    return load().fp8_grad_norm_workspace_bytes(items.array, len(items.array))
+
+
+def fp8_grad_norm(items, norm, ws, stream=None):
+    """norm [1] FP32 = the 2-norm of all gradients of `items`; ws: a uint8 CUDA tensor of
+    fp8_grad_norm_workspace_bytes(items)."""
+    dev, st = _here(stream)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_grad_norm(*_items(items, dev), _addr("norm", norm, _F32, _ONE, dev), w, nw, st))
+
+
+def fp8_grad_clip(items, norm, max_norm, stream=None):
+    """Every output of `items` = its gradient * min(1, max_norm / (norm + 1e-6)); norm [1] FP32 stays on the device."""
+    dev, st = _here(stream)
+    _check(load().fp8_grad_clip(*_items(items, dev), _addr("norm", norm, _F32, _ONE, dev), max_norm, st))
 
 
 def _is_fp32(t):

@@ -5,26 +5,9 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "elementwise.cuh"
 
 namespace fp8dpa {
-
-__device__ __forceinline__ uint32_t absmax2e(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7FFF7FFFu); }
-
-__device__ __forceinline__ void block_max_bf16_to(uint32_t m2, unsigned int *amax_bits)
-{
-    __shared__ uint32_t warp_max[32];
-    uint32_t m = max(m2 & 0xFFFFu, m2 >> 16);
-    m = __reduce_max_sync(0xffffffffu, m);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (lane == 0) warp_max[warp] = m;
-    __syncthreads();
-    if (warp == 0) {
-        const int nwarps = (blockDim.x + 31) >> 5;
-        m = lane < nwarps ? warp_max[lane] : 0u;
-        m = __reduce_max_sync(0xffffffffu, m);
-        if (lane == 0 && m != 0u) atomicMax(amax_bits, m << 16);
-    }
-}
 
 __device__ __forceinline__ float silu_mul(float g, float u)
 {
@@ -254,18 +237,6 @@ __global__ void __launch_bounds__(256) kurtosis_kernel(const uint16_t *__restric
 // Post-norm + residual, one CTA per token row.  The row of y stays in registers between the sum of squares and the
 // update: KG 16-byte groups per thread at 256 threads (KG = 1, 2, 4, 8 for up to 2048 ... 16384 columns, chosen at
 // launch so that short rows do not pay for the registers of long ones).
-
-// Eight BF16 values (four packed words) -> eight FP8 codes under `scale`: the codes fp8_cast gives for the same
-// values (binary32 product, one rounding to FP8).  fmt: 0 = E4M3, 1 = E5M2.
-__device__ __forceinline__ uint2 bf16x8_to_fp8x8(const uint32_t (&w)[4], float scale, int fmt)
-{
-    const float v0 = __fmul_rn(bf16_lo(w[0]), scale), v1 = __fmul_rn(bf16_hi(w[0]), scale);
-    const float v2 = __fmul_rn(bf16_lo(w[1]), scale), v3 = __fmul_rn(bf16_hi(w[1]), scale);
-    const float v4 = __fmul_rn(bf16_lo(w[2]), scale), v5 = __fmul_rn(bf16_hi(w[2]), scale);
-    const float v6 = __fmul_rn(bf16_lo(w[3]), scale), v7 = __fmul_rn(bf16_hi(w[3]), scale);
-    if (fmt == 0) return make_uint2(cvt_f32x4_to_fp8x4<0>(v0, v1, v2, v3), cvt_f32x4_to_fp8x4<0>(v4, v5, v6, v7));
-    return make_uint2(cvt_f32x4_to_fp8x4<1>(v0, v1, v2, v3), cvt_f32x4_to_fp8x4<1>(v4, v5, v6, v7));
-}
 
 template <int MODE, int KG>
 __global__ void __launch_bounds__(256) postnorm_residual_kernel(const uint16_t *__restrict__ x,
