@@ -268,12 +268,12 @@ def fp8_amax_kurtosis(x, amax, kurtosis, stream=None):
 
 def _addr(name, t, dtype, shape, dev):
     """Address of a contiguous tensor of the given type (or one of several) and shape on device `dev`; ValueError otherwise."""
-    if not t.is_cuda or t.get_device() != dev:
-        raise ValueError(f"{name}: expects a CUDA tensor on the current device, cuda:{dev}, got one on {t.device}")
-    if t.dtype not in dtype if isinstance(dtype, tuple) else t.dtype != dtype:
+    if t.dtype is not dtype and (dtype.__class__ is not tuple or t.dtype not in dtype):
         raise ValueError(f"{name}: unexpected type {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: unexpected shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: expects a CUDA tensor on the current device, cuda:{dev}, got one on {t.device}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: expects a contiguous tensor")
     return t.data_ptr()
@@ -289,11 +289,12 @@ def _scratch(ws, dev):
 
 def _here(stream):
     """(current device, address of the stream that the call goes to)."""
-    s = torch.cuda.current_stream() if stream is None else stream
     dev = torch.cuda.current_device()
-    if s.device_index != dev:
-        raise ValueError(f"stream of cuda:{s.device_index} while cuda:{dev} is current")
-    return dev, s.cuda_stream
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)      # torch.cuda.current_stream() without its 3 us of objects
+    if stream.device_index != dev:
+        raise ValueError(f"stream of cuda:{stream.device_index} while cuda:{dev} is current")
+    return dev, stream.cuda_stream
 
 
 _BF16, _F32, _U8, _I32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
