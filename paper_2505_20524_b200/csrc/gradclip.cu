@@ -1,8 +1,8 @@
 // Global gradient norm over many tensors and the scaling that clips it.
 //
-// The tensors are cut into chunks of GC_CHUNK elements; chunk c belongs to the tensor whose first chunk is the last one
-// not behind c (a search in the table of first chunks that travels with the launch).  CTA b takes the chunks b, b + grid,
-// ...: the assignment, and with it the order of every sum, depends on the sizes alone.
+// The tensors are cut into chunks of GC_CHUNK elements, numbered through all tensors; a CTA takes a contiguous share of them,
+// whose first tensor the host looks up, and streams through the tensors' parts in it.  The assignment, and with it the order
+// of every sum, depends on the sizes alone.
 #include <math.h>
 
 #include "common.cuh"
@@ -10,95 +10,119 @@
 namespace fp8dpa {
 
 constexpr int GC_THREADS = 256;
-constexpr int GC_PER_THREAD = 32;                         // elements: four groups of eight
-constexpr int GC_CHUNK = GC_THREADS * GC_PER_THREAD;
-constexpr int GC_ITEMS = 512;                             // tensors per launch (16 KB of kernel parameters)
+constexpr int GC_CHUNK = GC_THREADS * 8;
+constexpr int GC_ITEMS = 512;                             // tensors per launch (17 KB of kernel parameters)
 constexpr unsigned GC_MAX_BLOCKS = 148 * 8;
+// The clip keeps 32 elements of a thread in flight (four CTAs per SM), or 16 (eight) where a CTA's share is below this many
+// chunks and latency counts: 12.3 M FP32 elements in 389 tensors (5 chunks per CTA) take 17.4 us with 32 and 12.7 with 16,
+// 218 M BF16 elements (90 chunks per CTA) 218 us with 32 and 229 with 16.
+constexpr unsigned GC_SMALL_SHARE = 16;
 
 struct GradTable {
     const void *g[GC_ITEMS];
     void *out[GC_ITEMS];
     unsigned long long n[GC_ITEMS];
-    unsigned first[GC_ITEMS];                             // the tensor's first chunk
+    unsigned first[GC_ITEMS + 1];                         // the tensor's first chunk
+    unsigned short start[GC_MAX_BLOCKS];                  // the CTA's first tensor
     unsigned char types[GC_ITEMS];                        // bit 0: g is FP32, bit 1: out is FP32
     int items;
     unsigned chunks;
 };
-
-__device__ __forceinline__ int item_of_chunk(const GradTable &t, unsigned c)
+__device__ __forceinline__ unsigned first_chunk_of(unsigned chunks, unsigned block, unsigned blocks)
 {
-    int lo = 0, hi = t.items;                             // first[lo] <= c < first[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (t.first[mid] <= c) lo = mid;
-        else hi = mid;
-    }
-    return lo;
+    return (unsigned)((unsigned long long)chunks * block / blocks);
 }
 
-// eight elements from index i of a tensor of n, zeros behind its end
-__device__ __forceinline__ void load8(const void *g, bool fp32, unsigned long long i, unsigned long long n, float (&f)[8])
+// V consecutive values (V x 2 or 4 bytes: one 8- or 16-byte access) of a BF16 or FP32 tensor
+template <bool F32, int V>
+__device__ __forceinline__ void load_v(const void *p, unsigned long long i, float (&f)[V])
 {
-    if (i + 8 <= n) {
-        if (fp32) {
-            const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(g) + i);
-            const float4 a = p[0], b = p[1];
-            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-        } else {
-            const uint4 v = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(g) + i);
-            f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-            f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
-        }
-        return;
+    if constexpr (F32) {
+        static_assert(V == 4, "16 bytes");
+        const float4 v = __ldg(reinterpret_cast<const float4 *>(static_cast<const float *>(p) + i));
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    } else if constexpr (V == 8) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + i));
+        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+        f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+    } else {
+        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + i));
+        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
     }
+}
+template <bool F32>
+__device__ __forceinline__ float load_1(const void *p, unsigned long long i)
+{
+    return F32 ? static_cast<const float *>(p)[i] : __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
+}
+template <bool F32, int V>
+__device__ __forceinline__ void store_v(void *p, unsigned long long i, const float (&f)[V])
+{
+    if constexpr (F32) {
+        *reinterpret_cast<float4 *>(static_cast<float *>(p) + i) = make_float4(f[0], f[1], f[2], f[3]);
+    } else if constexpr (V == 8) {
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + i) =
+            make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+    } else {
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p) + i) = make_uint2(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]));
+    }
+}
+template <bool F32>
+__device__ __forceinline__ void store_1(void *p, unsigned long long i, float f)
+{
+    if (F32) static_cast<float *>(p)[i] = f;
+    else static_cast<uint16_t *>(p)[i] = (uint16_t)(pack_bf16x2(f, f) & 0xFFFFu);
+}
+
+// Squares of the elements [i, end): FP32 for 32 of a thread's at a time, FP64 above.
+template <bool F32>
+__device__ __forceinline__ double span_squares(const void *g, unsigned long long i, unsigned long long end)
+{
+    constexpr int V = F32 ? 4 : 8, U = 32 / V;
+    constexpr unsigned ROW = GC_THREADS * V;
+    double acc = 0.0;
+    for (; i + (unsigned long long)U * ROW <= end; i += (unsigned long long)U * ROW) {
+        float f[U][V], s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        f[e] = 0.0f;
-        if (i + e < n)
-            f[e] = fp32 ? static_cast<const float *>(g)[i + e] : __uint_as_float((uint32_t)static_cast<const uint16_t *>(g)[i + e] << 16);
-    }
-}
-
-__device__ __forceinline__ void store8(void *o, bool fp32, unsigned long long i, unsigned long long n, const float (&f)[8])
-{
-    const uint32_t w[4] = {pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7])};
-    if (i + 8 <= n) {
-        if (fp32) {
-            float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(o) + i);
-            p[0] = make_float4(f[0], f[1], f[2], f[3]);
-            p[1] = make_float4(f[4], f[5], f[6], f[7]);
-        } else {
-            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(o) + i) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        return;
-    }
+        for (int u = 0; u < U; ++u) load_v<F32, V>(g, i + u * ROW + threadIdx.x * V, f[u]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (i + e >= n) continue;
-        if (fp32) static_cast<float *>(o)[i + e] = f[e];
-        else static_cast<uint16_t *>(o)[i + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s = fmaf(f[u][e], f[u][e], s);
+        acc += (double)s;
     }
+    float s = 0.0f;                                       // fewer than U rows are left
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned long long at = i + u * ROW + threadIdx.x * V;
+        if (at + V <= end) {
+            float f[V];
+            load_v<F32, V>(g, at, f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) s = fmaf(f[e], f[e], s);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float f = at + e < end ? load_1<F32>(g, at + e) : 0.0f;
+                s = fmaf(f, f, s);
+            }
+        }
+    }
+    return acc + (double)s;
 }
 
-// Sum of squares of the CTA's chunks.  Squares and the 32 of a thread's chunk in FP32, everything above in FP64.
 __global__ void __launch_bounds__(GC_THREADS) grad_norm_kernel(const __grid_constant__ GradTable t, double *__restrict__ partial)
 {
     __shared__ double red[GC_THREADS / 32];
     double acc = 0.0;
-    for (unsigned c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-        const int k = item_of_chunk(t, c);
-        const void *g = t.g[k];
-        const unsigned long long n = t.n[k], i0 = (unsigned long long)(c - t.first[k]) * GC_CHUNK + threadIdx.x * 8;
-        const bool fp32 = t.types[k] & 1;
-        float s = 0.0f;
-#pragma unroll
-        for (int j = 0; j < GC_PER_THREAD / 8; ++j) {
-            float f[8];
-            load8(g, fp32, i0 + (unsigned long long)j * (GC_THREADS * 8), n, f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s = fmaf(f[e], f[e], s);
-        }
-        acc += (double)s;
+    const unsigned end = first_chunk_of(t.chunks, blockIdx.x + 1, gridDim.x);
+    unsigned c = first_chunk_of(t.chunks, blockIdx.x, gridDim.x);
+    for (int k = t.start[blockIdx.x]; c < end; ++k) {
+        const unsigned first = t.first[k], stop = min(end, t.first[k + 1]);
+        const unsigned long long i = (unsigned long long)(c - first) * GC_CHUNK;
+        const unsigned long long to = min(t.n[k], (unsigned long long)(stop - first) * GC_CHUNK);
+        acc += (t.types[k] & 1) ? span_squares<true>(t.g[k], i, to) : span_squares<false>(t.g[k], i, to);
+        c = stop;
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
@@ -118,36 +142,78 @@ __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *__re
     double acc = 0.0;
     for (size_t i = threadIdx.x; i < parts; i += 1024) acc += __ldcg(partial + i);
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = acc;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 32; ++w) acc += red[w];
-        *norm = (float)sqrt(acc);
+    for (int round = 0; round < 2; ++round) {             // over a warp's lanes, then over the warps
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
+        if (round == 0) {
+            if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = acc;
+            __syncthreads();
+            acc = red[threadIdx.x & 31];
+        }
+    }
+    if (threadIdx.x == 0) *norm = (float)sqrt(acc);
+}
+
+template <bool IN32, bool OUT32, int PER>
+__device__ __forceinline__ void span_scale(const void *g, void *o, unsigned long long begin, unsigned long long end, float c)
+{
+    constexpr int V = IN32 || OUT32 ? 4 : 8, U = PER / V;  // full 16-byte accesses of the wider side
+    constexpr unsigned ROW = GC_THREADS * V;
+    // last part first: what the norm read last is still in L2
+    const unsigned long long blocks = (end - begin) / ((unsigned long long)U * ROW);
+    const unsigned long long tail = begin + blocks * ((unsigned long long)U * ROW);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned long long at = tail + u * ROW + threadIdx.x * V;
+        if (at + V <= end) {
+            float f[V];
+            load_v<IN32, V>(g, at, f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] *= c;
+            store_v<OUT32, V>(o, at, f);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (at + e < end) store_1<OUT32>(o, at + e, load_1<IN32>(g, at + e) * c);
+        }
+    }
+    for (unsigned long long b = blocks; b > 0; --b) {
+        const unsigned long long i = begin + (b - 1) * ((unsigned long long)U * ROW) + threadIdx.x * V;
+        float f[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_v<IN32, V>(g, i + u * ROW, f[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[u][e] *= c;
+            store_v<OUT32, V>(o, i + u * ROW, f[u]);
+        }
     }
 }
 
 // out = g * min(1, max_norm / (norm + 1e-6)).  A tensor that is clipped in place under a factor of 1 stays untouched.
-__global__ void __launch_bounds__(GC_THREADS) grad_clip_kernel(const __grid_constant__ GradTable t, const float *__restrict__ norm,
+// PER elements of a thread are in flight.
+template <int PER>
+__global__ void __launch_bounds__(GC_THREADS, PER == 16 ? 8 : 1) grad_clip_kernel(const __grid_constant__ GradTable t, const float *__restrict__ norm,
                                                                float max_norm)
 {
     float f = max_norm / (__ldg(norm) + 1e-6f);
     if (f > 1.0f) f = 1.0f;                               // a NaN norm stays NaN
-    for (unsigned c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-        const int k = item_of_chunk(t, c);
+    const unsigned end = first_chunk_of(t.chunks, blockIdx.x + 1, gridDim.x);
+    unsigned c = first_chunk_of(t.chunks, blockIdx.x, gridDim.x);
+    for (int k = t.start[blockIdx.x]; c < end; ++k) {
+        const unsigned first = t.first[k], stop = min(end, t.first[k + 1]);
+        const unsigned long long i = (unsigned long long)(c - first) * GC_CHUNK;
+        const unsigned long long to = min(t.n[k], (unsigned long long)(stop - first) * GC_CHUNK);
         const void *g = t.g[k];
         void *o = t.out[k];
+        c = stop;
         if (f == 1.0f && o == g) continue;
-        const unsigned long long n = t.n[k], i0 = (unsigned long long)(c - t.first[k]) * GC_CHUNK + threadIdx.x * 8;
-        const bool in32 = t.types[k] & 1, out32 = t.types[k] & 2;
-        float v[GC_PER_THREAD / 8][8];
-#pragma unroll
-        for (int j = 0; j < GC_PER_THREAD / 8; ++j) load8(g, in32, i0 + (unsigned long long)j * (GC_THREADS * 8), n, v[j]);
-#pragma unroll
-        for (int j = 0; j < GC_PER_THREAD / 8; ++j) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[j][e] *= f;
-            store8(o, out32, i0 + (unsigned long long)j * (GC_THREADS * 8), n, v[j]);
+        switch (t.types[k]) {
+        case 0: span_scale<false, false, PER>(g, o, i, to, f); break;
+        case 1: span_scale<true, false, PER>(g, o, i, to, f); break;
+        case 2: span_scale<false, true, PER>(g, o, i, to, f); break;
+        default: span_scale<true, true, PER>(g, o, i, to, f); break;
         }
     }
 }
@@ -180,6 +246,8 @@ static int check_items(const char *who, const fp8_grad_item *items, int n_items,
     }
     return FP8_OK;
 }
+
+static unsigned grid_of(const GradTable &t) { return t.chunks < GC_MAX_BLOCKS ? t.chunks : GC_MAX_BLOCKS; }
 
 // The next launch's table from item *at on; chunk numbers stay below 2^31, one tensor may be cut for that.
 struct Cursor {
@@ -216,8 +284,27 @@ static void fill_table(GradTable &t, const fp8_grad_item *items, int n_items, Cu
             at.done = 0;
         }
     }
+    t.first[t.items] = t.chunks;
 }
-static unsigned grid_of(const GradTable &t) { return t.chunks < GC_MAX_BLOCKS ? t.chunks : GC_MAX_BLOCKS; }
+// The tensor in which each CTA's share, chunks * b / blocks on, begins.
+static void fill_starts(GradTable &t)
+{
+    const unsigned blocks = grid_of(t);
+    if (!blocks) return;
+    const unsigned whole = t.chunks / blocks, rest = t.chunks % blocks;
+    unsigned c = 0, part = 0;
+    int k = 0;
+    for (unsigned b = 0; b < blocks; ++b) {
+        while (t.first[k + 1] <= c) ++k;
+        t.start[b] = (unsigned short)k;
+        c += whole;
+        part += rest;
+        if (part >= blocks) {
+            part -= blocks;
+            ++c;
+        }
+    }
+}
 
 }  // namespace fp8dpa
 
@@ -259,6 +346,7 @@ extern "C" int fp8_grad_norm(const fp8_grad_item *items, int n_items, float *nor
     size_t parts = 0;
     while (at.item < n_items) {
         fill_table(t, items, n_items, at);
+        fill_starts(t);
         const unsigned grid = grid_of(t);
         if (grid == 0) break;                             // only empty tensors were left
         grad_norm_kernel<<<grid, GC_THREADS, 0, st>>>(t, partial + parts);
@@ -289,9 +377,11 @@ extern "C" int fp8_grad_clip(const fp8_grad_item *items, int n_items, const floa
     GradTable t;
     while (at.item < n_items) {
         fill_table(t, items, n_items, at);
+        fill_starts(t);
         const unsigned grid = grid_of(t);
         if (grid == 0) break;
-        grad_clip_kernel<<<grid, GC_THREADS, 0, st>>>(t, norm, max_norm);
+        if (t.chunks < GC_SMALL_SHARE * grid) grad_clip_kernel<16><<<grid, GC_THREADS, 0, st>>>(t, norm, max_norm);
+        else grad_clip_kernel<32><<<grid, GC_THREADS, 0, st>>>(t, norm, max_norm);
         FP8_CUDA_CHECK(cudaGetLastError());
     }
     return FP8_OK;
