@@ -268,15 +268,11 @@ def fp8_amax_kurtosis(x, amax, kurtosis, stream=None):
 
 def _addr(name, t, dtype, shape, dev):
     """Address of a contiguous tensor of the given type (or one of several) and shape on device `dev`; ValueError otherwise."""
-    if t.dtype is not dtype and (dtype.__class__ is not tuple or t.dtype not in dtype):
-        raise ValueError(f"{name}: unexpected type {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: unexpected shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.get_device() != dev:
-        raise ValueError(f"{name}: expects a CUDA tensor on the current device, cuda:{dev}, got one on {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: expects a contiguous tensor")
-    return t.data_ptr()
+    if ((t.dtype is dtype or (dtype.__class__ is tuple and t.dtype in dtype)) and t.shape == shape and t.is_contiguous()
+            and t.get_device() == dev):
+        return t.data_ptr()
+    raise ValueError(f"{name}: expects a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, cuda:{dev}; got "
+                     f"{'a' if t.is_contiguous() else 'a strided'} {t.dtype} of shape {tuple(t.shape)} on {t.device}")
 
 
 def _opt(name, t, dtype, shape, dev):

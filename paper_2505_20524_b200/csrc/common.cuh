@@ -51,6 +51,21 @@ inline int check_launch_registers(F *kernel, int expected, const char *name)
     return FP8_OK;
 }
 
+// Lets `Kernel` take `bytes` of dynamic shared memory.  The runtime is asked once per kernel and device (`bytes` is then the
+// most that any launch of this kernel needs).
+template <auto Kernel>
+inline int allow_shared(int bytes)
+{
+    static unsigned char done[64] = {0};
+    int dev = -1;
+    FP8_CUDA_CHECK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64 || !done[dev]) {
+        FP8_CUDA_CHECK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        if (dev >= 0 && dev < 64) done[dev] = 1;
+    }
+    return FP8_OK;
+}
+
 static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ---------------------------------------------------------------- device side

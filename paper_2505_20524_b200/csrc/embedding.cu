@@ -121,11 +121,11 @@ static SortPlan sort_plan(size_t T, size_t V)
     return p;
 }
 
-// Counts of the first digit per chunk, the keys themselves, and a mark on every row of the table that is touched.
+// Counts of the first digit per chunk, and the keys themselves.
 template <typename IdT>
 __global__ void __launch_bounds__(ES_THREADS) embedding_count_kernel(const IdT *__restrict__ ids, size_t T, unsigned V,
                                                                      unsigned chunk_len, int bits, uint32_t *__restrict__ keys,
-                                                                     int *__restrict__ table, uint8_t *__restrict__ touched)
+                                                                     int *__restrict__ table)
 {
     __shared__ int cnt[ES_MAX_DIGITS];
     const int digits = 1 << bits;
@@ -136,7 +136,6 @@ __global__ void __launch_bounds__(ES_THREADS) embedding_count_kernel(const IdT *
         const int id = checked_id(ids, t, V);
         const uint32_t key = id < 0 ? V : (uint32_t)id;
         keys[t] = key;
-        if (touched && id >= 0) touched[id] = 1;
         atomicAdd(&cnt[key & (digits - 1)], 1);
     }
     __syncthreads();
@@ -203,7 +202,7 @@ __device__ __forceinline__ void sort_scatter(const uint32_t *__restrict__ keys, 
         }
 #pragma unroll
         for (int j = 0; j < ES_ITEMS; ++j)
-            rank[j] = warp_stable_rank(pos[j] >= 0 ? (int)((key[j] >> shift) & (digits - 1)) : -1, warp_cnt[warp], lane);
+            rank[j] = warp_stable_rank(pos[j] >= 0 ? (int)((key[j] >> shift) & (digits - 1)) : -1, bits, warp_cnt[warp], lane);
         __syncthreads();
         for (int d = tid; d < digits; d += ES_THREADS) {         // the warps' counts become their starts
             int at = base[d];
@@ -228,18 +227,6 @@ __device__ __forceinline__ void sort_scatter(const uint32_t *__restrict__ keys, 
     }
 }
 
-// ---------------------------------------------------------------- gradient: rows of zeros
-// Rows [v0, v1) of the table that no token touches.
-__device__ __forceinline__ void fill_rows(uint8_t *__restrict__ dtable, size_t row_bytes, const uint8_t *__restrict__ touched,
-                                          size_t v0, size_t v1)
-{
-    for (size_t v = v0; v < v1; ++v) {
-        if (__ldcg(touched + v)) continue;
-        uint4 *row = reinterpret_cast<uint4 *>(dtable + v * row_bytes);
-        for (size_t c = threadIdx.x; c < row_bytes / 16; c += blockDim.x) row[c] = make_uint4(0u, 0u, 0u, 0u);
-    }
-}
-
 __global__ void __launch_bounds__(ES_THREADS) embedding_scatter_kernel(const uint32_t *__restrict__ keys,
                                                                        const int *__restrict__ pos_in, size_t T,
                                                                        unsigned chunk_len, unsigned chunks, int bits, int shift,
@@ -250,11 +237,215 @@ __global__ void __launch_bounds__(ES_THREADS) embedding_scatter_kernel(const uin
     sort_scatter(keys, pos_in, T, chunk_len, chunks, blockIdx.x, bits, shift, table, keys_out, pos_out, next_table);
 }
 
+// Up to SS_MAX_T positions are sorted by one CTA that keeps keys and positions in shared memory between the passes; up to
+// CS_MAX_T by one cluster of 8 CTAs, which read one another's counts through distributed shared memory and pass the keys on
+// through L2; the chunked form above takes the rest, with a launch per pass.  All three are chains of latencies: loads, ranks,
+// scans, scattered stores.
+constexpr int CS_THREADS = 1024;
+constexpr int CS_WARPS = CS_THREADS / 32;
+constexpr int CS_ITEMS = 8;
+constexpr int CS_CTAS = 8;
+constexpr size_t CS_MAX_T = (size_t)CS_CTAS * CS_THREADS * CS_ITEMS;
+constexpr int SS_ITEMS = 2;
+constexpr unsigned CS_CLEAR_CTAS = 17 * CS_CTAS;              // with the sorting cluster 144 of the 148 SMs
+constexpr size_t CS_CLEAR_BYTES = (size_t)40 << 20;
+constexpr size_t SS_MAX_T = (size_t)CS_THREADS * SS_ITEMS;
+
+struct ClusterSort {
+    const void *ids;
+    int ids_are_int64;
+    unsigned T, V;
+    int passes, bits, items;              // items: keys per thread; CTA c ranks positions c * items * 1024 ...
+    uint32_t *keys[2];
+    int *pos[2];
+    uint4 *zero;                          // 16-byte words of the table's first rows, which the idle SMs clear meanwhile
+    size_t zero_words;
+};
+
+// The CTAs behind the sorting ones: a share of the words to clear.  Rows among them that a token points at are written
+// later, by the kernels behind the sort.
+__device__ __forceinline__ void clear_share(const ClusterSort &p, unsigned block, unsigned blocks)
+{
+    const size_t share = (p.zero_words + blocks - 1) / blocks, i0 = block * share, i1 = min(p.zero_words, i0 + share);
+    for (size_t i = i0 + threadIdx.x; i < i1; i += 4 * CS_THREADS)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i + j * CS_THREADS < i1) p.zero[i + j * CS_THREADS] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+__device__ __forceinline__ uint32_t sort_key(const ClusterSort &p, unsigned i)
+{
+    const int id = p.ids_are_int64 ? checked_id(static_cast<const long long *>(p.ids), i, p.V)
+                                   : checked_id(static_cast<const int *>(p.ids), i, p.V);
+    return id < 0 ? p.V : (uint32_t)id;
+}
+
+// Sum over the threads before this one, of the CTA's 1024 (`warp_sum`: CS_WARPS entries).  Ends with a barrier behind its reads.
+__device__ __forceinline__ int scan_before(int v, int *warp_sum)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int scan = v;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, scan, off);
+        if (lane >= off) scan += u;
+    }
+    if (lane == 31) warp_sum[warp] = scan;
+    __syncthreads();
+    const int before = __reduce_add_sync(0xffffffffu, warp > lane ? warp_sum[lane] : 0);
+    __syncthreads();
+    return before + scan - v;
+}
+
+// The warps' counts of digit `tid` become their starts within the CTA; returns the digit's total.
+__device__ __forceinline__ int starts_of_warps(uint16_t *cnt, int digits)
+{
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < CS_WARPS; ++w) {
+        const int v = cnt[w * digits + threadIdx.x];
+        cnt[w * digits + threadIdx.x] = (uint16_t)at;
+        at += v;
+    }
+    return at;
+}
+
+__global__ void __launch_bounds__(CS_THREADS, 1) embedding_cta_sort_kernel(const ClusterSort p)
+{
+    extern __shared__ __align__(16) uint32_t sort_mem[];
+    cudaTriggerProgrammaticLaunchCompletion();
+    if (blockIdx.x > 0) return clear_share(p, blockIdx.x - 1, gridDim.x - 1);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int digits = 1 << p.bits, T = (int)p.T;
+    uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 16384
+    int *base = reinterpret_cast<int *>(cnt + CS_WARPS * digits);                 // [digits]
+    uint32_t *skey = reinterpret_cast<uint32_t *>(base + digits);                 // [items * 1024]
+    uint16_t *spos = reinterpret_cast<uint16_t *>(skey + p.items * CS_THREADS);   // [items * 1024]
+    __shared__ int warp_sum[CS_WARPS];
+    uint16_t *my_cnt = cnt + warp * digits;
+    const int first = warp * 32 * p.items + lane;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * p.bits;
+        for (int d = lane; d < digits / 2; d += 32) reinterpret_cast<uint32_t *>(my_cnt)[d] = 0u;
+        uint32_t key[SS_ITEMS], pr[SS_ITEMS];                                     // pr: position and, above 16 bits, rank
+#pragma unroll
+        for (int j = 0; j < SS_ITEMS; ++j) {
+            const int i = first + 32 * j;
+            if (j >= p.items || i >= T) continue;
+            key[j] = pass == 0 ? sort_key(p, i) : skey[i];
+            pr[j] = pass == 0 ? (uint32_t)i : spos[i];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < SS_ITEMS; ++j) {
+            if (j >= p.items) continue;
+            const int r = warp_stable_rank(first + 32 * j < T ? (int)((key[j] >> shift) & (digits - 1)) : -1, p.bits, my_cnt, lane);
+            if (first + 32 * j < T) pr[j] |= (uint32_t)r << 16;
+        }
+        __syncthreads();
+        const int total = tid < digits ? starts_of_warps(cnt, digits) : 0;
+        const int before = scan_before(total, warp_sum);
+        if (tid < digits) base[tid] = before;
+        __syncthreads();
+        const bool last = pass + 1 == p.passes;
+#pragma unroll
+        for (int j = 0; j < SS_ITEMS; ++j) {
+            if (j >= p.items || first + 32 * j >= T) continue;
+            const int d = (key[j] >> shift) & (digits - 1);
+            const int to = base[d] + my_cnt[d] + (int)(pr[j] >> 16);
+            if (last) {
+                p.keys[p.passes & 1][to] = key[j];
+                p.pos[p.passes & 1][to] = (int)(pr[j] & 0xFFFFu);
+            } else {
+                skey[to] = key[j];
+                spos[to] = (uint16_t)pr[j];
+            }
+        }
+        __syncthreads();
+    }
+}
+
+__device__ __forceinline__ int load_cluster_int(uint32_t saddr, int cta)
+{
+    uint32_t remote;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(saddr), "r"(cta));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(const ClusterSort p)
+{
+    extern __shared__ __align__(16) uint32_t sort_mem[];
+    cudaTriggerProgrammaticLaunchCompletion();
+    if (blockIdx.x >= CS_CTAS) return clear_share(p, blockIdx.x - CS_CTAS, gridDim.x - CS_CTAS);     // whole clusters
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = (int)cluster_ctarank();
+    const int digits = 1 << p.bits;
+    uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 8192 in a CTA
+    int *tot = reinterpret_cast<int *>(cnt + CS_WARPS * digits);                  // [digits]: this CTA's keys per digit
+    int *base = tot + digits;                                                     // [digits]
+    __shared__ int warp_sum[CS_WARPS];
+    uint16_t *my_cnt = cnt + warp * digits;
+    const unsigned first = ((unsigned)cta * CS_WARPS + warp) * 32u * p.items + lane;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * p.bits;
+        for (int d = lane; d < digits / 2; d += 32) reinterpret_cast<uint32_t *>(my_cnt)[d] = 0u;
+        uint32_t key[CS_ITEMS];
+        int pos[CS_ITEMS], rank[CS_ITEMS];
+#pragma unroll
+        for (int j = 0; j < CS_ITEMS; ++j) {
+            const unsigned i = first + 32u * j;
+            key[j] = 0u;
+            pos[j] = -1;
+            if (j < p.items && i < p.T) {
+                if (pass == 0) {
+                    key[j] = sort_key(p, i);
+                    pos[j] = (int)i;
+                } else {
+                    key[j] = __ldcg(p.keys[pass & 1] + i);
+                    pos[j] = __ldcg(p.pos[pass & 1] + i);
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < CS_ITEMS; ++j)
+            if (j < p.items) rank[j] = warp_stable_rank(pos[j] >= 0 ? (int)((key[j] >> shift) & (digits - 1)) : -1, p.bits, my_cnt, lane);
+        __syncthreads();
+        if (tid < digits) tot[tid] = starts_of_warps(cnt, digits);
+        cluster_sync_all();
+        int total = 0, mine = 0;
+        if (tid < digits) {
+            const uint32_t a = smem_u32(tot + tid);
+#pragma unroll
+            for (int c = 0; c < CS_CTAS; ++c) {
+                const int v = load_cluster_int(a, c);
+                if (c < cta) mine += v;
+                total += v;
+            }
+        }
+        const int before = scan_before(total, warp_sum);
+        if (tid < digits) base[tid] = before + mine;
+        __syncthreads();
+        uint32_t *keys_out = p.keys[(pass + 1) & 1];
+        int *pos_out = p.pos[(pass + 1) & 1];
+#pragma unroll
+        for (int j = 0; j < CS_ITEMS; ++j) {
+            if (j >= p.items || pos[j] < 0) continue;
+            const int d = (key[j] >> shift) & (digits - 1);
+            const int to = base[d] + my_cnt[d] + rank[j];
+            keys_out[to] = key[j];
+            pos_out[to] = pos[j];
+        }
+        cluster_sync_all();                     // the stores above, and everybody's reads of `tot`
+    }
+}
+
 // ---------------------------------------------------------------- gradient: sums
 constexpr int EG_THREADS = 256;
-constexpr int EG_RUN = 32;          // sorted positions per work item
-constexpr int EG_UNROLL = 4;        // rows of dy in flight per thread
-constexpr int EG_JOIN = 4;          // partial sums in flight per thread
+constexpr int EG_RUN = 32;          // sorted positions per work item (16: the same time, twice the sums to join)
+constexpr int EG_JOIN = 8;          // partial sums in flight per thread
+constexpr int EG_FILL_ROWS = 4096;  // rows of the table per filling block, at most
 
 struct GradParams {
     const uint16_t *dy;
@@ -267,25 +458,80 @@ struct GradParams {
     int is_fp32, accumulate, lanes_log2;
     float *partial;                  // [items][2][D]: sums of the item's first and last run where they cross its ends
     size_t items, item_blocks, col_blocks;
-    const uint8_t *touched;
-    size_t fill_rows_per_block;
+    size_t fill_rows, fill_from;     // rows of the table per filling block, and the first of them
 };
 
-__device__ __forceinline__ void store_row8(const GradParams &p, uint32_t v, unsigned c, const float (&acc)[8])
+// First place in the sorted keys that is not below v: a warp probes 32 places at a time.
+__device__ __forceinline__ size_t lower_bound(const uint32_t *keys, size_t T, uint32_t v, int lane)
 {
-    const size_t at = (size_t)v * p.n8 + c;
-    float r[8];
-    if (p.is_fp32) {
-        float4 *o = static_cast<float4 *>(p.dtable) + 2 * at;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        if (p.accumulate) { a = o[0]; b = o[1]; }
-        o[0] = make_float4(fmaf(acc[0], p.scale, a.x), fmaf(acc[1], p.scale, a.y), fmaf(acc[2], p.scale, a.z), fmaf(acc[3], p.scale, a.w));
-        o[1] = make_float4(fmaf(acc[4], p.scale, b.x), fmaf(acc[5], p.scale, b.y), fmaf(acc[6], p.scale, b.z), fmaf(acc[7], p.scale, b.w));
+    size_t lo = 0, hi = T;
+    while (lo < hi) {
+        const size_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const int below = __popc(__ballot_sync(0xffffffffu, at < hi && __ldcg(keys + min(at, hi - 1)) < v));
+        if (below == 0) return lo;
+        hi = min(hi, lo + below * step);
+        lo += (below - 1) * step + 1;
+    }
+    return lo;
+}
+
+// Zeros in the rows [v0, v1) that no token points at.
+__device__ __forceinline__ void fill_rows(const GradParams &p, size_t v0, size_t v1)
+{
+    __shared__ uint8_t touched[EG_FILL_ROWS];
+    __shared__ size_t range[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (size_t i = threadIdx.x; i < v1 - v0; i += EG_THREADS) touched[i] = 0;
+    if (warp < 2) {
+        const size_t at = lower_bound(p.keys, p.T, (uint32_t)(warp ? v1 : v0), lane);
+        if (lane == 0) range[warp] = at;
+    }
+    __syncthreads();
+    for (size_t i = range[0] + threadIdx.x; i < range[1]; i += EG_THREADS) touched[__ldcg(p.keys + i) - v0] = 1;
+    __syncthreads();
+    const size_t quads = (size_t)p.n8 * (p.is_fp32 ? 2 : 1);       // 16-byte words per row
+    uint4 *out = static_cast<uint4 *>(p.dtable) + v0 * quads;
+    if (quads >= 32) {                          // a warp per row
+        for (size_t r = warp; r < v1 - v0; r += EG_THREADS / 32) {
+            if (touched[r]) continue;
+            for (size_t c = lane; c < quads; c += 32) out[r * quads + c] = make_uint4(0u, 0u, 0u, 0u);
+        }
     } else {
-        uint4 *o = static_cast<uint4 *>(p.dtable) + at;
-        uint4 u = make_uint4(0u, 0u, 0u, 0u);
-        if (p.accumulate) u = *o;
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        for (size_t i = threadIdx.x; i < (v1 - v0) * quads; i += EG_THREADS)
+            if (!touched[(unsigned)i / (unsigned)quads]) out[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// Eight gradients of a row as they stand: one or two 16-byte words
+template <bool F32>
+struct Row8 {
+    uint4 w[F32 ? 2 : 1];
+};
+template <bool F32>
+__device__ __forceinline__ Row8<F32> load_row8(const GradParams &p, uint32_t v, unsigned c)
+{
+    Row8<F32> r;
+    const uint4 *o = static_cast<const uint4 *>(p.dtable) + ((size_t)v * p.n8 + c) * (F32 ? 2 : 1);
+    r.w[0] = o[0];
+    if (F32) r.w[F32 ? 1 : 0] = o[1];
+    return r;
+}
+template <bool F32>
+__device__ __forceinline__ void store_row8(const GradParams &p, uint32_t v, unsigned c, const float (&acc)[8], const Row8<F32> &old)
+{
+    uint4 *o = static_cast<uint4 *>(p.dtable) + ((size_t)v * p.n8 + c) * (F32 ? 2 : 1);
+    float r[8];
+    if (F32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint4 u = old.w[F32 ? h : 0];
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) r[4 * h + q] = fmaf(acc[4 * h + q], p.scale, __uint_as_float(w[q]));
+            reinterpret_cast<float4 *>(o)[h] = make_float4(r[4 * h], r[4 * h + 1], r[4 * h + 2], r[4 * h + 3]);
+        }
+    } else {
+        const uint32_t w[4] = {old.w[0].x, old.w[0].y, old.w[0].z, old.w[0].w};
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             r[2 * q] = fmaf(acc[2 * q], p.scale, bf16_lo(w[q]));
@@ -294,93 +540,104 @@ __device__ __forceinline__ void store_row8(const GradParams &p, uint32_t v, unsi
         *o = make_uint4(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]), pack_bf16x2(r[4], r[5]), pack_bf16x2(r[6], r[7]));
     }
 }
+template <bool F32>
+__device__ __forceinline__ Row8<F32> zero_row8()
+{
+    Row8<F32> r;
+    r.w[0] = r.w[F32 ? 1 : 0] = make_uint4(0u, 0u, 0u, 0u);
+    return r;
+}
 
 // Work item: EG_RUN neighbouring sorted positions, for the columns of one thread group (`lanes` threads, 8 columns each).
 // A run of equal ids that lies inside the item is finished here; one that crosses the item's start or end leaves its sum
-// in `partial` and is finished by embedding_join_kernel.  Blocks past the items write the untouched rows' zeros.
+// in `partial` ([item][0] the one that began before, [item][1] the one that goes on) and is finished by
+// embedding_join_kernel.  Blocks past the items write the untouched rows' zeros.
+// U rows of dy travel at a time, and with them the old gradients of the runs that end among them.
+template <bool F32, bool ACC, int U>
 __global__ void __launch_bounds__(EG_THREADS) embedding_sum_kernel(const GradParams p)
 {
+    extern __shared__ __align__(16) uint32_t item_mem[];
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
     const size_t work_blocks = p.item_blocks * p.col_blocks;
     if (blockIdx.x >= work_blocks) {
-        const size_t v0 = (blockIdx.x - work_blocks) * p.fill_rows_per_block;
-        fill_rows(static_cast<uint8_t *>(p.dtable), (size_t)p.n8 * (p.is_fp32 ? 32 : 16), p.touched, v0,
-                  min((size_t)p.V, v0 + p.fill_rows_per_block));
+        const size_t v0 = p.fill_from + (blockIdx.x - work_blocks) * p.fill_rows;
+        fill_rows(p, v0, min((size_t)p.V, v0 + p.fill_rows));
         return;
     }
-    const int lanes = 1 << p.lanes_log2;
-    const size_t item = (blockIdx.x / p.col_blocks) * (EG_THREADS >> p.lanes_log2) + (threadIdx.x >> p.lanes_log2);
+    const int lanes = 1 << p.lanes_log2, slots = EG_THREADS >> p.lanes_log2, slot = threadIdx.x >> p.lanes_log2;
+    // the block's keys, one before and one behind them, and its positions
+    uint32_t *skey = item_mem + 1;
+    int *spos = reinterpret_cast<int *>(item_mem + slots * EG_RUN + 2);
+    const size_t block0 = (blockIdx.x / p.col_blocks) * slots * EG_RUN;
+    for (int i = (int)threadIdx.x - 1; i <= slots * EG_RUN; i += EG_THREADS) {
+        const bool in = (i >= 0 || block0 > 0) && block0 + i < p.T;
+        skey[i] = in ? __ldcg(p.keys + block0 + i) : 0xFFFFFFFFu;
+        if (in && i >= 0 && i < slots * EG_RUN) spos[i] = __ldcg(p.pos + block0 + i);
+    }
+    __syncthreads();
+    const size_t item = (blockIdx.x / p.col_blocks) * slots + slot;
     const unsigned c = (unsigned)(blockIdx.x % p.col_blocks) * lanes + (threadIdx.x & (lanes - 1));
     if (item >= p.items || c >= p.n8) return;
-    const size_t i0 = item * EG_RUN, i1 = min(p.T, i0 + EG_RUN);
-    const uint32_t first = __ldg(p.keys + i0);
-    if (first >= p.V) return;                                   // padded positions: sorted behind every id
-    const bool from_before = i0 > 0 && __ldg(p.keys + i0 - 1) == first;
-    uint32_t cur = first;
-    bool head = from_before;                                    // the current run began before this item
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const uint32_t *key = skey + slot * EG_RUN;
+    const int *pos = spos + slot * EG_RUN;
+    const uint32_t before = key[-1];                             // 0xFFFFFFFF in front of the first position
+    const int count = (int)min((size_t)EG_RUN, p.T - item * EG_RUN);
     const size_t D = (size_t)p.n8 * 8;
-    for (size_t i = i0; i < i1; i += EG_UNROLL) {
-        uint32_t key[EG_UNROLL];
-        uint4 v[EG_UNROLL];
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < count && key[i] < p.V; i += U) {         // ids outside the table are sorted behind the others
+        uint4 v[U];
+        Row8<F32> old[ACC ? U : 1];
 #pragma unroll
-        for (int j = 0; j < EG_UNROLL; ++j) {
-            key[j] = i + j < i1 ? __ldg(p.keys + i + j) : 0xFFFFFFFFu;
-            if (key[j] < p.V) v[j] = __ldg(reinterpret_cast<const uint4 *>(p.dy) + (size_t)__ldg(p.pos + i + j) * p.n8 + c);
+        for (int j = 0; j < U; ++j) {
+            if (i + j >= count || key[i + j] >= p.V) continue;
+            v[j] = __ldg(reinterpret_cast<const uint4 *>(p.dy) + (size_t)pos[i + j] * p.n8 + c);
+            if (ACC && key[i + j + 1] != key[i + j] && key[i + j] != before) old[ACC ? j : 0] = load_row8<F32>(p, key[i + j], c);
         }
 #pragma unroll
-        for (int j = 0; j < EG_UNROLL; ++j) {
-            if (key[j] != cur && cur < p.V) {                    // the run ends
-                if (head) {
-                    float *o = p.partial + (item * 2) * D + (size_t)c * 8;
-                    *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                    *reinterpret_cast<float4 *>(o + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                } else if (i + j < i1 || i1 == p.T || __ldg(p.keys + i1) != cur) {
-                    store_row8(p, cur, c, acc);
-                } else {                                         // began here, goes on in the next item
-                    float *o = p.partial + (item * 2 + 1) * D + (size_t)c * 8;
-                    *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                    *reinterpret_cast<float4 *>(o + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                }
+        for (int j = 0; j < U; ++j) {
+            if (i + j >= count) continue;
+            const uint32_t k = key[i + j];
+            if (k >= p.V) continue;
+            const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
 #pragma unroll
-                for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-                head = false;
+            for (int q = 0; q < 4; ++q) {
+                acc[2 * q] += bf16_lo(w[q]);
+                acc[2 * q + 1] += bf16_hi(w[q]);
             }
-            cur = key[j];
-            if (cur < p.V) {
-                const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+            const bool ends = key[i + j + 1] != k;
+            if (!ends && i + j + 1 < count) continue;
+            if (ends && k != before) {
+                if (ACC) store_row8<F32>(p, k, c, acc, old[ACC ? j : 0]);
+                else store_row8<F32>(p, k, c, acc, zero_row8<F32>());
+            } else {
+                float *o = p.partial + (item * 2 + (k == before ? 0 : 1)) * D + (size_t)c * 8;
+                *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                *reinterpret_cast<float4 *>(o + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            }
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    acc[2 * q] += bf16_lo(w[q]);
-                    acc[2 * q + 1] += bf16_hi(w[q]);
-                }
-            }
-        }
-    }
-    if (cur < p.V) {                                             // the item is full and its last run still open
-        const bool goes_on = i1 < p.T && __ldg(p.keys + i1) == cur;
-        if (head || goes_on) {
-            float *o = p.partial + (item * 2 + (head ? 0 : 1)) * D + (size_t)c * 8;
-            *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-            *reinterpret_cast<float4 *>(o + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
-        } else {
-            store_row8(p, cur, c, acc);
+            for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
         }
     }
 }
 
 // The runs that cross items: the item in which such a run begins adds the following items' sums in order.
+template <bool F32>
 __global__ void __launch_bounds__(EG_THREADS) embedding_join_kernel(const GradParams p)
 {
+    cudaGridDependencySynchronize();
     const int lanes = 1 << p.lanes_log2;
     const size_t item = (blockIdx.x / p.col_blocks) * (EG_THREADS >> p.lanes_log2) + (threadIdx.x >> p.lanes_log2);
     const unsigned c = (unsigned)(blockIdx.x % p.col_blocks) * lanes + (threadIdx.x & (lanes - 1));
     if (item + 1 >= p.items || c >= p.n8) return;
     const size_t i1 = (item + 1) * EG_RUN;
-    const uint32_t key = __ldg(p.keys + i1 - 1);
-    if (key >= p.V || __ldg(p.keys + i1) != key) return;                       // nothing goes on
+    const uint32_t key = __ldcg(p.keys + i1 - 1);
+    if (key >= p.V || __ldcg(p.keys + i1) != key) return;                       // nothing goes on
     const size_t i0 = item * EG_RUN;
-    if (__ldg(p.keys + i0) == key && i0 > 0 && __ldg(p.keys + i0 - 1) == key) return;   // it began earlier
+    if (__ldcg(p.keys + i0) == key && i0 > 0 && __ldcg(p.keys + i0 - 1) == key) return;   // it began earlier
     const size_t D = (size_t)p.n8 * 8;
+    Row8<F32> old;
+    if (p.accumulate) old = load_row8<F32>(p, key, c);
     const float *src = p.partial + (item * 2 + 1) * D + (size_t)c * 8;
     const float4 a = __ldcg(reinterpret_cast<const float4 *>(src)), b = __ldcg(reinterpret_cast<const float4 *>(src) + 1);
     float acc[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -393,7 +650,7 @@ __global__ void __launch_bounds__(EG_THREADS) embedding_join_kernel(const GradPa
         for (int j = 0; j < EG_JOIN; ++j) {
             at[j] = 0xFFFFFFFFu;
             if (k + j >= p.items) continue;
-            at[j] = __ldg(p.keys + (k + j) * EG_RUN);
+            at[j] = __ldcg(p.keys + (k + j) * EG_RUN);
             const float4 *q = reinterpret_cast<const float4 *>(p.partial + ((k + j) * 2) * D + (size_t)c * 8);
             lo[j] = __ldcg(q);
             hi[j] = __ldcg(q + 1);
@@ -406,12 +663,12 @@ __global__ void __launch_bounds__(EG_THREADS) embedding_join_kernel(const GradPa
             acc[4] += hi[j].x; acc[5] += hi[j].y; acc[6] += hi[j].z; acc[7] += hi[j].w;
         }
     }
-    store_row8(p, key, c, acc);
+    store_row8<F32>(p, key, c, acc, p.accumulate ? old : zero_row8<F32>());
 }
 
 // ---------------------------------------------------------------- workspace of the gradient
 struct GradWs {
-    size_t keys0, keys1, pos0, pos1, table, touched, zero_bytes, partial, bytes;   // offsets; [table, table + zero_bytes) starts at zero
+    size_t keys0, keys1, pos0, pos1, table, partial, bytes;     // offsets
 };
 static GradWs grad_ws(size_t T, size_t V, size_t D)
 {
@@ -423,12 +680,43 @@ static GradWs grad_ws(size_t T, size_t V, size_t D)
     w.keys1 = at; at += up(T * 4);
     w.pos0 = at; at += up(T * 4);
     w.pos1 = at; at += up(T * 4);
-    w.table = at; at += up((size_t)sp.passes * sp.chunks * ((size_t)4 << sp.bits));
-    w.touched = at; at += up(V);
-    w.zero_bytes = at - w.table;
+    w.table = at; at += T <= CS_MAX_T ? 0 : up((size_t)sp.passes * sp.chunks * ((size_t)4 << sp.bits));
     w.partial = at; at += up((T + EG_RUN - 1) / EG_RUN * 2 * D * sizeof(float));
     w.bytes = at;
     return w;
+}
+
+constexpr int EMB_MAX_SHARED = 160 * 1024;          // the sorts: counts of 32 warps x 1024 digits (68 KB) and the keys
+// One launch with what the triple brackets cannot say: the cluster's size, and whether the kernel may start before the one in
+// front of it has ended (it then waits itself, before it reads what that one wrote).
+template <auto Kernel, typename P>
+static int launch(const P &p, unsigned grid, unsigned threads, size_t smem, unsigned cluster, bool early,
+                  cudaStream_t st)
+{
+    if (smem > 40 * 1024) {
+        const int rc = allow_shared<Kernel>(EMB_MAX_SHARED);
+        if (rc != FP8_OK) return rc;
+    }
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(grid);
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute a[2];
+    c.attrs = a;
+    if (cluster > 1) {
+        a[c.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        a[c.numAttrs].val.clusterDim.x = cluster;
+        a[c.numAttrs].val.clusterDim.y = a[c.numAttrs].val.clusterDim.z = 1;
+        ++c.numAttrs;
+    }
+    if (early) {
+        a[c.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        a[c.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++c.numAttrs;
+    }
+    FP8_CUDA_CHECK(cudaLaunchKernelEx(&c, Kernel, p));
+    return FP8_OK;
 }
 
 static int lanes_log2_for(size_t n8, int most)
@@ -544,23 +832,53 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     uint32_t *keys[2] = {reinterpret_cast<uint32_t *>(base + w.keys0), reinterpret_cast<uint32_t *>(base + w.keys1)};
     int *pos[2] = {reinterpret_cast<int *>(base + w.pos0), reinterpret_cast<int *>(base + w.pos1)};
     int *table = reinterpret_cast<int *>(base + w.table);
-    uint8_t *touched = base + w.touched;
     const SortPlan sp = sort_plan(T, V);
-    const unsigned chunk_len = (unsigned)(sp.chunk_tiles * ES_TILE), chunks = (unsigned)sp.chunks;
-    const size_t table_len = sp.chunks << sp.bits;
-    FP8_CUDA_CHECK(cudaMemsetAsync(table, 0, w.zero_bytes, st));
-    if (ids_are_int64)
-        embedding_count_kernel<long long><<<chunks, ES_THREADS, 0, st>>>(
-            static_cast<const long long *>(ids), T, (unsigned)V, chunk_len, sp.bits, keys[0], table, accumulate ? nullptr : touched);
-    else
-        embedding_count_kernel<int><<<chunks, ES_THREADS, 0, st>>>(
-            static_cast<const int *>(ids), T, (unsigned)V, chunk_len, sp.bits, keys[0], table, accumulate ? nullptr : touched);
-    FP8_CUDA_CHECK(cudaGetLastError());
-    for (int i = 0; i < sp.passes; ++i) {
-        embedding_scatter_kernel<<<chunks, ES_THREADS, 0, st>>>(
-            keys[i & 1], i ? pos[i & 1] : nullptr, T, chunk_len, chunks, sp.bits, i * sp.bits, table + i * table_len,
-            keys[(i + 1) & 1], pos[(i + 1) & 1], i + 1 < sp.passes ? table + (i + 1) * table_len : nullptr);
+    // while at most 8 SMs sort (12 us), the others clear the first rows of a table that is overwritten (131072 x 4096 in BF16:
+    // 179 us with 40 MB of them, 183 with none, 186 with 80)
+    const size_t row_bytes = D * (out_is_fp32 ? 4 : 2);
+    size_t cleared = accumulate || T > CS_MAX_T ? 0 : CS_CLEAR_BYTES / row_bytes;
+    if (cleared > V) cleared = V;
+    if (T <= CS_MAX_T) {
+        ClusterSort s;
+        s.ids = ids;
+        s.ids_are_int64 = ids_are_int64 ? 1 : 0;
+        s.T = (unsigned)T;
+        s.V = (unsigned)V;
+        s.passes = sp.passes;
+        s.bits = sp.bits;
+        const bool single = T <= SS_MAX_T;
+        const size_t across = single ? CS_THREADS : (size_t)CS_CTAS * CS_THREADS;
+        s.items = (int)((T + across - 1) / across);
+        for (int i = 0; i < 2; ++i) {
+            s.keys[i] = keys[i];
+            s.pos[i] = pos[i];
+        }
+        s.zero = static_cast<uint4 *>(dtable);
+        s.zero_words = cleared * row_bytes / 16;
+        const unsigned clearing = cleared ? CS_CLEAR_CTAS : 0;
+        if (single)
+            rc = launch<embedding_cta_sort_kernel>(s, 1 + clearing, CS_THREADS,
+                        (((size_t)CS_WARPS * 2 + 4) << sp.bits) + (size_t)s.items * CS_THREADS * 6, 1, false, st);
+        else
+            rc = launch<embedding_cluster_sort_kernel>(s, CS_CTAS + clearing, CS_THREADS, ((size_t)CS_WARPS * 2 + 8) << sp.bits, CS_CTAS, false, st);
+        if (rc != FP8_OK) return rc;
+    } else {
+        const unsigned chunk_len = (unsigned)(sp.chunk_tiles * ES_TILE), chunks = (unsigned)sp.chunks;
+        const size_t table_len = sp.chunks << sp.bits;
+        if (sp.passes > 1) FP8_CUDA_CHECK(cudaMemsetAsync(table + table_len, 0, (sp.passes - 1) * table_len * sizeof(int), st));
+        if (ids_are_int64)
+            embedding_count_kernel<long long><<<chunks, ES_THREADS, 0, st>>>(static_cast<const long long *>(ids), T, (unsigned)V,
+                                                                             chunk_len, sp.bits, keys[0], table);
+        else
+            embedding_count_kernel<int><<<chunks, ES_THREADS, 0, st>>>(static_cast<const int *>(ids), T, (unsigned)V, chunk_len,
+                                                                       sp.bits, keys[0], table);
         FP8_CUDA_CHECK(cudaGetLastError());
+        for (int i = 0; i < sp.passes; ++i) {
+            embedding_scatter_kernel<<<chunks, ES_THREADS, 0, st>>>(
+                keys[i & 1], i ? pos[i & 1] : nullptr, T, chunk_len, chunks, sp.bits, i * sp.bits, table + i * table_len,
+                keys[(i + 1) & 1], pos[(i + 1) & 1], i + 1 < sp.passes ? table + (i + 1) * table_len : nullptr);
+            FP8_CUDA_CHECK(cudaGetLastError());
+        }
     }
     GradParams p;
     p.dy = static_cast<const uint16_t *>(dy_bf16);
@@ -579,20 +897,23 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     const size_t slots = EG_THREADS >> p.lanes_log2;
     p.item_blocks = (p.items + slots - 1) / slots;
     p.col_blocks = (p.n8 + (1u << p.lanes_log2) - 1) >> p.lanes_log2;
-    p.touched = touched;
-    const size_t row_bytes = D * (out_is_fp32 ? 4 : 2);
-    p.fill_rows_per_block = row_bytes >= 65536 ? 1 : 65536 / row_bytes;
+    p.fill_from = cleared;
+    p.fill_rows = row_bytes >= 131072 ? 1 : 131072 / row_bytes;
+    if (p.fill_rows > EG_FILL_ROWS) p.fill_rows = EG_FILL_ROWS;
     const size_t work = p.item_blocks * p.col_blocks;
-    const size_t fill = accumulate ? 0 : (V + p.fill_rows_per_block - 1) / p.fill_rows_per_block;
+    const size_t fill = accumulate ? 0 : (V - cleared + p.fill_rows - 1) / p.fill_rows;
     if (work + fill > 0x7FFFFFFFull) {
         set_error("fp8_embedding_bwd: T=%zu V=%zu D=%zu needs more blocks than a grid holds", T, V, D);
         return FP8_ERR_SHAPE;
     }
-    embedding_sum_kernel<<<(unsigned)(work + fill), EG_THREADS, 0, st>>>(p);
-    FP8_CUDA_CHECK(cudaGetLastError());
-    if (p.items > 1) {
-        embedding_join_kernel<<<(unsigned)work, EG_THREADS, 0, st>>>(p);
-        FP8_CUDA_CHECK(cudaGetLastError());
-    }
-    return FP8_OK;
+    const size_t smem = (slots * EG_RUN * 2 + 2) * sizeof(uint32_t);
+    const unsigned blocks = (unsigned)(work + fill);
+    if (p.is_fp32 && p.accumulate) rc = launch<embedding_sum_kernel<true, true, 4>>(p, blocks, EG_THREADS, smem, 1, true, st);
+    else if (p.is_fp32) rc = launch<embedding_sum_kernel<true, false, 8>>(p, blocks, EG_THREADS, smem, 1, true, st);
+    else if (p.accumulate) rc = launch<embedding_sum_kernel<false, true, 4>>(p, blocks, EG_THREADS, smem, 1, true, st);
+    else rc = launch<embedding_sum_kernel<false, false, 8>>(p, blocks, EG_THREADS, smem, 1, true, st);
+    if (rc != FP8_OK || p.items == 1) return rc;
+    if (p.is_fp32) rc = launch<embedding_join_kernel<true>>(p, (unsigned)work, EG_THREADS, 0, 1, true, st);
+    else rc = launch<embedding_join_kernel<false>>(p, (unsigned)work, EG_THREADS, 0, 1, true, st);
+    return rc;
 }

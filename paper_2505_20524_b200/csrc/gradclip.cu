@@ -313,15 +313,12 @@ using namespace fp8dpa;
 extern "C" size_t fp8_grad_norm_workspace_bytes(const fp8_grad_item *items, int n_items)
 {
     if (!items || n_items <= 0) return 0;
-    Cursor at;
-    GradTable t;
-    size_t parts = 0;
-    while (at.item < n_items) {
-        fill_table(t, items, n_items, at);
-        parts += grid_of(t);
-    }
-    const size_t bytes = (parts * sizeof(double) + 255) & ~(size_t)255;
-    return bytes ? bytes : 256;
+    // a launch takes GC_ITEMS tensors or 2^30 chunks, and leaves a sum per CTA
+    size_t chunks = 0;
+    for (int i = 0; i < n_items; ++i) chunks += items[i].n / GC_CHUNK + 1;
+    const size_t launches = (size_t)n_items / GC_ITEMS + 1 + 2 * (chunks >> 30);
+    const size_t parts = launches > 1 ? launches * GC_MAX_BLOCKS : chunks < GC_MAX_BLOCKS ? chunks : GC_MAX_BLOCKS;
+    return (parts * sizeof(double) + 255) & ~(size_t)255;
 }
 
 extern "C" int fp8_grad_norm(const fp8_grad_item *items, int n_items, float *norm, void *ws, size_t ws_bytes, void *stream)

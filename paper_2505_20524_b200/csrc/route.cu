@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(RT_THREADS) route_place_kernel(const RoutePara
         __syncwarp();
         const size_t i = tile + tid;
         if (tile != i0) e = i < i1 ? __ldcg(q.expert + i) : -1;
-        const int rank = warp_stable_rank(e, warp_cnt[warp], lane);
+        const int rank = warp_stable_rank(e, quads_log2 + 2, warp_cnt[warp], lane);
         __syncthreads();
         if (tid < q.E) {
             int at = base[tid];

@@ -152,7 +152,7 @@ def test_workspace_sizes_are_host_arithmetic(lib):
     for T in (1, 31, 33, 8192, 600001, 1 << 24):
         for V in (1, 1000, 1 << 20):
             n = lib.fp8_embedding_bwd_workspace_bytes(T, V, 64)
-            assert n >= 16 * T + V and n % 256 == 0
+            assert n >= 16 * T and n % 256 == 0
         assert 0 < lib.fp8_layernorm_bwd_workspace_bytes(T, 4096) <= 148 * 8 * 2 * 4096 * 4
         assert 0 < lib.fp8_moe_route_workspace_bytes(T, 256) < 1 << 20
 
