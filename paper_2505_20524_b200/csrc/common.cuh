@@ -66,6 +66,26 @@ inline int allow_shared(int bytes)
     return FP8_OK;
 }
 
+// Launch of a kernel that may start before the one in front of it on the stream has ended; it calls
+// cudaGridDependencySynchronize() itself before it reads what that one wrote.  Only behind a kernel of the same entry point,
+// itself launched in order: what came before that one has then ended too.
+template <typename... P, typename... A>
+inline int launch_early(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(grid);
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a[0].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = a;
+    c.numAttrs = 1;
+    FP8_CUDA_CHECK(cudaLaunchKernelEx(&c, kernel, P(args)...));
+    return FP8_OK;
+}
+
 static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ---------------------------------------------------------------- device side
@@ -362,6 +382,13 @@ __device__ __forceinline__ uint32_t cluster_ctarank()
 {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// address of the same shared-memory place in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t saddr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
     return r;
 }
 __device__ __forceinline__ void cluster_sync_all()

@@ -367,10 +367,8 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cta_sort_kernel(const
 
 __device__ __forceinline__ int load_cluster_int(uint32_t saddr, int cta)
 {
-    uint32_t remote;
     int v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(saddr), "r"(cta));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_addr(saddr, cta)) : "memory");
     return v;
 }
 
@@ -687,11 +685,9 @@ static GradWs grad_ws(size_t T, size_t V, size_t D)
 }
 
 constexpr int EMB_MAX_SHARED = 160 * 1024;          // the sorts: counts of 32 warps x 1024 digits (68 KB) and the keys
-// One launch with what the triple brackets cannot say: the cluster's size, and whether the kernel may start before the one in
-// front of it has ended (it then waits itself, before it reads what that one wrote).
-template <auto Kernel, typename P>
-static int launch(const P &p, unsigned grid, unsigned threads, size_t smem, unsigned cluster, bool early,
-                  cudaStream_t st)
+// A sort: `cluster` CTAs to a cluster (1: none)
+template <auto Kernel>
+static int launch_sort(const ClusterSort &p, unsigned grid, size_t smem, unsigned cluster, cudaStream_t st)
 {
     if (smem > 40 * 1024) {
         const int rc = allow_shared<Kernel>(EMB_MAX_SHARED);
@@ -699,24 +695,27 @@ static int launch(const P &p, unsigned grid, unsigned threads, size_t smem, unsi
     }
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(grid);
-    c.blockDim = dim3(threads);
+    c.blockDim = dim3(CS_THREADS);
     c.dynamicSmemBytes = smem;
     c.stream = st;
-    cudaLaunchAttribute a[2];
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeClusterDimension;
+    a[0].val.clusterDim.x = cluster;
+    a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
     c.attrs = a;
-    if (cluster > 1) {
-        a[c.numAttrs].id = cudaLaunchAttributeClusterDimension;
-        a[c.numAttrs].val.clusterDim.x = cluster;
-        a[c.numAttrs].val.clusterDim.y = a[c.numAttrs].val.clusterDim.z = 1;
-        ++c.numAttrs;
-    }
-    if (early) {
-        a[c.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        a[c.numAttrs].val.programmaticStreamSerializationAllowed = 1;
-        ++c.numAttrs;
-    }
+    c.numAttrs = cluster > 1 ? 1 : 0;
     FP8_CUDA_CHECK(cudaLaunchKernelEx(&c, Kernel, p));
     return FP8_OK;
+}
+template <bool F32, bool ACC, int U>
+static int launch_sums(const GradParams &p, unsigned grid, size_t smem, cudaStream_t st)
+{
+    constexpr auto kernel = embedding_sum_kernel<F32, ACC, U>;
+    if (smem > 40 * 1024) {
+        const int rc = allow_shared<embedding_sum_kernel<F32, ACC, U>>(EMB_MAX_SHARED);
+        if (rc != FP8_OK) return rc;
+    }
+    return launch_early(kernel, grid, EG_THREADS, smem, st, p);
 }
 
 static int lanes_log2_for(size_t n8, int most)
@@ -857,10 +856,10 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
         s.zero_words = cleared * row_bytes / 16;
         const unsigned clearing = cleared ? CS_CLEAR_CTAS : 0;
         if (single)
-            rc = launch<embedding_cta_sort_kernel>(s, 1 + clearing, CS_THREADS,
-                        (((size_t)CS_WARPS * 2 + 4) << sp.bits) + (size_t)s.items * CS_THREADS * 6, 1, false, st);
+            rc = launch_sort<embedding_cta_sort_kernel>(
+                s, 1 + clearing, (((size_t)CS_WARPS * 2 + 4) << sp.bits) + (size_t)s.items * CS_THREADS * 6, 1, st);
         else
-            rc = launch<embedding_cluster_sort_kernel>(s, CS_CTAS + clearing, CS_THREADS, ((size_t)CS_WARPS * 2 + 8) << sp.bits, CS_CTAS, false, st);
+            rc = launch_sort<embedding_cluster_sort_kernel>(s, CS_CTAS + clearing, ((size_t)CS_WARPS * 2 + 8) << sp.bits, CS_CTAS, st);
         if (rc != FP8_OK) return rc;
     } else {
         const unsigned chunk_len = (unsigned)(sp.chunk_tiles * ES_TILE), chunks = (unsigned)sp.chunks;
@@ -908,12 +907,12 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     }
     const size_t smem = (slots * EG_RUN * 2 + 2) * sizeof(uint32_t);
     const unsigned blocks = (unsigned)(work + fill);
-    if (p.is_fp32 && p.accumulate) rc = launch<embedding_sum_kernel<true, true, 4>>(p, blocks, EG_THREADS, smem, 1, true, st);
-    else if (p.is_fp32) rc = launch<embedding_sum_kernel<true, false, 8>>(p, blocks, EG_THREADS, smem, 1, true, st);
-    else if (p.accumulate) rc = launch<embedding_sum_kernel<false, true, 4>>(p, blocks, EG_THREADS, smem, 1, true, st);
-    else rc = launch<embedding_sum_kernel<false, false, 8>>(p, blocks, EG_THREADS, smem, 1, true, st);
+    if (p.is_fp32 && p.accumulate) rc = launch_sums<true, true, 4>(p, blocks, smem, st);
+    else if (p.is_fp32) rc = launch_sums<true, false, 8>(p, blocks, smem, st);
+    else if (p.accumulate) rc = launch_sums<false, true, 4>(p, blocks, smem, st);
+    else rc = launch_sums<false, false, 8>(p, blocks, smem, st);
     if (rc != FP8_OK || p.items == 1) return rc;
-    if (p.is_fp32) rc = launch<embedding_join_kernel<true>>(p, (unsigned)work, EG_THREADS, 0, 1, true, st);
-    else rc = launch<embedding_join_kernel<false>>(p, (unsigned)work, EG_THREADS, 0, 1, true, st);
+    if (p.is_fp32) rc = launch_early(embedding_join_kernel<true>, (unsigned)work, EG_THREADS, 0, st, p);
+    else rc = launch_early(embedding_join_kernel<false>, (unsigned)work, EG_THREADS, 0, st, p);
     return rc;
 }

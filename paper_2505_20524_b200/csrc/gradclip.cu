@@ -113,6 +113,7 @@ __device__ __forceinline__ double span_squares(const void *g, unsigned long long
 
 __global__ void __launch_bounds__(GC_THREADS) grad_norm_kernel(const __grid_constant__ GradTable t, double *__restrict__ partial)
 {
+    cudaTriggerProgrammaticLaunchCompletion();
     __shared__ double red[GC_THREADS / 32];
     double acc = 0.0;
     const unsigned end = first_chunk_of(t.chunks, blockIdx.x + 1, gridDim.x);
@@ -138,6 +139,7 @@ __global__ void __launch_bounds__(GC_THREADS) grad_norm_kernel(const __grid_cons
 __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *__restrict__ partial, size_t parts,
                                                               float *__restrict__ norm)
 {
+    cudaGridDependencySynchronize();
     __shared__ double red[32];
     double acc = 0.0;
     for (size_t i = threadIdx.x; i < parts; i += 1024) acc += __ldcg(partial + i);
@@ -350,9 +352,11 @@ extern "C" int fp8_grad_norm(const fp8_grad_item *items, int n_items, float *nor
         FP8_CUDA_CHECK(cudaGetLastError());
         parts += grid;
     }
-    grad_norm_join_kernel<<<1, 1024, 0, st>>>(partial, parts, norm);
-    FP8_CUDA_CHECK(cudaGetLastError());
-    return FP8_OK;
+    if (parts == 0) {                                     // nothing but empty tensors
+        FP8_CUDA_CHECK(cudaMemsetAsync(norm, 0, sizeof(float), st));
+        return FP8_OK;
+    }
+    return launch_early(grad_norm_join_kernel, 1, 1024, 0, st, partial, parts, norm);
 }
 
 extern "C" int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *norm, float max_norm, void *stream)

@@ -232,6 +232,7 @@ struct LnBwd {
 template <int KG, bool WARP, bool KEEP, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) layernorm_bwd_kernel(const LnBwd p)
 {
+    cudaTriggerProgrammaticLaunchCompletion();
     extern __shared__ __align__(16) uint4 ring_mem[];
     __shared__ __align__(16) float2 red[2][32];
     const Ring<KG> ring{smem_u32(ring_mem + threadIdx.x)};
@@ -401,6 +402,7 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_sum_kernel(const float *__
                                                                  float *__restrict__ dgamma, float *__restrict__ dbeta,
                                                                  int accumulate)
 {
+    cudaGridDependencySynchronize();
     __shared__ float red[32][33];
     const unsigned j = blockIdx.x * 32 + (threadIdx.x & 31);      // over [2][D]
     const int r = threadIdx.x >> 5;
@@ -426,7 +428,7 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_sum_kernel(const float *__
 struct LnShape {
     int kg;
     bool warp;
-    unsigned threads, per_sm;
+    unsigned threads, per_sm, min_rows;      // min_rows: rows that a CTA has at least, where there are more than 148 of them
 };
 static LnShape ln_shape(size_t D, bool backward)
 {
@@ -436,19 +438,23 @@ static LnShape ln_shape(size_t D, bool backward)
     if (s.warp) {
         s.kg = D <= 256 ? 1 : D <= 512 ? 2 : 4;
         s.threads = 256;
+        s.min_rows = 1;
         s.per_sm = backward ? 2 : 3;
     } else {
         s.kg = D <= 4096 ? 2 : 4;
         s.threads = ((n8 + s.kg - 1) / s.kg + 31) & ~31u;
         s.per_sm = (backward || s.kg == 4 ? 512 : 768) / s.threads;
         if (s.per_sm < 1) s.per_sm = 1;
+        s.min_rows = backward ? 8 : 1;          // fewer sums to add up behind the pass
     }
     return s;
 }
 static unsigned ln_grid(const LnShape &s, size_t T)
 {
-    const size_t rows = s.warp ? s.threads / 32 : 1;
-    const size_t most = (size_t)148 * s.per_sm, want = (T + rows - 1) / rows;
+    const size_t rows = s.warp ? s.threads / 32 : s.min_rows;
+    const size_t most = (size_t)148 * s.per_sm;
+    size_t want = (T + rows - 1) / rows;
+    if (!s.warp && want < 148) want = T < 148 ? T : 148;
     return (unsigned)(want < most ? want : most);
 }
 
@@ -565,8 +571,6 @@ extern "C" int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, cons
     else if (s.kg == 2) rc = ln_launch<layernorm_bwd_kernel<2, false, true, 256, 2>, 2, 256>(p, s, st);
     else rc = ln_launch<layernorm_bwd_kernel<4, false, false, 512, 1>, 4, 512>(p, s, st);
     if (rc != FP8_OK) return rc;
-    layernorm_bwd_sum_kernel<<<(unsigned)((2 * D + 31) / 32), 1024, 0, st>>>(partial, (int)ln_grid(s, T), (unsigned)D, dgamma,
-                                                                            dbeta, accumulate ? 1 : 0);
-    FP8_CUDA_CHECK(cudaGetLastError());
-    return FP8_OK;
+    return launch_early(layernorm_bwd_sum_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, partial, (int)ln_grid(s, T),
+                        (unsigned)D, dgamma, dbeta, accumulate ? 1 : 0);
 }

@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(G == 1 ? 512 : RT_THREADS) route_choose_kernel
     __shared__ float probs[RT_WARPS][G * PL];
     __shared__ double zsum[RT_WARPS];
     __shared__ int nsum[RT_WARPS];
+    cudaTriggerProgrammaticLaunchCompletion();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gl = G == 1 ? 0 : lane, group = tid / G;
     const int warps = blockDim.x >> 5, groups = blockDim.x / G;
     for (int e = tid; e < q.E; e += blockDim.x) cnt[e] = 0;
@@ -292,6 +293,7 @@ __global__ void __launch_bounds__(RT_THREADS) route_place_kernel(const RoutePara
     const int slice = tid >> quads_log2, quad = tid & ((1 << quads_log2) - 1), e_pad = 4 << quads_log2;
     const bool stats = blockIdx.x == gridDim.x - 1;        // without rows it is the only one
     const size_t copies = q.T * q.k, i0 = blockIdx.x * q.chunk * q.k, i1 = min(copies, i0 + q.chunk * q.k);
+    cudaGridDependencySynchronize();
     int e = !stats && i0 + tid < i1 ? __ldcg(q.expert + i0 + tid) : -1;       // the first tile's, on its way meanwhile
     if (slice < slices) {
         int4 total = make_int4(0, 0, 0, 0), mine = total;
@@ -619,9 +621,7 @@ extern "C" int fp8_moe_route(const void *logits, int is_fp32, const float *bias,
     int quads_log2 = 0;
     while ((4 << quads_log2) < E) ++quads_log2;
     const int slices = (RT_THREADS >> quads_log2) < 32 ? RT_THREADS >> quads_log2 : 32;
-    route_place_kernel<<<rows ? q.ctas + 1 : 1, RT_THREADS, 0, st>>>(q, quads_log2, slices);
-    FP8_CUDA_CHECK(cudaGetLastError());
-    return FP8_OK;
+    return launch_early(route_place_kernel, rows ? q.ctas + 1 : 1, RT_THREADS, 0, st, q, quads_log2, slices);
 }
 
 extern "C" int fp8_moe_route_bwd(const void *logits, int is_fp32, const int *expert, const int *counts, const int *n_routed,
