@@ -90,6 +90,7 @@ __global__ void __launch_bounds__(EF_THREADS) embedding_fwd_kernel(const void *_
             if (out8) reinterpret_cast<uint2 *>(out8)[at] = bf16x8_to_fp8x8(w[j], qs, fmt);
         }
     }
+    cudaGridDependencySynchronize();
     if (amax_bits) block_max_bf16_to(m, amax_bits);
 }
 
@@ -757,7 +758,6 @@ static int embedding_fwd(const char *who, const void *table, int table_is_fp32, 
     int rc = check_arch();
     if (rc != FP8_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (amax_out) FP8_CUDA_CHECK(cudaMemsetAsync(amax_out, 0, sizeof(float), st));
     const unsigned n8 = (unsigned)(D / 8);
     const int ll = lanes_log2_for(n8, 8);
     const size_t per_block = (size_t)(EF_THREADS >> ll) * EF_ROWS;
@@ -765,8 +765,8 @@ static int embedding_fwd(const char *who, const void *table, int table_is_fp32, 
     uint16_t *o = static_cast<uint16_t *>(out_bf16);
     unsigned int *ab = reinterpret_cast<unsigned int *>(amax_out);
 #define FP8DPA_LAUNCH_EF(IdT, F32) \
-    embedding_fwd_kernel<IdT, F32><<<blocks, EF_THREADS, 0, st>>>(table, static_cast<const IdT *>(ids), T, (unsigned)V, n8, \
-                                                                  scale, o, ab, q_scale, out8, fmt, ll)
+    return launch_behind_amax(embedding_fwd_kernel<IdT, F32>, T * D, ab, blocks, EF_THREADS, 0, st, table, \
+                              static_cast<const IdT *>(ids), T, (unsigned)V, n8, scale, o, ab, q_scale, out8, fmt, ll)
     if (ids_are_int64) {
         if (table_is_fp32) FP8DPA_LAUNCH_EF(long long, true);
         else FP8DPA_LAUNCH_EF(long long, false);
@@ -775,8 +775,6 @@ static int embedding_fwd(const char *who, const void *table, int table_is_fp32, 
         else FP8DPA_LAUNCH_EF(int, false);
     }
 #undef FP8DPA_LAUNCH_EF
-    FP8_CUDA_CHECK(cudaGetLastError());
-    return FP8_OK;
 }
 
 extern "C" int fp8_embedding_fwd(const void *table, int table_is_fp32, size_t V, size_t D, const void *ids,

@@ -1,8 +1,10 @@
 // Global gradient norm over many tensors and the scaling that clips it.
 //
-// The tensors are cut into chunks of GC_CHUNK elements, numbered through all tensors; a CTA takes a contiguous share of them,
-// whose first tensor the host looks up, and streams through the tensors' parts in it.  The assignment, and with it the order
-// of every sum, depends on the sizes alone.
+// The tensors are cut into chunks of GC_CHUNK elements, numbered through all tensors.  A CTA of the clip takes one chunk, one
+// of the norm GC_NORM_CHUNKS of them, and finds its tensor in a table that travels with the launch; the assignment, and with
+// it the order of every sum, depends on the sizes alone.  Many short CTAs in order, not a few that stay: 218 M BF16 elements
+// to FP32 are scaled at 6.7 TB/s in blocks of 4096 and at 5.5 to 6.0 by 148 x 2 ... 8 CTAs that loop (a share each, or every
+// grid-th block), and read at 7.1 TB/s against 6.6.
 #include <math.h>
 
 #include "common.cuh"
@@ -10,27 +12,27 @@
 namespace fp8dpa {
 
 constexpr int GC_THREADS = 256;
-constexpr int GC_CHUNK = GC_THREADS * 8;
+constexpr int GC_PER_THREAD = 16;
+constexpr int GC_CHUNK = GC_THREADS * GC_PER_THREAD;
+constexpr int GC_NORM_CHUNKS = 4;
 constexpr int GC_ITEMS = 512;                             // tensors per launch (17 KB of kernel parameters)
-constexpr unsigned GC_MAX_BLOCKS = 148 * 8;
-// The clip keeps 32 elements of a thread in flight (four CTAs per SM), or 16 (eight) where a CTA's share is below this many
-// chunks and latency counts: 12.3 M FP32 elements in 389 tensors (5 chunks per CTA) take 17.4 us with 32 and 12.7 with 16,
-// 218 M BF16 elements (90 chunks per CTA) 218 us with 32 and 229 with 16.
-constexpr unsigned GC_SMALL_SHARE = 16;
+constexpr int GC_BUCKETS = 1024;
 
 struct GradTable {
     const void *g[GC_ITEMS];
     void *out[GC_ITEMS];
     unsigned long long n[GC_ITEMS];
     unsigned first[GC_ITEMS + 1];                         // the tensor's first chunk
-    unsigned short start[GC_MAX_BLOCKS];                  // the CTA's first tensor
+    unsigned short start[GC_BUCKETS];                     // the tensor that holds chunk j << bucket_log2
     unsigned char types[GC_ITEMS];                        // bit 0: g is FP32, bit 1: out is FP32
-    int items;
+    int items, bucket_log2;
     unsigned chunks;
 };
-__device__ __forceinline__ unsigned first_chunk_of(unsigned chunks, unsigned block, unsigned blocks)
+__device__ __forceinline__ int item_of_chunk(const GradTable &t, unsigned c)
 {
-    return (unsigned)((unsigned long long)chunks * block / blocks);
+    int k = t.start[c >> t.bucket_log2];
+    while (t.first[k + 1] <= c) ++k;
+    return k;
 }
 
 // V consecutive values (V x 2 or 4 bytes: one 8- or 16-byte access) of a BF16 or FP32 tensor
@@ -81,34 +83,33 @@ __device__ __forceinline__ double span_squares(const void *g, unsigned long long
     constexpr int V = F32 ? 4 : 8, U = 32 / V;
     constexpr unsigned ROW = GC_THREADS * V;
     double acc = 0.0;
-    for (; i + (unsigned long long)U * ROW <= end; i += (unsigned long long)U * ROW) {
+    for (; i < end; i += (unsigned long long)U * ROW) {
         float f[U][V], s = 0.0f;
+        if (i + (unsigned long long)U * ROW <= end) {     // without conditions between them the loads go out together
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_v<F32, V>(g, i + u * ROW + threadIdx.x * V, f[u]);
+            for (int u = 0; u < U; ++u) load_v<F32, V>(g, i + u * ROW + threadIdx.x * V, f[u]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const unsigned long long at = i + u * ROW + threadIdx.x * V;
+#pragma unroll
+                for (int e = 0; e < V; ++e) f[u][e] = 0.0f;
+                if (at + V <= end) {
+                    load_v<F32, V>(g, at, f[u]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (at + e < end) f[u][e] = load_1<F32>(g, at + e);
+                }
+            }
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int e = 0; e < V; ++e) s = fmaf(f[u][e], f[u][e], s);
         acc += (double)s;
     }
-    float s = 0.0f;                                       // fewer than U rows are left
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const unsigned long long at = i + u * ROW + threadIdx.x * V;
-        if (at + V <= end) {
-            float f[V];
-            load_v<F32, V>(g, at, f);
-#pragma unroll
-            for (int e = 0; e < V; ++e) s = fmaf(f[e], f[e], s);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float f = at + e < end ? load_1<F32>(g, at + e) : 0.0f;
-                s = fmaf(f, f, s);
-            }
-        }
-    }
-    return acc + (double)s;
+    return acc;
 }
 
 __global__ void __launch_bounds__(GC_THREADS) grad_norm_kernel(const __grid_constant__ GradTable t, double *__restrict__ partial)
@@ -116,9 +117,9 @@ __global__ void __launch_bounds__(GC_THREADS) grad_norm_kernel(const __grid_cons
     cudaTriggerProgrammaticLaunchCompletion();
     __shared__ double red[GC_THREADS / 32];
     double acc = 0.0;
-    const unsigned end = first_chunk_of(t.chunks, blockIdx.x + 1, gridDim.x);
-    unsigned c = first_chunk_of(t.chunks, blockIdx.x, gridDim.x);
-    for (int k = t.start[blockIdx.x]; c < end; ++k) {
+    unsigned c = blockIdx.x * GC_NORM_CHUNKS;
+    const unsigned end = min(t.chunks, c + GC_NORM_CHUNKS);
+    for (int k = item_of_chunk(t, c); c < end; ++k) {
         const unsigned first = t.first[k], stop = min(end, t.first[k + 1]);
         const unsigned long long i = (unsigned long long)(c - first) * GC_CHUNK;
         const unsigned long long to = min(t.n[k], (unsigned long long)(stop - first) * GC_CHUNK);
@@ -142,6 +143,7 @@ __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *__re
     cudaGridDependencySynchronize();
     __shared__ double red[32];
     double acc = 0.0;
+#pragma unroll 8
     for (size_t i = threadIdx.x; i < parts; i += 1024) acc += __ldcg(partial + i);
 #pragma unroll
     for (int round = 0; round < 2; ++round) {             // over a warp's lanes, then over the warps
@@ -156,67 +158,49 @@ __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *__re
     if (threadIdx.x == 0) *norm = (float)sqrt(acc);
 }
 
-template <bool IN32, bool OUT32, int PER>
-__device__ __forceinline__ void span_scale(const void *g, void *o, unsigned long long begin, unsigned long long end, float c)
+template <bool IN32, bool OUT32>
+__device__ __forceinline__ void scale_chunk(const void *g, void *o, unsigned long long i, unsigned long long end, float c)
 {
-    constexpr int V = IN32 || OUT32 ? 4 : 8, U = PER / V;  // full 16-byte accesses of the wider side
+    constexpr int V = IN32 || OUT32 ? 4 : 8, U = GC_PER_THREAD / V;      // full 16-byte accesses of the wider side
     constexpr unsigned ROW = GC_THREADS * V;
-    // last part first: what the norm read last is still in L2
-    const unsigned long long blocks = (end - begin) / ((unsigned long long)U * ROW);
-    const unsigned long long tail = begin + blocks * ((unsigned long long)U * ROW);
+    i += threadIdx.x * V;
+    float f[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (i + u * ROW + V <= end) load_v<IN32, V>(g, i + u * ROW, f[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const unsigned long long at = tail + u * ROW + threadIdx.x * V;
+        const unsigned long long at = i + u * ROW;
         if (at + V <= end) {
-            float f[V];
-            load_v<IN32, V>(g, at, f);
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] *= c;
-            store_v<OUT32, V>(o, at, f);
+            for (int e = 0; e < V; ++e) f[u][e] *= c;
+            store_v<OUT32, V>(o, at, f[u]);
         } else {
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 if (at + e < end) store_1<OUT32>(o, at + e, load_1<IN32>(g, at + e) * c);
         }
     }
-    for (unsigned long long b = blocks; b > 0; --b) {
-        const unsigned long long i = begin + (b - 1) * ((unsigned long long)U * ROW) + threadIdx.x * V;
-        float f[U][V];
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_v<IN32, V>(g, i + u * ROW, f[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) f[u][e] *= c;
-            store_v<OUT32, V>(o, i + u * ROW, f[u]);
-        }
-    }
 }
 
-// out = g * min(1, max_norm / (norm + 1e-6)).  A tensor that is clipped in place under a factor of 1 stays untouched.
-// PER elements of a thread are in flight.
-template <int PER>
-__global__ void __launch_bounds__(GC_THREADS, PER == 16 ? 8 : 1) grad_clip_kernel(const __grid_constant__ GradTable t, const float *__restrict__ norm,
-                                                               float max_norm)
+// out = g * min(1, max_norm / (norm + 1e-6)).  A tensor that is clipped in place under a factor of 1 stays untouched.  The last
+// chunk first: what the norm read last is still in L2.
+__global__ void __launch_bounds__(GC_THREADS, 8) grad_clip_kernel(const __grid_constant__ GradTable t,
+                                                                  const float *__restrict__ norm, float max_norm)
 {
     float f = max_norm / (__ldg(norm) + 1e-6f);
     if (f > 1.0f) f = 1.0f;                               // a NaN norm stays NaN
-    const unsigned end = first_chunk_of(t.chunks, blockIdx.x + 1, gridDim.x);
-    unsigned c = first_chunk_of(t.chunks, blockIdx.x, gridDim.x);
-    for (int k = t.start[blockIdx.x]; c < end; ++k) {
-        const unsigned first = t.first[k], stop = min(end, t.first[k + 1]);
-        const unsigned long long i = (unsigned long long)(c - first) * GC_CHUNK;
-        const unsigned long long to = min(t.n[k], (unsigned long long)(stop - first) * GC_CHUNK);
-        const void *g = t.g[k];
-        void *o = t.out[k];
-        c = stop;
-        if (f == 1.0f && o == g) continue;
-        switch (t.types[k]) {
-        case 0: span_scale<false, false, PER>(g, o, i, to, f); break;
-        case 1: span_scale<true, false, PER>(g, o, i, to, f); break;
-        case 2: span_scale<false, true, PER>(g, o, i, to, f); break;
-        default: span_scale<true, true, PER>(g, o, i, to, f); break;
-        }
+    const unsigned c = t.chunks - 1 - blockIdx.x;
+    const int k = item_of_chunk(t, c);
+    const void *g = t.g[k];
+    void *o = t.out[k];
+    if (f == 1.0f && o == g) return;
+    const unsigned long long i = (unsigned long long)(c - t.first[k]) * GC_CHUNK, end = min(t.n[k], i + GC_CHUNK);
+    switch (t.types[k]) {
+    case 0: return scale_chunk<false, false>(g, o, i, end, f);
+    case 1: return scale_chunk<true, false>(g, o, i, end, f);
+    case 2: return scale_chunk<false, true>(g, o, i, end, f);
+    default: return scale_chunk<true, true>(g, o, i, end, f);
     }
 }
 
@@ -248,8 +232,6 @@ static int check_items(const char *who, const fp8_grad_item *items, int n_items,
     }
     return FP8_OK;
 }
-
-static unsigned grid_of(const GradTable &t) { return t.chunks < GC_MAX_BLOCKS ? t.chunks : GC_MAX_BLOCKS; }
 
 // The next launch's table from item *at on; chunk numbers stay below 2^31, one tensor may be cut for that.
 struct Cursor {
@@ -288,23 +270,15 @@ static void fill_table(GradTable &t, const fp8_grad_item *items, int n_items, Cu
     }
     t.first[t.items] = t.chunks;
 }
-// The tensor in which each CTA's share, chunks * b / blocks on, begins.
+// Where a CTA begins to look for its tensor.
 static void fill_starts(GradTable &t)
 {
-    const unsigned blocks = grid_of(t);
-    if (!blocks) return;
-    const unsigned whole = t.chunks / blocks, rest = t.chunks % blocks;
-    unsigned c = 0, part = 0;
+    t.bucket_log2 = 0;
+    while ((t.chunks >> t.bucket_log2) >= (unsigned)GC_BUCKETS) ++t.bucket_log2;
     int k = 0;
-    for (unsigned b = 0; b < blocks; ++b) {
-        while (t.first[k + 1] <= c) ++k;
-        t.start[b] = (unsigned short)k;
-        c += whole;
-        part += rest;
-        if (part >= blocks) {
-            part -= blocks;
-            ++c;
-        }
+    for (unsigned j = 0; j << t.bucket_log2 < t.chunks; ++j) {
+        while (t.first[k + 1] <= j << t.bucket_log2) ++k;
+        t.start[j] = (unsigned short)k;
     }
 }
 
@@ -315,11 +289,10 @@ using namespace fp8dpa;
 extern "C" size_t fp8_grad_norm_workspace_bytes(const fp8_grad_item *items, int n_items)
 {
     if (!items || n_items <= 0) return 0;
-    // a launch takes GC_ITEMS tensors or 2^30 chunks, and leaves a sum per CTA
+    // a sum per GC_NORM_CHUNKS chunks, and one more for each launch (of GC_ITEMS tensors or 2^30 chunks)
     size_t chunks = 0;
-    for (int i = 0; i < n_items; ++i) chunks += items[i].n / GC_CHUNK + 1;
-    const size_t launches = (size_t)n_items / GC_ITEMS + 1 + 2 * (chunks >> 30);
-    const size_t parts = launches > 1 ? launches * GC_MAX_BLOCKS : chunks < GC_MAX_BLOCKS ? chunks : GC_MAX_BLOCKS;
+    for (int i = 0; i < n_items; ++i) chunks += (items[i].n + GC_CHUNK - 1) / GC_CHUNK;
+    const size_t parts = chunks / GC_NORM_CHUNKS + (size_t)n_items / GC_ITEMS + 2 * (chunks >> 30) + 2;
     return (parts * sizeof(double) + 255) & ~(size_t)255;
 }
 
@@ -345,9 +318,9 @@ extern "C" int fp8_grad_norm(const fp8_grad_item *items, int n_items, float *nor
     size_t parts = 0;
     while (at.item < n_items) {
         fill_table(t, items, n_items, at);
+        if (t.chunks == 0) break;                         // only empty tensors were left
         fill_starts(t);
-        const unsigned grid = grid_of(t);
-        if (grid == 0) break;                             // only empty tensors were left
+        const unsigned grid = (t.chunks + GC_NORM_CHUNKS - 1) / GC_NORM_CHUNKS;
         grad_norm_kernel<<<grid, GC_THREADS, 0, st>>>(t, partial + parts);
         FP8_CUDA_CHECK(cudaGetLastError());
         parts += grid;
@@ -378,11 +351,9 @@ extern "C" int fp8_grad_clip(const fp8_grad_item *items, int n_items, const floa
     GradTable t;
     while (at.item < n_items) {
         fill_table(t, items, n_items, at);
+        if (t.chunks == 0) break;
         fill_starts(t);
-        const unsigned grid = grid_of(t);
-        if (grid == 0) break;
-        if (t.chunks < GC_SMALL_SHARE * grid) grad_clip_kernel<16><<<grid, GC_THREADS, 0, st>>>(t, norm, max_norm);
-        else grad_clip_kernel<32><<<grid, GC_THREADS, 0, st>>>(t, norm, max_norm);
+        grad_clip_kernel<<<t.chunks, GC_THREADS, 0, st>>>(t, norm, max_norm);
         FP8_CUDA_CHECK(cudaGetLastError());
     }
     return FP8_OK;

@@ -203,6 +203,7 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p
         }
         stage = stage == LN_STAGES - 1 ? 0 : stage + 1;
     }
+    cudaGridDependencySynchronize();
     if (p.amax_bits) block_max_bf16_to(m, p.amax_bits);
 }
 
@@ -459,15 +460,13 @@ static unsigned ln_grid(const LnShape &s, size_t T)
 }
 
 template <auto Kernel, int KG, int MAXT, typename P>
-static int ln_launch(const P &p, const LnShape &s, cudaStream_t st)
+static int ln_launch(const P &p, const LnShape &s, unsigned int *amax, cudaStream_t st)
 {
     if (ring_bytes<KG>(MAXT) > 40 * 1024) {
         const int rc = allow_shared<Kernel>((int)ring_bytes<KG>(MAXT));
         if (rc != FP8_OK) return rc;
     }
-    Kernel<<<ln_grid(s, p.T), s.threads, ring_bytes<KG>(s.threads), st>>>(p);
-    FP8_CUDA_CHECK(cudaGetLastError());
-    return FP8_OK;
+    return launch_behind_amax(Kernel, p.T * p.n8 * 8, amax, ln_grid(s, p.T), s.threads, ring_bytes<KG>(s.threads), st, p);
 }
 
 }  // namespace fp8dpa
@@ -502,15 +501,14 @@ static int layernorm_fwd(const char *who, const void *x, const float *gamma, con
     int rc = check_arch();
     if (rc != FP8_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (amax_out) FP8_CUDA_CHECK(cudaMemsetAsync(amax_out, 0, sizeof(float), st));
     LnFwd p = {static_cast<const uint16_t *>(x), gamma, beta, static_cast<const uint16_t *>(residual), T, (unsigned)(D / 8), eps,
                static_cast<uint16_t *>(out), mean, rstd, reinterpret_cast<unsigned int *>(amax_out), q_scale, out8, fmt};
     const LnShape s = ln_shape(D, false);
-    if (s.warp && s.kg == 1) return ln_launch<layernorm_fwd_kernel<1, true, 256, 3>, 1, 256>(p, s, st);
-    if (s.warp && s.kg == 2) return ln_launch<layernorm_fwd_kernel<2, true, 256, 3>, 2, 256>(p, s, st);
-    if (s.warp) return ln_launch<layernorm_fwd_kernel<4, true, 256, 2>, 4, 256>(p, s, st);
-    if (s.kg == 2) return ln_launch<layernorm_fwd_kernel<2, false, 256, 3>, 2, 256>(p, s, st);
-    return ln_launch<layernorm_fwd_kernel<4, false, 512, 1>, 4, 512>(p, s, st);
+    if (s.warp && s.kg == 1) return ln_launch<layernorm_fwd_kernel<1, true, 256, 3>, 1, 256>(p, s, p.amax_bits, st);
+    if (s.warp && s.kg == 2) return ln_launch<layernorm_fwd_kernel<2, true, 256, 3>, 2, 256>(p, s, p.amax_bits, st);
+    if (s.warp) return ln_launch<layernorm_fwd_kernel<4, true, 256, 2>, 4, 256>(p, s, p.amax_bits, st);
+    if (s.kg == 2) return ln_launch<layernorm_fwd_kernel<2, false, 256, 3>, 2, 256>(p, s, p.amax_bits, st);
+    return ln_launch<layernorm_fwd_kernel<4, false, 512, 1>, 4, 512>(p, s, p.amax_bits, st);
 }
 
 extern "C" int fp8_layernorm_fwd(const void *x_bf16, const float *gamma, const float *beta, const void *residual_bf16,
@@ -566,10 +564,10 @@ extern "C" int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, cons
     float *partial = static_cast<float *>(ws);
     LnBwd p = {static_cast<const uint16_t *>(dout_bf16), static_cast<const uint16_t *>(x_bf16), gamma, mean, rstd, T,
                (unsigned)(D / 8), static_cast<uint16_t *>(dx_bf16), partial};
-    if (s.warp && s.kg == 1) rc = ln_launch<layernorm_bwd_kernel<1, true, true, 256, 2>, 1, 256>(p, s, st);
-    else if (s.warp) rc = ln_launch<layernorm_bwd_kernel<2, true, true, 256, 2>, 2, 256>(p, s, st);
-    else if (s.kg == 2) rc = ln_launch<layernorm_bwd_kernel<2, false, true, 256, 2>, 2, 256>(p, s, st);
-    else rc = ln_launch<layernorm_bwd_kernel<4, false, false, 512, 1>, 4, 512>(p, s, st);
+    if (s.warp && s.kg == 1) rc = ln_launch<layernorm_bwd_kernel<1, true, true, 256, 2>, 1, 256>(p, s, nullptr, st);
+    else if (s.warp) rc = ln_launch<layernorm_bwd_kernel<2, true, true, 256, 2>, 2, 256>(p, s, nullptr, st);
+    else if (s.kg == 2) rc = ln_launch<layernorm_bwd_kernel<2, false, true, 256, 2>, 2, 256>(p, s, nullptr, st);
+    else rc = ln_launch<layernorm_bwd_kernel<4, false, false, 512, 1>, 4, 512>(p, s, nullptr, st);
     if (rc != FP8_OK) return rc;
     return launch_early(layernorm_bwd_sum_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, partial, (int)ln_grid(s, T),
                         (unsigned)D, dgamma, dbeta, accumulate ? 1 : 0);

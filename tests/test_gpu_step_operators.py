@@ -212,6 +212,28 @@ def test_layernorm_forward_keeps_its_digits_far_from_zero():
     within(rstd, rs, 160 * U * rs + rs ** 3 * (66 * U * 1000) ** 2)
 
 
+def test_amax_of_large_outputs():
+    """From 2^24 elements on the amax is set to zero by a kernel beside the main one: the same results, stale values ignored,
+    call after call on the same scalar."""
+    T, D, V = 4100, 4096, 300
+    g, x, gamma, beta = ln_data(T, D, seed=5)
+    table, ids = rnd(g, V, D, std=0.02, dtype=BF16), token_ids(g, T, V)
+    out, a = torch.empty_like(x), scalar(1e30)
+    for k in range(3):
+        fp8.fp8_layernorm_fwd(x, gamma, beta, 1e-5, out, amax_out=a)
+        assert a.item() == out.float().abs().max().item()
+        fp8.fp8_embedding_fwd(table, ids, 50.0 / (k + 1), out, a)
+        assert a.item() == out.float().abs().max().item()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fp8.fp8_layernorm_fwd(x, gamma, beta, 1e-5, out, amax_out=a)
+    x.mul_(0.5)
+    for _ in range(2):
+        a.fill_(1e30)
+        graph.replay()
+        assert a.item() == out.float().abs().max().item()
+
+
 def test_layernorm_constant_rows_and_infinities():
     T, D = 3, 128
     x = torch.full((T, D), 2.5, dtype=BF16, device="cuda")
