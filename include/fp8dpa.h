@@ -336,7 +336,8 @@ FP8_API int fp8_linear_wgrad_blockwise(const uint8_t *dY8, const uint8_t *X8, co
  * result is the same from call to call.  Without `accumulate` every row is overwritten (zeros where no token points);
  * with it only the rows that a token points at are read and written.  Ids outside [0, V) contribute nothing.
  * ws: scratch of fp8_embedding_bwd_workspace_bytes(T, V, D), 256-byte aligned, contents need no preparation; calls that
- * share it must be ordered.  D % 8 == 0, D <= 2^20, T and V <= 2^30.  Outputs must not overlap inputs. */
+ * share it must be ordered.  D % 8 == 0, D <= 2^20, T and V <= 2^30.  ids need the alignment of their own type only.  Outputs
+ * must not overlap inputs. */
 FP8_API int fp8_embedding_fwd(const void *table, int table_is_fp32, size_t V, size_t D, const void *ids, int ids_are_int64,
                       size_t T, float scale, void *out_bf16, float *amax_out, void *stream);
 FP8_API int fp8_embedding_fwd_q(const void *table, int table_is_fp32, size_t V, size_t D, const void *ids, int ids_are_int64,
@@ -388,7 +389,7 @@ FP8_API int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, const f
  * counts held fixed; dloss (nullable: 1) a device scalar, dweight [T, k] FP32 (nullable: 0).  Rows that are not routed get 0;
  * rows with a NaN or +inf logit get NaN.  expert, counts, n_routed as the forward left them.
  * ws: scratch of fp8_moe_route_workspace_bytes(T, E), 256-byte aligned; calls that share it must be ordered.
- * E <= 256, k <= min(E, 16), T <= 2^26. */
+ * E <= 256, k <= min(E, 16), T <= 2^26.  logits and dlogits 16-byte aligned, the others to their own type. */
 FP8_API size_t fp8_moe_route_workspace_bytes(size_t T, int E);
 FP8_API int fp8_moe_route(const void *logits, int is_fp32, const float *bias, size_t T, int E, int k, int normalize,
                   float balance_coef, float z_coef, int *expert, float *weight, int *counts, int *offsets, int *rows,
@@ -405,7 +406,8 @@ FP8_API int fp8_moe_route_bwd(const void *logits, int is_fp32, const int *expert
  * below 2^-149 vanish), sums of 32 of them too, everything above binary64; fixed order.  `out` is not read.
  * fp8_grad_clip: out_i = g_i * c with c = min(1, max_norm / (*norm + 1e-6)), one binary32 product rounded to the type of
  * out; out may be g itself (same type), and then nothing is touched when c = 1.  A NaN norm gives NaN, an infinite one 0
- * (NaN for infinite entries).  *norm may have been combined over ranks in between.  max_norm > 0, finite.
+ * (NaN for infinite entries).  *norm may have been combined over ranks in between.  max_norm > 0, finite.  No two outputs
+ * overlap, and none overlaps another item's g: a tensor is listed once.
  * ws: scratch of fp8_grad_norm_workspace_bytes(items, n_items) (which reads the n only), 256-byte aligned; calls that
  * share it must be ordered. */
 typedef struct {

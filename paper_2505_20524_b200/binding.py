@@ -425,6 +425,8 @@ class GradItems:
         if not self.tensors[0] or len(self.tensors[0]) != len(self.tensors[1]):
             raise ValueError(f"{len(self.tensors[0])} gradients and {len(self.tensors[1])} outputs")
         self.device = self.tensors[0][0].get_device()
+        if self.device < 0:
+            raise ValueError("expects CUDA tensors")
         self.array = (GradItem * len(self.tensors[0]))()
         for i, (g, o) in enumerate(zip(*self.tensors)):
             self.array[i] = GradItem(_addr(f"grads[{i}]", g, _FLOATS, g.shape, self.device),

@@ -86,6 +86,7 @@ inline int launch_early(void (*kernel)(P...), unsigned grid, unsigned threads, s
     return FP8_OK;
 }
 
+static inline bool aligned_to(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ---------------------------------------------------------------- device side

@@ -751,8 +751,8 @@ static int embedding_fwd(const char *who, const void *table, int table_is_fp32, 
         set_error("%s: unsupported shape T=%zu V=%zu D=%zu (D %% 8 == 0, D <= 2^20, T and V <= 2^30)", who, T, V, D);
         return FP8_ERR_SHAPE;
     }
-    if (!aligned16(table) || !aligned16(ids) || !aligned16(out_bf16) || !aligned16(out8)) {
-        set_error("%s: pointers must be 16-byte aligned", who);
+    if (!aligned16(table) || !aligned_to(ids, ids_are_int64 ? 8 : 4) || !aligned16(out_bf16) || !aligned16(out8)) {
+        set_error("%s: pointers must be 16-byte aligned (ids: to their own size)", who);
         return FP8_ERR_ALIGN;
     }
     int rc = check_arch();
@@ -813,8 +813,8 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
         set_error("fp8_embedding_bwd: unsupported shape T=%zu V=%zu D=%zu (D %% 8 == 0, D <= 2^20, T and V <= 2^30)", T, V, D);
         return FP8_ERR_SHAPE;
     }
-    if (!aligned16(dy_bf16) || !aligned16(ids) || !aligned16(dtable)) {
-        set_error("fp8_embedding_bwd: pointers must be 16-byte aligned");
+    if (!aligned16(dy_bf16) || !aligned_to(ids, ids_are_int64 ? 8 : 4) || !aligned16(dtable)) {
+        set_error("fp8_embedding_bwd: pointers must be 16-byte aligned (ids: to their own size)");
         return FP8_ERR_ALIGN;
     }
     const GradWs w = grad_ws(T, V, D);

@@ -591,8 +591,8 @@ extern "C" int fp8_moe_route(const void *logits, int is_fp32, const float *bias,
     }
     int rc = route_check("fp8_moe_route", T, E, k, balance_coef, z_coef);
     if (rc != FP8_OK) return rc;
-    if (!aligned16(logits) || !aligned16(expert) || !aligned16(weight)) {
-        set_error("fp8_moe_route: tensor pointers must be 16-byte aligned");
+    if (!aligned16(logits) || !aligned_to(expert, 4) || !aligned_to(weight, 4) || !aligned_to(rows, 4)) {
+        set_error("fp8_moe_route: logits must be 16-byte aligned, the per-token outputs 4-byte");
         return FP8_ERR_ALIGN;
     }
     const size_t need = fp8_moe_route_workspace_bytes(T, E);
@@ -634,8 +634,8 @@ extern "C" int fp8_moe_route_bwd(const void *logits, int is_fp32, const int *exp
     }
     int rc = route_check("fp8_moe_route_bwd", T, E, k, balance_coef, z_coef);
     if (rc != FP8_OK) return rc;
-    if (!aligned16(logits) || !aligned16(expert) || !aligned16(dweight) || !aligned16(dlogits)) {
-        set_error("fp8_moe_route_bwd: tensor pointers must be 16-byte aligned");
+    if (!aligned16(logits) || !aligned_to(expert, 4) || !aligned_to(dweight, 4) || !aligned16(dlogits)) {
+        set_error("fp8_moe_route_bwd: logits and dlogits must be 16-byte aligned, expert and dweight 4-byte");
         return FP8_ERR_ALIGN;
     }
     rc = check_arch();

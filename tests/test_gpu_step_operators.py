@@ -93,7 +93,9 @@ EMB_BWD = [  # T, V, D, id pattern
     (33, 50, 16, "same"), (64, 50, 16, "same"), (100, 7, 2056, "random"), (1000, 100000, 64, "random"),
     (5000, 40, 72, "random"), (5000, 1000, 264, "same"), (4096, 3000, 128, "sorted"), (4097, 3000, 128, "runs32"),
     (70000, 1100, 8, "zipf"), (9000, (1 << 20) + 5, 8, "zipf"), (600001, 2000, 8, "zipf"), (77, 9, 40, "padding"),
-    (2048, 1024, 8, "random"), (2049, 1023, 8, "random"), (700, 300, 4104, "zipf"),
+    (2048, 1024, 8, "random"), (2049, 1023, 8, "random"), (700, 300, 4104, "zipf"), (2000, (1 << 20) - 1, 8, "zipf"),
+    (3000, (1 << 20) - 1, 8, "zipf"), (66000, (1 << 20) - 1, 8, "zipf"), (16384, 512, 16, "same"), (65536, 513, 8, "sorted"),
+    (65537, 513, 8, "runs32"),
 ]
 
 
@@ -145,6 +147,37 @@ def test_embedding_gradient(T, V, D, kind, dt, accumulate):
     if accumulate:
         first[n == 0] = 0
     assert torch.equal(first, got)
+
+
+def test_embedding_gradient_ignores_what_stands_at_padded_positions():
+    T, V, D = 3000, 50, 64
+    g = gen(6)
+    ids, dy = torch.randint(0, V, (T,), generator=g, device="cuda"), rnd(g, T, D, dtype=BF16)
+    pad = torch.rand(T, generator=g, device="cuda") < 0.3
+    ids[pad] = -1
+    clean, dirty = torch.empty((V, D), device="cuda"), torch.empty((V, D), device="cuda")
+    ws = ws_of(fp8.fp8_embedding_bwd_workspace_bytes(T, V, D))
+    fp8.fp8_embedding_bwd(dy, ids, 1.0, clean, ws)
+    dy[pad] = math.nan
+    fp8.fp8_embedding_bwd(dy, ids, 1.0, dirty, ws)
+    assert torch.equal(clean, dirty) and torch.isfinite(dirty).all()
+
+
+def test_embedding_takes_slices_of_the_ids():
+    """ids need no more than their own alignment: the tokens shifted by one."""
+    T, V, D = 33, 60, 32
+    g = gen(7)
+    table, dy = rnd(g, V, D), rnd(g, T, D, dtype=BF16)
+    for dt in (torch.int64, torch.int32):
+        ids = torch.randint(0, V, (T + 1,), generator=g, device="cuda", dtype=dt)
+        out = torch.empty((T, D), dtype=BF16, device="cuda")
+        fp8.fp8_embedding_fwd(table, ids[1:], 1.0, out)
+        assert torch.equal(out, table[ids[1:].long()].to(BF16))
+        a, b = torch.empty((V, D), device="cuda"), torch.empty((V, D), device="cuda")
+        ws = ws_of(fp8.fp8_embedding_bwd_workspace_bytes(T, V, D))
+        fp8.fp8_embedding_bwd(dy, ids[1:], 1.0, a, ws)
+        fp8.fp8_embedding_bwd(dy, ids[1:].clone(), 1.0, b, ws)
+        assert torch.equal(a, b)
 
 
 # ------------------------------------------------------------------------------------------------ layer norm
@@ -605,6 +638,47 @@ def test_gradient_norm_of_infinities_and_nan():
     assert math.isnan(norm.item())
     fp8.fp8_grad_clip(items, norm, 1.0)
     assert torch.isnan(y).all()
+
+
+# ------------------------------------------------------------------------------------------------ beyond 32 bits
+def test_offsets_beyond_32_bits():
+    """Tables, rows and gradients of more than 2^32 bytes (and 2^31 elements): the far end is read and written."""
+    V, D, T = 600_000, 4096, 40
+    table = torch.zeros((V, D), dtype=BF16, device="cuda")                       # 4.9 GB
+    ids = torch.arange(V - T, V, device="cuda")
+    table[V - T:] = rnd(gen(1), T, D, dtype=BF16)
+    out = torch.empty((T, D), dtype=BF16, device="cuda")
+    fp8.fp8_embedding_fwd(table, ids, 1.0, out)
+    assert torch.equal(out, table[V - T:])
+    dy = rnd(gen(2), T, D, dtype=BF16)
+    table[300_000:300_010] = 5.0
+    fp8.fp8_embedding_bwd(dy, ids, 2.0, table, ws_of(fp8.fp8_embedding_bwd_workspace_bytes(T, V, D)))
+    assert torch.equal(table[V - T:], (dy.float() * 2).to(BF16)) and not table[:V - T].any()
+    # layer norm over the same memory: V rows, the last ones looked at
+    table[V - 3:] = rnd(gen(3), 3, D, dtype=BF16)
+    gamma, beta = 1 + 0.1 * rnd(gen(4), D), rnd(gen(5), D)
+    mean, rstd = torch.empty(V, device="cuda"), torch.empty(V, device="cuda")
+    y = torch.empty_like(table)
+    fp8.fp8_layernorm_fwd(table, gamma, beta, 1e-5, y, mean=mean, rstd=rstd)
+    want, mu, rs, size = ln_reference(table[V - 3:], gamma, beta, float(np.float32(1e-5)))
+    within(y[V - 3:], want, HALF[BF16] * want.abs() + 240 * U * size * (1 + 2 ** -7))
+    assert (y[12345] == beta.to(BF16)).all()
+    dg, db = torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    y.zero_()
+    y[V - 3:] = 1.0                                                              # the upstream gradient: the last rows only
+    wdx, wsize, *_ = ln_backward_reference(y[V - 3:], table[V - 3:], gamma, mean[V - 3:], rstd[V - 3:])
+    fp8.fp8_layernorm_bwd(y, table, gamma, mean, rstd, y, dg, db, ws_of(fp8.fp8_layernorm_bwd_workspace_bytes(V, D)))
+    within(y[V - 3:], wdx, HALF[BF16] * wdx.abs() + 96 * U * wsize * (1 + 2 ** -7))
+    assert not y[:V - 3].any() and (db == 3.0).all()
+    # one gradient of 2.4 G elements
+    flat = table.view(-1)
+    flat.zero_()
+    flat[-5:] = 3.0
+    items = fp8.fp8_grad_items([flat])
+    norm = norm_of(items)
+    assert abs(norm.item() - math.sqrt(45)) <= 19 * U * math.sqrt(45)
+    fp8.fp8_grad_clip(items, norm, 1.0)
+    assert (flat[-5:].float() - 3 / math.sqrt(45)).abs().max() <= 2 ** -8 * 0.45 + 1e-6 and not flat[:-5].any()
 
 
 # ------------------------------------------------------------------------------------------------ arguments

@@ -45,6 +45,9 @@ CASES = [
     ("fp8_embedding_fwd", EMB_FWD, dict(V=(1 << 30) + 1), SHAPE),
     ("fp8_embedding_fwd", EMB_FWD, dict(table=A + 8), ALIGN),
     ("fp8_embedding_fwd", EMB_FWD, dict(ids=A + 4), ALIGN),
+    ("fp8_embedding_fwd", EMB_FWD, dict(ids=A + 8), None),
+    ("fp8_embedding_fwd", EMB_FWD, dict(ids=A + 4, i64=0), None),
+    ("fp8_embedding_fwd", EMB_FWD, dict(ids=A + 2, i64=0), ALIGN),
     ("fp8_embedding_fwd", EMB_FWD, dict(out=A + 2), ALIGN),
     ("fp8_embedding_fwd_q", EMB_FWD_Q, {}, None),
     ("fp8_embedding_fwd_q", EMB_FWD_Q, dict(out=None), None),
@@ -95,7 +98,9 @@ CASES = [
     ("fp8_moe_route", ROUTE, dict(T=0), SHAPE),
     ("fp8_moe_route", ROUTE, dict(T=(1 << 26) + 1), SHAPE),
     ("fp8_moe_route", ROUTE, dict(bal=NAN), SHAPE),
-    ("fp8_moe_route", ROUTE, dict(weight=A + 4), ALIGN),
+    ("fp8_moe_route", ROUTE, dict(weight=A + 4), None),
+    ("fp8_moe_route", ROUTE, dict(weight=A + 2), ALIGN),
+    ("fp8_moe_route", ROUTE, dict(logits=A + 8), ALIGN),
     ("fp8_moe_route", ROUTE, dict(nws=0), WORKSPACE),
     ("fp8_moe_route_bwd", ROUTE_BWD, {}, None),
     ("fp8_moe_route_bwd", ROUTE_BWD, dict(expert=None), NULL),
@@ -121,6 +126,14 @@ def items(*entries):
     for i, e in enumerate(entries):
         arr[i] = binding.GradItem(*e)
     return arr, len(entries)
+
+
+def test_lists_of_gradients_are_checked():
+    import torch
+    with pytest.raises(ValueError):
+        binding.fp8_grad_items([torch.zeros(8)])                 # not on a GPU
+    with pytest.raises(ValueError):
+        binding.fp8_grad_items([])
 
 
 def test_gradient_clip_refusals(lib):
