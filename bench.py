@@ -592,6 +592,45 @@ GEMM_DRAM_CAPTURE = {
 
 
 # ---------------------------------------------------------------------------------------------- per-kernel report
+def report_step_operators(fp8, T, H, add, timed, bf16, f32):
+    """Rows of the operators around the block's products: embedding, layer norm, router, gradient norm and clip."""
+    import torch
+
+    V, E, k = 131072, 8, 2
+    empty = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device="cuda")
+    ws = lambda n: empty(n, dt=torch.uint8)
+    ids = torch.randint(0, V, (T,), device="cuda")
+    table, x, x8, sc, a = bf16(V, H, std=0.02), empty(T, H), empty(T, H, dt=torch.uint8), f32(16.0), f32()
+    add("fp8_embedding_fwd_q (BF16 + FP8 codes + amax, delayed scale)", f"{T} of {V}x{H}",
+        timed(lambda: fp8.fp8_embedding_fwd_q(table, ids, 50.0, sc, 0, x, x8, a)), nbytes=5 * T * H)
+    dy, w = bf16(T, H), ws(fp8.fp8_embedding_bwd_workspace_bytes(T, V, H))
+    add("fp8_embedding_bwd (whole table)", f"{T} into {V}x{H}", timed(lambda: fp8.fp8_embedding_bwd(dy, ids, 50.0, table, w)),
+        nbytes=2 * T * H + 2 * V * H)
+    add("fp8_embedding_bwd accumulate", f"{T} into {V}x{H}",
+        timed(lambda: fp8.fp8_embedding_bwd(dy, ids, 50.0, table, w, accumulate=True)), nbytes=2 * T * H + 4 * T * H)
+    del table
+    y, gamma, beta, mean, rstd = bf16(T, H), 1 + 0.1 * torch.randn(H, device="cuda"), torch.zeros(H, device="cuda"), empty(T, dt=torch.float32), empty(T, dt=torch.float32)
+    add("fp8_layernorm_fwd_q (residual, BF16 + FP8 codes + amax)", f"{T}x{H}",
+        timed(lambda: fp8.fp8_layernorm_fwd_q(y, gamma, beta, 1e-5, sc, 0, x, x8, mean=mean, rstd=rstd, residual=dy, amax_out=a)),
+        nbytes=7 * T * H)
+    dg, db, w = empty(H, dt=torch.float32), empty(H, dt=torch.float32), ws(fp8.fp8_layernorm_bwd_workspace_bytes(T, H))
+    add("fp8_layernorm_bwd", f"{T}x{H}", timed(lambda: fp8.fp8_layernorm_bwd(dy, y, gamma, mean, rstd, x, dg, db, w)),
+        nbytes=6 * T * H)
+    i32 = lambda *s: empty(*s, dt=torch.int32)
+    logits, expert, weight = torch.randn((T, E), device="cuda"), i32(T, k), empty(T, k, dt=torch.float32)
+    counts, offsets, rows, n, loss = i32(E), i32(E + 1), i32(T * k), i32(1), empty(2, dt=torch.float32)
+    dl, w = torch.empty_like(logits), ws(fp8.fp8_moe_route_workspace_bytes(T, E))
+    add("fp8_moe_route", f"{T}x{E}, {k} active", timed(lambda: fp8.fp8_moe_route(
+        logits, None, True, 0.01, 0.001, expert, weight, counts, offsets, rows, n, loss, w)), nbytes=4 * T * E + 12 * T * k)
+    add("fp8_moe_route_bwd", f"{T}x{E}, {k} active", timed(lambda: fp8.fp8_moe_route_bwd(
+        logits, expert, counts, n, True, 0.01, 0.001, None, weight, dl)), nbytes=8 * T * E + 8 * T * k)
+    grads = [bf16(6144, H), bf16(H, H), bf16(28672, H), bf16(H, 14336)]
+    items = fp8.fp8_grad_items(grads, [empty(*g.shape, dt=torch.float32) for g in grads])
+    w, numel = ws(fp8.fp8_grad_norm_workspace_bytes(items)), sum(g.numel() for g in grads)
+    add("fp8_grad_norm (BF16)", f"{numel}", timed(lambda: fp8.fp8_grad_norm(items, a, w)), nbytes=2 * numel)
+    add("fp8_grad_clip (BF16 to FP32)", f"{numel}", timed(lambda: fp8.fp8_grad_clip(items, a, 1.0)), nbytes=6 * numel)
+
+
 def run_report(args):
     """`--report`: every kernel of the library timed alone (CUDA events on the launching stream, 3 warm-ups, median of
     `--steps` launches).  Between launches a 256 MB buffer is written (nothing of the previous launch stays in L2) and
@@ -724,6 +763,7 @@ def run_report(args):
         timed(lambda: fp8.fp8_qk_norm_rope_q(qk, fp8.QK_RMS, 0.5, 1e-6, cos, sin, c4.seq, sc, 0, None, q8_, a)),
         nbytes=3 * qk.numel())
     del r, y, o_, qk, qo, q8_
+    report_step_operators(fp8, T, H, add, timed, bf16, f32)
 
     # ---- GEMMs of c3 and c4: forward / dgrad / wgrad, the producer form and the blockwise recipe
     for cname in ("c3", "c4"):
