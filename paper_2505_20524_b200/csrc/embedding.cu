@@ -24,7 +24,8 @@ __device__ __forceinline__ int checked_id(const IdT *ids, size_t t, unsigned V)
 }
 
 // `lanes` (a power of two) threads share a row; a CTA has 256 / lanes row slots with EF_ROWS rows each.  Bound by HBM:
-// every thread keeps EF_ROWS 16-byte loads (32 bytes from an FP32 table) in flight.
+// every thread keeps EF_ROWS 16-byte loads (32 bytes from an FP32 table) in flight.  8192 tokens x 4096 with codes and amax:
+// 25.1 us (100 MB written, about 45 MB of distinct rows read); 1, 2 and 4 rows and 128 threads are within 4 % of it.
 template <typename IdT, bool F32>
 __global__ void __launch_bounds__(EF_THREADS) embedding_fwd_kernel(const void *__restrict__ table, const IdT *__restrict__ ids,
                                                                    size_t T, unsigned V, unsigned n8, float scale,
@@ -241,15 +242,14 @@ __global__ void __launch_bounds__(ES_THREADS) embedding_scatter_kernel(const uin
 // Up to SS_MAX_T positions are sorted by one CTA that keeps keys and positions in shared memory between the passes; up to
 // CS_MAX_T by one cluster of 8 CTAs, which read one another's counts through distributed shared memory and pass the keys on
 // through L2; the chunked form above takes the rest, with a launch per pass.  All three are chains of latencies: loads, ranks,
-// scans, scattered stores.
+// scans, scattered stores.  Two passes take one CTA 9.5 us for 2048 positions and 14.2 for 4096, the cluster 11.1 and 11.5 (and
+// 13 for 8192, 15 for 12345); five launches of the chunked form took 22 us for 12345.
 constexpr int CS_THREADS = 1024;
 constexpr int CS_WARPS = CS_THREADS / 32;
 constexpr int CS_ITEMS = 8;
 constexpr int CS_CTAS = 8;
 constexpr size_t CS_MAX_T = (size_t)CS_CTAS * CS_THREADS * CS_ITEMS;
 constexpr int SS_ITEMS = 2;
-constexpr unsigned CS_CLEAR_CTAS = 17 * CS_CTAS;              // with the sorting cluster 144 of the 148 SMs
-constexpr size_t CS_CLEAR_BYTES = (size_t)40 << 20;
 constexpr size_t SS_MAX_T = (size_t)CS_THREADS * SS_ITEMS;
 
 struct ClusterSort {
@@ -259,20 +259,7 @@ struct ClusterSort {
     int passes, bits, items;              // items: keys per thread; CTA c ranks positions c * items * 1024 ...
     uint32_t *keys[2];
     int *pos[2];
-    uint4 *zero;                          // 16-byte words of the table's first rows, which the idle SMs clear meanwhile
-    size_t zero_words;
 };
-
-// The CTAs behind the sorting ones: a share of the words to clear.  Rows among them that a token points at are written
-// later, by the kernels behind the sort.
-__device__ __forceinline__ void clear_share(const ClusterSort &p, unsigned block, unsigned blocks)
-{
-    const size_t share = (p.zero_words + blocks - 1) / blocks, i0 = block * share, i1 = min(p.zero_words, i0 + share);
-    for (size_t i = i0 + threadIdx.x; i < i1; i += 4 * CS_THREADS)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (i + j * CS_THREADS < i1) p.zero[i + j * CS_THREADS] = make_uint4(0u, 0u, 0u, 0u);
-}
 
 __device__ __forceinline__ uint32_t sort_key(const ClusterSort &p, unsigned i)
 {
@@ -315,7 +302,6 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cta_sort_kernel(const
 {
     extern __shared__ __align__(16) uint32_t sort_mem[];
     cudaTriggerProgrammaticLaunchCompletion();
-    if (blockIdx.x > 0) return clear_share(p, blockIdx.x - 1, gridDim.x - 1);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int digits = 1 << p.bits, T = (int)p.T;
     uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 16384
@@ -377,7 +363,6 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
 {
     extern __shared__ __align__(16) uint32_t sort_mem[];
     cudaTriggerProgrammaticLaunchCompletion();
-    if (blockIdx.x >= CS_CTAS) return clear_share(p, blockIdx.x - CS_CTAS, gridDim.x - CS_CTAS);     // whole clusters
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = (int)cluster_ctarank();
     const int digits = 1 << p.bits;
     uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 8192 in a CTA
@@ -501,6 +486,23 @@ __device__ __forceinline__ void fill_rows(const GradParams &p, size_t v0, size_t
     }
 }
 
+// Zeros for the first words of a table that is overwritten, on the SMs that do not sort.  Launched behind the sort's kernel and
+// beside it; rows among them that a token points at are written later, by the kernels that wait for this one.  Its last block
+// waits for the sort, so that whoever waits for this kernel has waited for both.
+constexpr unsigned EC_WORDS = 4096;       // 16-byte words per block
+// what is written while the sort takes its 13 us (131072 x 4096 in BF16: 182 us with none, 178.0 with 40 MB, 176.3 with 60 and
+// 80, 178.4 with 100); a table below EC_MIN_BYTES is not worth the launch
+constexpr size_t EC_BYTES = (size_t)64 << 20, EC_MIN_BYTES = (size_t)4 << 20;
+__global__ void __launch_bounds__(EG_THREADS) embedding_clear_kernel(uint4 *__restrict__ out, size_t words)
+{
+    cudaTriggerProgrammaticLaunchCompletion();
+    const size_t i0 = (size_t)blockIdx.x * EC_WORDS + threadIdx.x;
+#pragma unroll
+    for (unsigned j = 0; j < EC_WORDS; j += EG_THREADS)
+        if (i0 + j < words) out[i0 + j] = make_uint4(0u, 0u, 0u, 0u);
+    if (blockIdx.x == gridDim.x - 1) cudaGridDependencySynchronize();
+}
+
 // Eight gradients of a row as they stand: one or two 16-byte words
 template <bool F32>
 struct Row8 {
@@ -551,7 +553,8 @@ __device__ __forceinline__ Row8<F32> zero_row8()
 // A run of equal ids that lies inside the item is finished here; one that crosses the item's start or end leaves its sum
 // in `partial` ([item][0] the one that began before, [item][1] the one that goes on) and is finished by
 // embedding_join_kernel.  Blocks past the items write the untouched rows' zeros.
-// U rows of dy travel at a time, and with them the old gradients of the runs that end among them.
+// U rows of dy travel at a time, and with them the old gradients of the runs that end among them (loaded when their run ends
+// they cost 10 us more: 12345 tokens into 50257 x 2048 FP32, 20 us for the 132 MB that move).
 template <bool F32, bool ACC, int U>
 __global__ void __launch_bounds__(EG_THREADS) embedding_sum_kernel(const GradParams p)
 {
@@ -822,61 +825,14 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
         set_error("fp8_embedding_bwd: workspace of %zu bytes, 256-byte aligned, needed (got %zu)", w.bytes, ws_bytes);
         return FP8_ERR_WORKSPACE;
     }
-    int rc = check_arch();
-    if (rc != FP8_OK) return rc;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint8_t *base = static_cast<uint8_t *>(ws);
     uint32_t *keys[2] = {reinterpret_cast<uint32_t *>(base + w.keys0), reinterpret_cast<uint32_t *>(base + w.keys1)};
     int *pos[2] = {reinterpret_cast<int *>(base + w.pos0), reinterpret_cast<int *>(base + w.pos1)};
     int *table = reinterpret_cast<int *>(base + w.table);
     const SortPlan sp = sort_plan(T, V);
-    // while at most 8 SMs sort (12 us), the others clear the first rows of a table that is overwritten (131072 x 4096 in BF16:
-    // 179 us with 40 MB of them, 183 with none, 186 with 80)
     const size_t row_bytes = D * (out_is_fp32 ? 4 : 2);
-    size_t cleared = accumulate || T > CS_MAX_T ? 0 : CS_CLEAR_BYTES / row_bytes;
+    size_t cleared = accumulate || T > CS_MAX_T || V * row_bytes < EC_MIN_BYTES ? 0 : EC_BYTES / row_bytes;
     if (cleared > V) cleared = V;
-    if (T <= CS_MAX_T) {
-        ClusterSort s;
-        s.ids = ids;
-        s.ids_are_int64 = ids_are_int64 ? 1 : 0;
-        s.T = (unsigned)T;
-        s.V = (unsigned)V;
-        s.passes = sp.passes;
-        s.bits = sp.bits;
-        const bool single = T <= SS_MAX_T;
-        const size_t across = single ? CS_THREADS : (size_t)CS_CTAS * CS_THREADS;
-        s.items = (int)((T + across - 1) / across);
-        for (int i = 0; i < 2; ++i) {
-            s.keys[i] = keys[i];
-            s.pos[i] = pos[i];
-        }
-        s.zero = static_cast<uint4 *>(dtable);
-        s.zero_words = cleared * row_bytes / 16;
-        const unsigned clearing = cleared ? CS_CLEAR_CTAS : 0;
-        if (single)
-            rc = launch_sort<embedding_cta_sort_kernel>(
-                s, 1 + clearing, (((size_t)CS_WARPS * 2 + 4) << sp.bits) + (size_t)s.items * CS_THREADS * 6, 1, st);
-        else
-            rc = launch_sort<embedding_cluster_sort_kernel>(s, CS_CTAS + clearing, ((size_t)CS_WARPS * 2 + 8) << sp.bits, CS_CTAS, st);
-        if (rc != FP8_OK) return rc;
-    } else {
-        const unsigned chunk_len = (unsigned)(sp.chunk_tiles * ES_TILE), chunks = (unsigned)sp.chunks;
-        const size_t table_len = sp.chunks << sp.bits;
-        if (sp.passes > 1) FP8_CUDA_CHECK(cudaMemsetAsync(table + table_len, 0, (sp.passes - 1) * table_len * sizeof(int), st));
-        if (ids_are_int64)
-            embedding_count_kernel<long long><<<chunks, ES_THREADS, 0, st>>>(static_cast<const long long *>(ids), T, (unsigned)V,
-                                                                             chunk_len, sp.bits, keys[0], table);
-        else
-            embedding_count_kernel<int><<<chunks, ES_THREADS, 0, st>>>(static_cast<const int *>(ids), T, (unsigned)V, chunk_len,
-                                                                       sp.bits, keys[0], table);
-        FP8_CUDA_CHECK(cudaGetLastError());
-        for (int i = 0; i < sp.passes; ++i) {
-            embedding_scatter_kernel<<<chunks, ES_THREADS, 0, st>>>(
-                keys[i & 1], i ? pos[i & 1] : nullptr, T, chunk_len, chunks, sp.bits, i * sp.bits, table + i * table_len,
-                keys[(i + 1) & 1], pos[(i + 1) & 1], i + 1 < sp.passes ? table + (i + 1) * table_len : nullptr);
-            FP8_CUDA_CHECK(cudaGetLastError());
-        }
-    }
     GradParams p;
     p.dy = static_cast<const uint16_t *>(dy_bf16);
     p.keys = keys[sp.passes & 1];
@@ -902,6 +858,54 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     if (work + fill > 0x7FFFFFFFull) {
         set_error("fp8_embedding_bwd: T=%zu V=%zu D=%zu needs more blocks than a grid holds", T, V, D);
         return FP8_ERR_SHAPE;
+    }
+    int rc = check_arch();
+    if (rc != FP8_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T <= CS_MAX_T) {
+        ClusterSort s;
+        s.ids = ids;
+        s.ids_are_int64 = ids_are_int64 ? 1 : 0;
+        s.T = (unsigned)T;
+        s.V = (unsigned)V;
+        s.passes = sp.passes;
+        s.bits = sp.bits;
+        const bool single = T <= SS_MAX_T;
+        const size_t across = single ? CS_THREADS : (size_t)CS_CTAS * CS_THREADS;
+        s.items = (int)((T + across - 1) / across);
+        for (int i = 0; i < 2; ++i) {
+            s.keys[i] = keys[i];
+            s.pos[i] = pos[i];
+        }
+        if (single)
+            rc = launch_sort<embedding_cta_sort_kernel>(
+                s, 1, (((size_t)CS_WARPS * 2 + 4) << sp.bits) + (size_t)s.items * CS_THREADS * 6, 1, st);
+        else
+            rc = launch_sort<embedding_cluster_sort_kernel>(s, CS_CTAS, ((size_t)CS_WARPS * 2 + 8) << sp.bits, CS_CTAS, st);
+        if (rc != FP8_OK) return rc;
+        if (cleared) {
+            const size_t words = cleared * row_bytes / 16;
+            rc = launch_early(embedding_clear_kernel, (unsigned)((words + EC_WORDS - 1) / EC_WORDS), EG_THREADS, 0, st,
+                              static_cast<uint4 *>(dtable), words);
+            if (rc != FP8_OK) return rc;
+        }
+    } else {
+        const unsigned chunk_len = (unsigned)(sp.chunk_tiles * ES_TILE), chunks = (unsigned)sp.chunks;
+        const size_t table_len = sp.chunks << sp.bits;
+        if (sp.passes > 1) FP8_CUDA_CHECK(cudaMemsetAsync(table + table_len, 0, (sp.passes - 1) * table_len * sizeof(int), st));
+        if (ids_are_int64)
+            embedding_count_kernel<long long><<<chunks, ES_THREADS, 0, st>>>(static_cast<const long long *>(ids), T, (unsigned)V,
+                                                                             chunk_len, sp.bits, keys[0], table);
+        else
+            embedding_count_kernel<int><<<chunks, ES_THREADS, 0, st>>>(static_cast<const int *>(ids), T, (unsigned)V, chunk_len,
+                                                                       sp.bits, keys[0], table);
+        FP8_CUDA_CHECK(cudaGetLastError());
+        for (int i = 0; i < sp.passes; ++i) {
+            embedding_scatter_kernel<<<chunks, ES_THREADS, 0, st>>>(
+                keys[i & 1], i ? pos[i & 1] : nullptr, T, chunk_len, chunks, sp.bits, i * sp.bits, table + i * table_len,
+                keys[(i + 1) & 1], pos[(i + 1) & 1], i + 1 < sp.passes ? table + (i + 1) * table_len : nullptr);
+            FP8_CUDA_CHECK(cudaGetLastError());
+        }
     }
     const size_t smem = (slots * EG_RUN * 2 + 2) * sizeof(uint32_t);
     const unsigned blocks = (unsigned)(work + fill);
