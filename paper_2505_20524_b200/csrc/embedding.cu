@@ -239,34 +239,101 @@ __global__ void __launch_bounds__(ES_THREADS) embedding_scatter_kernel(const uin
     sort_scatter(keys, pos_in, T, chunk_len, chunks, blockIdx.x, bits, shift, table, keys_out, pos_out, next_table);
 }
 
-// Up to SS_MAX_T positions are sorted by one CTA that keeps keys and positions in shared memory between the passes; up to
-// CS_MAX_T by one cluster of 8 CTAs, which read one another's counts through distributed shared memory and pass the keys on
-// through L2; the chunked form above takes the rest, with a launch per pass.  All three are chains of latencies: loads, ranks,
-// scans, scattered stores.  Two passes take one CTA 9.5 us for 2048 positions and 14.2 for 4096, the cluster 11.1 and 11.5 (and
-// 13 for 8192, 15 for 12345); five launches of the chunked form took 22 us for 12345.
+// Up to ER_MAX_T positions find their places by counting: position i comes behind every j with a smaller key, and behind every
+// j < i with the same.  A CTA counts for 32 positions, one to a lane; its 8 warps share the keys among them.  No step waits for
+// another CTA, and all SMs take part: T^2 comparisons in 3.7 us for 1024 positions, 4.2 for 2048 and 6.2 for 4096, where the
+// cluster below takes 10.7, 10.9 and 11.2; with more positions than 32 per SM it falls behind (64 to a CTA, 8192: 14.5 against 11.4).
+constexpr int ER_THREADS = 256;
+constexpr int ER_WARPS = ER_THREADS / 32;
+constexpr int ER_TILE = 256;              // keys that a warp stages at a time
+constexpr size_t ER_MAX_T = 32 * 148;
+
+struct RankIds {
+    const void *ids;
+    unsigned T, V;
+    uint32_t *keys;                       // out, in order
+    int *pos;
+};
+template <typename IdT>
+__device__ __forceinline__ uint32_t id_key(const void *ids, unsigned V, unsigned i)
+{
+    const int id = checked_id(static_cast<const IdT *>(ids), i, V);
+    return id < 0 ? V : (uint32_t)id;
+}
+
+template <typename IdT>
+__global__ void __launch_bounds__(ER_THREADS) embedding_rank_kernel(const RankIds p)
+{
+    __shared__ __align__(16) uint32_t tile[ER_WARPS][2][ER_TILE];
+    __shared__ int counts[ER_WARPS][32];
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned p0 = blockIdx.x * 32, i = p0 + lane;
+    const uint32_t mine = i < p.T ? id_key<IdT>(p.ids, p.V, i) : 0u;
+    int cnt = 0;
+    // the warp's keys: tiles warp, warp + 8, ...; the next one is on its way while one is compared
+    uint32_t next[ER_TILE / 32];
+    const auto fetch = [&](unsigned j0) {
+#pragma unroll
+        for (int m = 0; m < ER_TILE / 32; ++m) {
+            const unsigned j = j0 + m * 32 + lane;
+            next[m] = j < p.T ? id_key<IdT>(p.ids, p.V, j) : 0xFFFFFFFFu;
+        }
+    };
+    fetch(warp * ER_TILE);
+    int buffer = 0;
+    for (unsigned j0 = warp * ER_TILE; j0 < p.T; j0 += ER_WARPS * ER_TILE, buffer ^= 1) {
+        uint32_t *keys = tile[warp][buffer];
+#pragma unroll
+        for (int m = 0; m < ER_TILE / 32; ++m) keys[m * 32 + lane] = next[m];
+        __syncwarp();
+        fetch(j0 + ER_WARPS * ER_TILE);
+        if (j0 + ER_TILE <= p0 || j0 >= p0 + 32) {                // all before the CTA's positions, or all behind them
+            const uint32_t below = mine + (j0 < p0 ? 1u : 0u);
+#pragma unroll 8
+            for (int q = 0; q < ER_TILE / 4; ++q) {
+                const uint4 k = *reinterpret_cast<const uint4 *>(keys + 4 * q);
+                cnt += (k.x < below ? 1 : 0) + (k.y < below ? 1 : 0) + (k.z < below ? 1 : 0) + (k.w < below ? 1 : 0);
+            }
+        } else {
+            const int at = (int)i - (int)j0;                      // the lane's own place in the tile
+#pragma unroll 4
+            for (int q = 0; q < ER_TILE / 4; ++q) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(keys + 4 * q);
+                const uint32_t k[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cnt += k[e] < mine + (4 * q + e < at ? 1u : 0u) ? 1 : 0;
+            }
+        }
+    }
+    counts[warp][lane] = cnt;
+    __syncthreads();
+    if (warp == 0 && i < p.T) {
+        int rank = 0;
+#pragma unroll
+        for (int w = 0; w < ER_WARPS; ++w) rank += counts[w][lane];
+        p.keys[rank] = mine;
+        p.pos[rank] = (int)i;
+    }
+}
+
+// Up to CS_MAX_T positions are sorted by one cluster of 8 CTAs, which read one another's counts through distributed shared memory
+// and pass the keys on through L2; the chunked form above takes the rest, with a launch per pass.  Both are chains of latencies:
+// loads, ranks, scans, scattered stores (two passes: 11.4 us for 8192 positions, 14.4 for 12345; five launches of the chunked
+// form took 22 us for 12345, one CTA that sorts alone 41).
 constexpr int CS_THREADS = 1024;
 constexpr int CS_WARPS = CS_THREADS / 32;
 constexpr int CS_ITEMS = 8;
 constexpr int CS_CTAS = 8;
 constexpr size_t CS_MAX_T = (size_t)CS_CTAS * CS_THREADS * CS_ITEMS;
-constexpr int SS_ITEMS = 2;
-constexpr size_t SS_MAX_T = (size_t)CS_THREADS * SS_ITEMS;
 
 struct ClusterSort {
     const void *ids;
-    int ids_are_int64;
     unsigned T, V;
     int passes, bits, items;              // items: keys per thread; CTA c ranks positions c * items * 1024 ...
     uint32_t *keys[2];
     int *pos[2];
 };
-
-__device__ __forceinline__ uint32_t sort_key(const ClusterSort &p, unsigned i)
-{
-    const int id = p.ids_are_int64 ? checked_id(static_cast<const long long *>(p.ids), i, p.V)
-                                   : checked_id(static_cast<const int *>(p.ids), i, p.V);
-    return id < 0 ? p.V : (uint32_t)id;
-}
 
 // Sum over the threads before this one, of the CTA's 1024 (`warp_sum`: CS_WARPS entries).  Ends with a barrier behind its reads.
 __device__ __forceinline__ int scan_before(int v, int *warp_sum)
@@ -298,60 +365,6 @@ __device__ __forceinline__ int starts_of_warps(uint16_t *cnt, int digits)
     return at;
 }
 
-__global__ void __launch_bounds__(CS_THREADS, 1) embedding_cta_sort_kernel(const ClusterSort p)
-{
-    extern __shared__ __align__(16) uint32_t sort_mem[];
-    cudaTriggerProgrammaticLaunchCompletion();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int digits = 1 << p.bits, T = (int)p.T;
-    uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 16384
-    int *base = reinterpret_cast<int *>(cnt + CS_WARPS * digits);                 // [digits]
-    uint32_t *skey = reinterpret_cast<uint32_t *>(base + digits);                 // [items * 1024]
-    uint16_t *spos = reinterpret_cast<uint16_t *>(skey + p.items * CS_THREADS);   // [items * 1024]
-    __shared__ int warp_sum[CS_WARPS];
-    uint16_t *my_cnt = cnt + warp * digits;
-    const int first = warp * 32 * p.items + lane;
-    for (int pass = 0; pass < p.passes; ++pass) {
-        const int shift = pass * p.bits;
-        for (int d = lane; d < digits / 2; d += 32) reinterpret_cast<uint32_t *>(my_cnt)[d] = 0u;
-        uint32_t key[SS_ITEMS], pr[SS_ITEMS];                                     // pr: position and, above 16 bits, rank
-#pragma unroll
-        for (int j = 0; j < SS_ITEMS; ++j) {
-            const int i = first + 32 * j;
-            if (j >= p.items || i >= T) continue;
-            key[j] = pass == 0 ? sort_key(p, i) : skey[i];
-            pr[j] = pass == 0 ? (uint32_t)i : spos[i];
-        }
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < SS_ITEMS; ++j) {
-            if (j >= p.items) continue;
-            const int r = warp_stable_rank(first + 32 * j < T ? (int)((key[j] >> shift) & (digits - 1)) : -1, p.bits, my_cnt, lane);
-            if (first + 32 * j < T) pr[j] |= (uint32_t)r << 16;
-        }
-        __syncthreads();
-        const int total = tid < digits ? starts_of_warps(cnt, digits) : 0;
-        const int before = scan_before(total, warp_sum);
-        if (tid < digits) base[tid] = before;
-        __syncthreads();
-        const bool last = pass + 1 == p.passes;
-#pragma unroll
-        for (int j = 0; j < SS_ITEMS; ++j) {
-            if (j >= p.items || first + 32 * j >= T) continue;
-            const int d = (key[j] >> shift) & (digits - 1);
-            const int to = base[d] + my_cnt[d] + (int)(pr[j] >> 16);
-            if (last) {
-                p.keys[p.passes & 1][to] = key[j];
-                p.pos[p.passes & 1][to] = (int)(pr[j] & 0xFFFFu);
-            } else {
-                skey[to] = key[j];
-                spos[to] = (uint16_t)pr[j];
-            }
-        }
-        __syncthreads();
-    }
-}
-
 __device__ __forceinline__ int load_cluster_int(uint32_t saddr, int cta)
 {
     int v;
@@ -359,6 +372,7 @@ __device__ __forceinline__ int load_cluster_int(uint32_t saddr, int cta)
     return v;
 }
 
+template <typename IdT>
 __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(const ClusterSort p)
 {
     extern __shared__ __align__(16) uint32_t sort_mem[];
@@ -383,7 +397,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
             pos[j] = -1;
             if (j < p.items && i < p.T) {
                 if (pass == 0) {
-                    key[j] = sort_key(p, i);
+                    key[j] = id_key<IdT>(p.ids, p.V, i);
                     pos[j] = (int)i;
                 } else {
                     key[j] = __ldcg(p.keys[pass & 1] + i);
@@ -689,26 +703,25 @@ static GradWs grad_ws(size_t T, size_t V, size_t D)
 }
 
 constexpr int EMB_MAX_SHARED = 160 * 1024;          // the sorts: counts of 32 warps x 1024 digits (68 KB) and the keys
-// A sort: `cluster` CTAs to a cluster (1: none)
-template <auto Kernel>
-static int launch_sort(const ClusterSort &p, unsigned grid, size_t smem, unsigned cluster, cudaStream_t st)
+template <typename IdT>
+static int launch_cluster_sort(const ClusterSort &p, size_t smem, cudaStream_t st)
 {
     if (smem > 40 * 1024) {
-        const int rc = allow_shared<Kernel>(EMB_MAX_SHARED);
+        const int rc = allow_shared<embedding_cluster_sort_kernel<IdT>>(EMB_MAX_SHARED);
         if (rc != FP8_OK) return rc;
     }
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(grid);
+    c.gridDim = dim3(CS_CTAS);
     c.blockDim = dim3(CS_THREADS);
     c.dynamicSmemBytes = smem;
     c.stream = st;
     cudaLaunchAttribute a[1];
     a[0].id = cudaLaunchAttributeClusterDimension;
-    a[0].val.clusterDim.x = cluster;
+    a[0].val.clusterDim.x = CS_CTAS;
     a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
     c.attrs = a;
-    c.numAttrs = cluster > 1 ? 1 : 0;
-    FP8_CUDA_CHECK(cudaLaunchKernelEx(&c, Kernel, p));
+    c.numAttrs = 1;
+    FP8_CUDA_CHECK(cudaLaunchKernelEx(&c, embedding_cluster_sort_kernel<IdT>, p));
     return FP8_OK;
 }
 template <bool F32, bool ACC, int U>
@@ -863,26 +876,28 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     if (rc != FP8_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (T <= CS_MAX_T) {
-        ClusterSort s;
-        s.ids = ids;
-        s.ids_are_int64 = ids_are_int64 ? 1 : 0;
-        s.T = (unsigned)T;
-        s.V = (unsigned)V;
-        s.passes = sp.passes;
-        s.bits = sp.bits;
-        const bool single = T <= SS_MAX_T;
-        const size_t across = single ? CS_THREADS : (size_t)CS_CTAS * CS_THREADS;
-        s.items = (int)((T + across - 1) / across);
-        for (int i = 0; i < 2; ++i) {
-            s.keys[i] = keys[i];
-            s.pos[i] = pos[i];
+        if (T <= ER_MAX_T) {
+            const RankIds s = {ids, (unsigned)T, (unsigned)V, keys[sp.passes & 1], pos[sp.passes & 1]};
+            const unsigned grid = (unsigned)((T + 31) / 32);
+            if (ids_are_int64) embedding_rank_kernel<long long><<<grid, ER_THREADS, 0, st>>>(s);
+            else embedding_rank_kernel<int><<<grid, ER_THREADS, 0, st>>>(s);
+            FP8_CUDA_CHECK(cudaGetLastError());
+        } else {
+            ClusterSort s;
+            s.ids = ids;
+            s.T = (unsigned)T;
+            s.V = (unsigned)V;
+            s.passes = sp.passes;
+            s.bits = sp.bits;
+            s.items = (int)((T + CS_CTAS * CS_THREADS - 1) / (CS_CTAS * CS_THREADS));
+            for (int i = 0; i < 2; ++i) {
+                s.keys[i] = keys[i];
+                s.pos[i] = pos[i];
+            }
+            const size_t smem = ((size_t)CS_WARPS * 2 + 8) << sp.bits;
+            rc = ids_are_int64 ? launch_cluster_sort<long long>(s, smem, st) : launch_cluster_sort<int>(s, smem, st);
+            if (rc != FP8_OK) return rc;
         }
-        if (single)
-            rc = launch_sort<embedding_cta_sort_kernel>(
-                s, 1, (((size_t)CS_WARPS * 2 + 4) << sp.bits) + (size_t)s.items * CS_THREADS * 6, 1, st);
-        else
-            rc = launch_sort<embedding_cluster_sort_kernel>(s, CS_CTAS, ((size_t)CS_WARPS * 2 + 8) << sp.bits, CS_CTAS, st);
-        if (rc != FP8_OK) return rc;
         if (cleared) {
             const size_t words = cleared * row_bytes / 16;
             rc = launch_early(embedding_clear_kernel, (unsigned)((words + EC_WORDS - 1) / EC_WORDS), EG_THREADS, 0, st,

@@ -96,6 +96,7 @@ EMB_BWD = [  # T, V, D, id pattern
     (2048, 1024, 8, "random"), (2049, 1023, 8, "random"), (700, 300, 4104, "zipf"), (2000, (1 << 20) - 1, 8, "zipf"),
     (3000, (1 << 20) - 1, 8, "zipf"), (66000, (1 << 20) - 1, 8, "zipf"), (16384, 512, 16, "same"), (65536, 513, 8, "sorted"),
     (65537, 513, 8, "runs32"),
+    (4736, 700, 16, "zipf"), (4737, 700, 16, "zipf"), (257, 30, 8, "same"), (2049, 9, 8, "runs32"),
     (3000, 40000, 1024, "zipf"), (100, 70000, 264, "random"), (2100, 2500, 1024, "random"),      # first rows cleared apart: part, all
 ]
 
