@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(ES_THREADS) embedding_scatter_kernel(const uin
 // Up to ER_MAX_T positions find their places by counting: position i comes behind every j with a smaller key, and behind every
 // j < i with the same.  A CTA counts for 32 positions, one to a lane; its 8 warps share the keys among them.  No step waits for
 // another CTA, and all SMs take part: T^2 comparisons in 3.7 us for 1024 positions, 4.2 for 2048 and 6.2 for 4096, where the
-// cluster below takes 10.7, 10.9 and 11.2; with more positions than 32 per SM it falls behind (64 to a CTA, 8192: 14.5 against 11.4).
+// cluster below takes 8.5 to 9.2; with more positions than 32 per SM it falls behind (64 to a CTA, 8192: 14.5 against 9.5).
 constexpr int ER_THREADS = 256;
 constexpr int ER_WARPS = ER_THREADS / 32;
 constexpr int ER_TILE = 256;              // keys that a warp stages at a time
@@ -317,10 +317,10 @@ __global__ void __launch_bounds__(ER_THREADS) embedding_rank_kernel(const RankId
     }
 }
 
-// Up to CS_MAX_T positions are sorted by one cluster of 8 CTAs, which read one another's counts through distributed shared memory
-// and pass the keys on through L2; the chunked form above takes the rest, with a launch per pass.  Both are chains of latencies:
-// loads, ranks, scans, scattered stores (two passes: 11.4 us for 8192 positions, 14.4 for 12345; five launches of the chunked
-// form took 22 us for 12345, one CTA that sorts alone 41).
+// Up to CS_MAX_T positions are sorted by one cluster of 8 CTAs, which read one another's counts and hand the keys on through
+// distributed shared memory; the chunked form above takes the rest, with a launch per pass.  Both are chains of latencies:
+// loads, ranks, scans, scattered stores (two passes: 9.5 us for 8192 positions, 12.5 for 12345, 2 us more when the keys pass
+// through L2; five launches of the chunked form took 22 us for 12345, one CTA that sorts alone 41).
 constexpr int CS_THREADS = 1024;
 constexpr int CS_WARPS = CS_THREADS / 32;
 constexpr int CS_ITEMS = 8;
@@ -331,8 +331,8 @@ struct ClusterSort {
     const void *ids;
     unsigned T, V;
     int passes, bits, items;              // items: keys per thread; CTA c ranks positions c * items * 1024 ...
-    uint32_t *keys[2];
-    int *pos[2];
+    uint32_t *keys;                       // out, in order
+    int *pos;
 };
 
 // Sum over the threads before this one, of the CTA's 1024 (`warp_sum`: CS_WARPS entries).  Ends with a barrier behind its reads.
@@ -372,6 +372,13 @@ __device__ __forceinline__ int load_cluster_int(uint32_t saddr, int cta)
     return v;
 }
 
+__device__ __forceinline__ void store_cluster(uint32_t saddr, unsigned cta, uint32_t v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(saddr, cta)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 template <typename IdT>
 __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(const ClusterSort p)
 {
@@ -382,6 +389,9 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
     uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 8192 in a CTA
     int *tot = reinterpret_cast<int *>(cnt + CS_WARPS * digits);                  // [digits]: this CTA's keys per digit
     int *base = tot + digits;                                                     // [digits]
+    const unsigned held = (unsigned)p.items * CS_THREADS;                         // places of the order that a CTA holds
+    uint32_t *skey = reinterpret_cast<uint32_t *>(base + digits);                 // [held]: keys between the passes
+    int *spos = reinterpret_cast<int *>(skey + held);                             // [held]: their positions
     __shared__ int warp_sum[CS_WARPS];
     uint16_t *my_cnt = cnt + warp * digits;
     const unsigned first = ((unsigned)cta * CS_WARPS + warp) * 32u * p.items + lane;
@@ -400,8 +410,8 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
                     key[j] = id_key<IdT>(p.ids, p.V, i);
                     pos[j] = (int)i;
                 } else {
-                    key[j] = __ldcg(p.keys[pass & 1] + i);
-                    pos[j] = __ldcg(p.pos[pass & 1] + i);
+                    key[j] = skey[i - cta * held];
+                    pos[j] = spos[i - cta * held];
                 }
             }
         }
@@ -425,17 +435,24 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
         const int before = scan_before(total, warp_sum);
         if (tid < digits) base[tid] = before + mine;
         __syncthreads();
-        uint32_t *keys_out = p.keys[(pass + 1) & 1];
-        int *pos_out = p.pos[(pass + 1) & 1];
+        const bool last = pass + 1 == p.passes;
+        if (last) cluster_arrive();             // done with the others' `tot`
 #pragma unroll
         for (int j = 0; j < CS_ITEMS; ++j) {
             if (j >= p.items || pos[j] < 0) continue;
             const int d = (key[j] >> shift) & (digits - 1);
-            const int to = base[d] + my_cnt[d] + rank[j];
-            keys_out[to] = key[j];
-            pos_out[to] = pos[j];
+            const unsigned to = base[d] + my_cnt[d] + rank[j];
+            if (last) {
+                p.keys[to] = key[j];
+                p.pos[to] = pos[j];
+            } else {
+                const unsigned there = (to / CS_THREADS) / (unsigned)p.items;     // the CTA that holds this place
+                store_cluster(smem_u32(skey + (to - there * held)), there, key[j]);
+                store_cluster(smem_u32(spos + (to - there * held)), there, (uint32_t)pos[j]);
+            }
         }
-        cluster_sync_all();                     // the stores above, and everybody's reads of `tot`
+        if (last) cluster_wait();               // nobody leaves while its `tot` may be read
+        else cluster_sync_all();                // the stores above, and everybody's reads of `tot`
     }
 }
 
@@ -504,7 +521,7 @@ __device__ __forceinline__ void fill_rows(const GradParams &p, size_t v0, size_t
 // beside it; rows among them that a token points at are written later, by the kernels that wait for this one.  Its last block
 // waits for the sort, so that whoever waits for this kernel has waited for both.
 constexpr unsigned EC_WORDS = 4096;       // 16-byte words per block
-// what is written while the sort takes its 13 us (131072 x 4096 in BF16: 182 us with none, 178.0 with 40 MB, 176.3 with 60 and
+// what is written while the sort takes its 10 us (131072 x 4096 in BF16: 182 us with none, 178.0 with 40 MB, 176.3 with 60 and
 // 80, 178.4 with 100); a table below EC_MIN_BYTES is not worth the launch
 constexpr size_t EC_BYTES = (size_t)64 << 20, EC_MIN_BYTES = (size_t)4 << 20;
 __global__ void __launch_bounds__(EG_THREADS) embedding_clear_kernel(uint4 *__restrict__ out, size_t words)
@@ -890,11 +907,9 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
             s.passes = sp.passes;
             s.bits = sp.bits;
             s.items = (int)((T + CS_CTAS * CS_THREADS - 1) / (CS_CTAS * CS_THREADS));
-            for (int i = 0; i < 2; ++i) {
-                s.keys[i] = keys[i];
-                s.pos[i] = pos[i];
-            }
-            const size_t smem = ((size_t)CS_WARPS * 2 + 8) << sp.bits;
+            s.keys = keys[sp.passes & 1];
+            s.pos = pos[sp.passes & 1];
+            const size_t smem = (((size_t)CS_WARPS * 2 + 8) << sp.bits) + (size_t)s.items * CS_THREADS * 8;
             rc = ids_are_int64 ? launch_cluster_sort<long long>(s, smem, st) : launch_cluster_sort<int>(s, smem, st);
             if (rc != FP8_OK) return rc;
         }
