@@ -768,6 +768,56 @@ def test_calls_go_to_the_given_stream_and_into_a_graph():
         assert all(torch.equal(t, v) for t, v in zip(outputs, want2))
 
 
+def test_calls_on_one_workspace_in_order_and_on_two_at_once():
+    """Calls back to back on one stream may share a workspace; calls on two streams with a workspace each run at once."""
+    V, D, E, k = 3000, 320, 40, 4
+    sizes = [5000, 700, 9000, 33, 5000, 4737]                   # every order of the ids up to 65536, one behind the other
+    g = gen(61)
+    data = []
+    for T in sizes:
+        x = rnd(g, T, D, dtype=BF16)
+        mu = x.float().mean(1)
+        data.append(dict(T=T, ids=pattern(g, T, V, "zipf"), x=x, dy=rnd(g, T, D, dtype=BF16), logits=rnd(g, T, E), mean=mu,
+                         rstd=(x.float() - mu[:, None]).square().mean(1).rsqrt()))
+    gamma = 1 + 0.1 * rnd(g, D)
+    most = max(sizes)
+
+    def scratch():
+        return [ws_of(n) for n in (max(fp8.fp8_embedding_bwd_workspace_bytes(T, V, D) for T in sizes),
+                                   max(fp8.fp8_layernorm_bwd_workspace_bytes(T, D) for T in sizes),
+                                   fp8.fp8_moe_route_workspace_bytes(most, E), 1 << 16)]
+
+    def calls(d, w, stream=None):
+        T = d["T"]
+        dtable, dx, dg, db, norm = torch.empty((V, D), device="cuda"), torch.empty_like(d["x"]), torch.empty(D, device="cuda"), torch.empty(D, device="cuda"), scalar(0)
+        r, dl = route_outputs(T, E, k), torch.empty_like(d["logits"])
+        s = dict(stream=stream)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())     # the fills of the outputs
+        fp8.fp8_embedding_bwd(d["dy"], d["ids"], 1.5, dtable, w[0], **s)
+        fp8.fp8_layernorm_bwd(d["dy"], d["x"], gamma, d["mean"], d["rstd"], dx, dg, db, w[1], **s)
+        fp8.fp8_moe_route(d["logits"], None, True, CB, CZ, r["expert"], r["weight"], r["counts"], r["offsets"], r["rows"],
+                          r["n_routed"], r["loss"], w[2], **s)
+        fp8.fp8_moe_route_bwd(d["logits"], r["expert"], r["counts"], r["n_routed"], True, CB, CZ, None, None, dl, **s)
+        items = fp8.fp8_grad_items([dtable, dg, db])
+        fp8.fp8_grad_norm(items, norm, w[3], **s)
+        fp8.fp8_grad_clip(items, norm, 0.7, **s)
+        return [dtable, dx, dg, db, norm, dl, *r.values()]
+
+    want = []
+    for d in data:
+        want.append(calls(d, scratch()))
+        torch.cuda.synchronize()
+    w = scratch()
+    got = [calls(d, w) for d in data]                            # nothing waits between them
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o, v in zip(got, want) for a, b in zip(o, v))
+    streams, ws = [torch.cuda.Stream() for _ in range(2)], [scratch(), scratch()]
+    got = [calls(d, ws[i % 2], streams[i % 2]) for i, d in enumerate(data)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o, v in zip(got, want) for a, b in zip(o, v))
+
+
 def test_a_training_step_around_the_fp8_products():
     """Token ids to clipped gradients through the package's own calls: embedding with codes, FP8 linear layer, layer norm with
     residual, its backward, the linear layer's gradients, the table's gradient, norm and clip; the gradients against a 64-bit
