@@ -332,8 +332,8 @@ FP8_API int fp8_linear_wgrad_blockwise(const uint8_t *dY8, const uint8_t *X8, co
  * fp8_embedding_fwd_q: the producer form under delayed scaling: also out8 = FP8cast(*q_scale * out) of the BF16-rounded
  * values (bit-identical to fp8_cast of out_bf16); out_bf16 may be NULL when only the codes are wanted.
  * fp8_embedding_bwd: dtable[v, :] (+)= scale * sum over t with ids[t] = v of dy[t, :], dy [T, D] BF16, dtable [V, D] BF16 or
- * FP32.  Sums are FP32 in ascending t within runs of 32 equal ids and then over the runs in order, rounded once: the
- * result is the same from call to call.  Without `accumulate` every row is overwritten (zeros where no token points);
+ * FP32.  Sums are FP32 in a fixed order (ascending t within stretches of the positions sorted by id, then over the
+ * stretches), rounded once: the result is the same from call to call.  Without `accumulate` every row is overwritten (zeros where no token points);
  * with it only the rows that a token points at are read and written.  Ids outside [0, V) contribute nothing.
  * ws: scratch of fp8_embedding_bwd_workspace_bytes(T, V, D), 256-byte aligned, contents need no preparation; calls that
  * share it must be ordered.  D % 8 == 0, D <= 2^20, T and V <= 2^30.  ids need the alignment of their own type only.  Outputs

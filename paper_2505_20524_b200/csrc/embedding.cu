@@ -127,8 +127,9 @@ static SortPlan sort_plan(size_t T, size_t V)
 template <typename IdT>
 __global__ void __launch_bounds__(ES_THREADS) embedding_count_kernel(const IdT *__restrict__ ids, size_t T, unsigned V,
                                                                      unsigned chunk_len, int bits, uint32_t *__restrict__ keys,
-                                                                     int *__restrict__ table)
+                                                                     int *__restrict__ table, int *__restrict__ split_count)
 {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *split_count = 0;
     __shared__ int cnt[ES_MAX_DIGITS];
     const int digits = 1 << bits;
     for (int d = threadIdx.x; d < digits; d += ES_THREADS) cnt[d] = 0;
@@ -253,6 +254,7 @@ struct RankIds {
     unsigned T, V;
     uint32_t *keys;                       // out, in order
     int *pos;
+    int *split_count;                     // set to zero for the kernels behind
 };
 template <typename IdT>
 __device__ __forceinline__ uint32_t id_key(const void *ids, unsigned V, unsigned i)
@@ -268,6 +270,7 @@ __global__ void __launch_bounds__(ER_THREADS) embedding_rank_kernel(const RankId
     __shared__ int counts[ER_WARPS][32];
     cudaTriggerProgrammaticLaunchCompletion();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.split_count = 0;
     const unsigned p0 = blockIdx.x * 32, i = p0 + lane;
     const uint32_t mine = i < p.T ? id_key<IdT>(p.ids, p.V, i) : 0u;
     int cnt = 0;
@@ -333,6 +336,7 @@ struct ClusterSort {
     int passes, bits, items;              // items: keys per thread; CTA c ranks positions c * items * 1024 ...
     uint32_t *keys;                       // out, in order
     int *pos;
+    int *split_count;                     // set to zero for the kernels behind
 };
 
 // Sum over the threads before this one, of the CTA's 1024 (`warp_sum`: CS_WARPS entries).  Ends with a barrier behind its reads.
@@ -386,6 +390,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
     cudaTriggerProgrammaticLaunchCompletion();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = (int)cluster_ctarank();
     const int digits = 1 << p.bits;
+    if (cta == 0 && tid == 0) *p.split_count = 0;
     uint16_t *cnt = reinterpret_cast<uint16_t *>(sort_mem);                       // [CS_WARPS][digits]: at most 8192 in a CTA
     int *tot = reinterpret_cast<int *>(cnt + CS_WARPS * digits);                  // [digits]: this CTA's keys per digit
     int *base = tot + digits;                                                     // [digits]
@@ -458,8 +463,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) embedding_cluster_sort_kernel(c
 
 // ---------------------------------------------------------------- gradient: sums
 constexpr int EG_THREADS = 256;
-constexpr int EG_RUN = 32;          // sorted positions per work item (16: the same time, twice the sums to join)
-constexpr int EG_JOIN = 8;          // partial sums in flight per thread
+constexpr unsigned EG_JOIN_BLOCKS = 148 * 8;
 constexpr int EG_FILL_ROWS = 4096;  // rows of the table per filling block, at most
 
 struct GradParams {
@@ -471,6 +475,9 @@ struct GradParams {
     float scale;
     void *dtable;
     int is_fp32, accumulate, lanes_log2;
+    int run_log2;                    // sorted positions per work item
+    int *split_count;                // the runs that go on from the item they begin in to the next: how many,
+    uint2 *split;                    // and (item, id) of each
     float *partial;                  // [items][2][D]: sums of the item's first and last run where they cross its ends
     size_t items, item_blocks, col_blocks;
     size_t fill_rows, fill_from;     // rows of the table per filling block, and the first of them
@@ -580,10 +587,10 @@ __device__ __forceinline__ Row8<F32> zero_row8()
     return r;
 }
 
-// Work item: EG_RUN neighbouring sorted positions, for the columns of one thread group (`lanes` threads, 8 columns each).
+// Work item: 2^run_log2 neighbouring sorted positions, for the columns of one thread group (`lanes` threads, 8 columns each).
 // A run of equal ids that lies inside the item is finished here; one that crosses the item's start or end leaves its sum
 // in `partial` ([item][0] the one that began before, [item][1] the one that goes on) and is finished by
-// embedding_join_kernel.  Blocks past the items write the untouched rows' zeros.
+// embedding_join_kernel, which takes the runs from a list of the items that they begin in.  Blocks past the items write the untouched rows' zeros.
 // U rows of dy travel at a time, and with them the old gradients of the runs that end among them (loaded when their run ends
 // they cost 10 us more: 12345 tokens into 50257 x 2048 FP32, 20 us for the 132 MB that move).
 template <bool F32, bool ACC, int U>
@@ -598,24 +605,24 @@ __global__ void __launch_bounds__(EG_THREADS) embedding_sum_kernel(const GradPar
         fill_rows(p, v0, min((size_t)p.V, v0 + p.fill_rows));
         return;
     }
-    const int lanes = 1 << p.lanes_log2, slots = EG_THREADS >> p.lanes_log2, slot = threadIdx.x >> p.lanes_log2;
+    const int run = 1 << p.run_log2, lanes = 1 << p.lanes_log2, slots = EG_THREADS >> p.lanes_log2, slot = threadIdx.x >> p.lanes_log2;
     // the block's keys, one before and one behind them, and its positions
     uint32_t *skey = item_mem + 1;
-    int *spos = reinterpret_cast<int *>(item_mem + slots * EG_RUN + 2);
-    const size_t block0 = (blockIdx.x / p.col_blocks) * slots * EG_RUN;
-    for (int i = (int)threadIdx.x - 1; i <= slots * EG_RUN; i += EG_THREADS) {
+    int *spos = reinterpret_cast<int *>(item_mem + slots * run + 2);
+    const size_t block0 = (blockIdx.x / p.col_blocks) * slots * run;
+    for (int i = (int)threadIdx.x - 1; i <= slots * run; i += EG_THREADS) {
         const bool in = (i >= 0 || block0 > 0) && block0 + i < p.T;
         skey[i] = in ? __ldcg(p.keys + block0 + i) : 0xFFFFFFFFu;
-        if (in && i >= 0 && i < slots * EG_RUN) spos[i] = __ldcg(p.pos + block0 + i);
+        if (in && i >= 0 && i < slots * run) spos[i] = __ldcg(p.pos + block0 + i);
     }
     __syncthreads();
     const size_t item = (blockIdx.x / p.col_blocks) * slots + slot;
     const unsigned c = (unsigned)(blockIdx.x % p.col_blocks) * lanes + (threadIdx.x & (lanes - 1));
     if (item >= p.items || c >= p.n8) return;
-    const uint32_t *key = skey + slot * EG_RUN;
-    const int *pos = spos + slot * EG_RUN;
+    const uint32_t *key = skey + slot * run;
+    const int *pos = spos + slot * run;
     const uint32_t before = key[-1];                             // 0xFFFFFFFF in front of the first position
-    const int count = (int)min((size_t)EG_RUN, p.T - item * EG_RUN);
+    const int count = (int)min((size_t)run, p.T - item * run);
     const size_t D = (size_t)p.n8 * 8;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < count && key[i] < p.V; i += U) {         // ids outside the table are sorted behind the others
@@ -647,6 +654,7 @@ __global__ void __launch_bounds__(EG_THREADS) embedding_sum_kernel(const GradPar
                 float *o = p.partial + (item * 2 + (k == before ? 0 : 1)) * D + (size_t)c * 8;
                 *reinterpret_cast<float4 *>(o) = make_float4(acc[0], acc[1], acc[2], acc[3]);
                 *reinterpret_cast<float4 *>(o + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                if (c == 0 && k != before) p.split[atomicAdd(p.split_count, 1)] = make_uint2((unsigned)item, k);      // in any order
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
@@ -654,54 +662,76 @@ __global__ void __launch_bounds__(EG_THREADS) embedding_sum_kernel(const GradPar
     }
 }
 
-// The runs that cross items: the item in which such a run begins adds the following items' sums in order.
-template <bool F32>
-__global__ void __launch_bounds__(EG_THREADS) embedding_join_kernel(const GradParams p)
+// The runs that cross items.  A CTA takes a run and up to 128 lanes of its columns; its 256 / lanes thread groups share the
+// items that the run reaches (group g the g-th, g + groups-th, ..., J of them in flight), then add up in pairs: a fixed order,
+// whichever CTA it is.
+template <bool F32, int J>
+__global__ void __launch_bounds__(EG_THREADS) embedding_join_kernel(const GradParams p, int lanes_log2, unsigned col_blocks)
 {
+    __shared__ float4 red[2][EG_THREADS];
     cudaGridDependencySynchronize();
-    const int lanes = 1 << p.lanes_log2;
-    const size_t item = (blockIdx.x / p.col_blocks) * (EG_THREADS >> p.lanes_log2) + (threadIdx.x >> p.lanes_log2);
-    const unsigned c = (unsigned)(blockIdx.x % p.col_blocks) * lanes + (threadIdx.x & (lanes - 1));
-    if (item + 1 >= p.items || c >= p.n8) return;
-    const size_t i1 = (item + 1) * EG_RUN;
-    const uint32_t key = __ldcg(p.keys + i1 - 1);
-    if (key >= p.V || __ldcg(p.keys + i1) != key) return;                       // nothing goes on
-    const size_t i0 = item * EG_RUN;
-    if (__ldcg(p.keys + i0) == key && i0 > 0 && __ldcg(p.keys + i0 - 1) == key) return;   // it began earlier
-    const size_t D = (size_t)p.n8 * 8;
-    Row8<F32> old;
-    if (p.accumulate) old = load_row8<F32>(p, key, c);
-    const float *src = p.partial + (item * 2 + 1) * D + (size_t)c * 8;
-    const float4 a = __ldcg(reinterpret_cast<const float4 *>(src)), b = __ldcg(reinterpret_cast<const float4 *>(src) + 1);
-    float acc[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    // the following items that the run reaches, EG_JOIN of them in flight at a time (loads past the run's end are unused)
-    bool open = true;
-    for (size_t k = item + 1; open && k < p.items; k += EG_JOIN) {
-        float4 lo[EG_JOIN], hi[EG_JOIN];
-        uint32_t at[EG_JOIN];
-#pragma unroll
-        for (int j = 0; j < EG_JOIN; ++j) {
-            at[j] = 0xFFFFFFFFu;
-            if (k + j >= p.items) continue;
-            at[j] = __ldcg(p.keys + (k + j) * EG_RUN);
-            const float4 *q = reinterpret_cast<const float4 *>(p.partial + ((k + j) * 2) * D + (size_t)c * 8);
-            lo[j] = __ldcg(q);
-            hi[j] = __ldcg(q + 1);
+    const int lanes = 1 << lanes_log2, groups = EG_THREADS >> lanes_log2, group = threadIdx.x >> lanes_log2;
+    const size_t D = (size_t)p.n8 * 8, run = (size_t)1 << p.run_log2;
+    uint2 entry = __ldcg(p.split + blockIdx.x / col_blocks);     // on its way with the count; used if there are so many
+    const size_t pieces = (size_t)__ldcg(p.split_count) * col_blocks;
+    for (size_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        if (piece != blockIdx.x) entry = __ldcg(p.split + piece / col_blocks);
+        const size_t item = entry.x;
+        const uint32_t key = entry.y;
+        const unsigned c = (unsigned)(piece % col_blocks) * lanes + (threadIdx.x & (lanes - 1));
+        const bool in = c < p.n8;
+        Row8<F32> old = zero_row8<F32>();
+        float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (in && group == 0) {
+            if (p.accumulate) old = load_row8<F32>(p, key, c);
+            const float4 *q = reinterpret_cast<const float4 *>(p.partial + (item * 2 + 1) * D + (size_t)c * 8);
+            const float4 a = __ldcg(q), b = __ldcg(q + 1);
+            acc[0] = a.x; acc[1] = a.y; acc[2] = a.z; acc[3] = a.w; acc[4] = b.x; acc[5] = b.y; acc[6] = b.z; acc[7] = b.w;
         }
+        bool open = in;                                          // loads past the run's end are unused
+        for (size_t k = item + 1 + group; open && k < p.items; k += (size_t)J * groups) {
+            float4 lo[J], hi[J];
+            uint32_t at[J];
 #pragma unroll
-        for (int j = 0; j < EG_JOIN; ++j) {
-            open = open && at[j] == key;
-            if (!open) continue;
-            acc[0] += lo[j].x; acc[1] += lo[j].y; acc[2] += lo[j].z; acc[3] += lo[j].w;
-            acc[4] += hi[j].x; acc[5] += hi[j].y; acc[6] += hi[j].z; acc[7] += hi[j].w;
+            for (int j = 0; j < J; ++j) {
+                const size_t n = k + (size_t)j * groups;
+                at[j] = 0xFFFFFFFFu;
+                if (n >= p.items) continue;
+                at[j] = __ldcg(p.keys + n * run);
+                const float4 *q = reinterpret_cast<const float4 *>(p.partial + n * 2 * D + (size_t)c * 8);
+                lo[j] = __ldcg(q);
+                hi[j] = __ldcg(q + 1);
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                open = open && at[j] == key;
+                if (!open) continue;
+                acc[0] += lo[j].x; acc[1] += lo[j].y; acc[2] += lo[j].z; acc[3] += lo[j].w;
+                acc[4] += hi[j].x; acc[5] += hi[j].y; acc[6] += hi[j].z; acc[7] += hi[j].w;
+            }
         }
+        for (int half = groups / 2; half > 0; half /= 2) {
+            red[0][threadIdx.x] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            red[1][threadIdx.x] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+            __syncthreads();
+            if (group < half) {
+                const float4 a = red[0][threadIdx.x + half * lanes], b = red[1][threadIdx.x + half * lanes];
+                acc[0] += a.x; acc[1] += a.y; acc[2] += a.z; acc[3] += a.w;
+                acc[4] += b.x; acc[5] += b.y; acc[6] += b.z; acc[7] += b.w;
+            }
+            __syncthreads();
+        }
+        if (in && group == 0) store_row8<F32>(p, key, c, acc, old);
     }
-    store_row8<F32>(p, key, c, acc, p.accumulate ? old : zero_row8<F32>());
 }
 
 // ---------------------------------------------------------------- workspace of the gradient
+// Sorted positions per work item.  Rows of up to 64 columns take few threads: shorter items give them more groups to work at
+// once, and the join shares out the longer list of sums.  (Longer rows: 16 takes the same time as 32, with twice the sums.)
+static int eg_run_log2(size_t D) { return D <= 64 ? 3 : 5; }
+
 struct GradWs {
-    size_t keys0, keys1, pos0, pos1, table, partial, bytes;     // offsets
+    size_t keys0, keys1, pos0, pos1, table, split, partial, bytes;     // offsets
 };
 static GradWs grad_ws(size_t T, size_t V, size_t D)
 {
@@ -714,7 +744,9 @@ static GradWs grad_ws(size_t T, size_t V, size_t D)
     w.pos0 = at; at += up(T * 4);
     w.pos1 = at; at += up(T * 4);
     w.table = at; at += T <= CS_MAX_T ? 0 : up((size_t)sp.passes * sp.chunks * ((size_t)4 << sp.bits));
-    w.partial = at; at += up((T + EG_RUN - 1) / EG_RUN * 2 * D * sizeof(float));
+    const size_t items = ((T - 1) >> eg_run_log2(D)) + 1;
+    w.split = at; at += up((items + 1) * sizeof(uint2));
+    w.partial = at; at += up(items * 2 * D * sizeof(float));
     w.bytes = at;
     return w;
 }
@@ -876,7 +908,10 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     p.accumulate = accumulate ? 1 : 0;
     p.lanes_log2 = lanes_log2_for(p.n8, 8);
     p.partial = reinterpret_cast<float *>(base + w.partial);
-    p.items = (T + EG_RUN - 1) / EG_RUN;
+    p.run_log2 = eg_run_log2(D);
+    p.split_count = reinterpret_cast<int *>(base + w.split);
+    p.split = reinterpret_cast<uint2 *>(p.split_count) + 1;
+    p.items = ((T - 1) >> p.run_log2) + 1;
     const size_t slots = EG_THREADS >> p.lanes_log2;
     p.item_blocks = (p.items + slots - 1) / slots;
     p.col_blocks = (p.n8 + (1u << p.lanes_log2) - 1) >> p.lanes_log2;
@@ -894,7 +929,7 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (T <= CS_MAX_T) {
         if (T <= ER_MAX_T) {
-            const RankIds s = {ids, (unsigned)T, (unsigned)V, keys[sp.passes & 1], pos[sp.passes & 1]};
+            const RankIds s = {ids, (unsigned)T, (unsigned)V, keys[sp.passes & 1], pos[sp.passes & 1], p.split_count};
             const unsigned grid = (unsigned)((T + 31) / 32);
             if (ids_are_int64) embedding_rank_kernel<long long><<<grid, ER_THREADS, 0, st>>>(s);
             else embedding_rank_kernel<int><<<grid, ER_THREADS, 0, st>>>(s);
@@ -909,6 +944,7 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
             s.items = (int)((T + CS_CTAS * CS_THREADS - 1) / (CS_CTAS * CS_THREADS));
             s.keys = keys[sp.passes & 1];
             s.pos = pos[sp.passes & 1];
+            s.split_count = p.split_count;
             const size_t smem = (((size_t)CS_WARPS * 2 + 8) << sp.bits) + (size_t)s.items * CS_THREADS * 8;
             rc = ids_are_int64 ? launch_cluster_sort<long long>(s, smem, st) : launch_cluster_sort<int>(s, smem, st);
             if (rc != FP8_OK) return rc;
@@ -925,10 +961,10 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
         if (sp.passes > 1) FP8_CUDA_CHECK(cudaMemsetAsync(table + table_len, 0, (sp.passes - 1) * table_len * sizeof(int), st));
         if (ids_are_int64)
             embedding_count_kernel<long long><<<chunks, ES_THREADS, 0, st>>>(static_cast<const long long *>(ids), T, (unsigned)V,
-                                                                             chunk_len, sp.bits, keys[0], table);
+                                                                             chunk_len, sp.bits, keys[0], table, p.split_count);
         else
             embedding_count_kernel<int><<<chunks, ES_THREADS, 0, st>>>(static_cast<const int *>(ids), T, (unsigned)V, chunk_len,
-                                                                       sp.bits, keys[0], table);
+                                                                       sp.bits, keys[0], table, p.split_count);
         FP8_CUDA_CHECK(cudaGetLastError());
         for (int i = 0; i < sp.passes; ++i) {
             embedding_scatter_kernel<<<chunks, ES_THREADS, 0, st>>>(
@@ -937,14 +973,21 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
             FP8_CUDA_CHECK(cudaGetLastError());
         }
     }
-    const size_t smem = (slots * EG_RUN * 2 + 2) * sizeof(uint32_t);
+    const size_t smem = ((slots << p.run_log2) * 2 + 2) * sizeof(uint32_t);
     const unsigned blocks = (unsigned)(work + fill);
     if (p.is_fp32 && p.accumulate) rc = launch_sums<true, true, 4>(p, blocks, smem, st);
     else if (p.is_fp32) rc = launch_sums<true, false, 8>(p, blocks, smem, st);
     else if (p.accumulate) rc = launch_sums<false, true, 4>(p, blocks, smem, st);
     else rc = launch_sums<false, false, 8>(p, blocks, smem, st);
     if (rc != FP8_OK || p.items == 1) return rc;
-    if (p.is_fp32) rc = launch_early(embedding_join_kernel<true>, (unsigned)work, EG_THREADS, 0, st, p);
-    else rc = launch_early(embedding_join_kernel<false>, (unsigned)work, EG_THREADS, 0, st, p);
+    // narrow rows have a group for (almost) every item that a run reaches, wide ones few groups
+    const int jl = lanes_log2_for(p.n8, 7);
+    const unsigned cols = (p.n8 + (1u << jl) - 1) >> jl;
+    const size_t most = p.items * cols;
+    const unsigned grid = (unsigned)(most < EG_JOIN_BLOCKS ? most : EG_JOIN_BLOCKS);
+    if (p.is_fp32 && jl > 3) rc = launch_early(embedding_join_kernel<true, 8>, grid, EG_THREADS, 0, st, p, jl, cols);
+    else if (p.is_fp32) rc = launch_early(embedding_join_kernel<true, 2>, grid, EG_THREADS, 0, st, p, jl, cols);
+    else if (jl > 3) rc = launch_early(embedding_join_kernel<false, 8>, grid, EG_THREADS, 0, st, p, jl, cols);
+    else rc = launch_early(embedding_join_kernel<false, 2>, grid, EG_THREADS, 0, st, p, jl, cols);
     return rc;
 }
