@@ -140,7 +140,7 @@ __device__ __forceinline__ void local_best(const float (&score)[PL], float &best
         }
 }
 
-// Forward, first kernel.  G lanes per token (1 up to 16 experts, a warp above), PL experts per lane; the tokens of the CTA's
+// Forward, first kernel.  G lanes per token (1, or a warp), PL experts per lane; the tokens of the CTA's
 // chunk go to the groups in turn.  Bound by instruction issue and by the latency of the k maxima, which follow one another:
 // two warp reductions each (the largest score, the lowest expert that has it).
 template <bool F32, int G, int PL>
@@ -549,17 +549,24 @@ static size_t route_ctas(size_t T) { return (T + route_chunk(T) - 1) / route_chu
 
 using namespace fp8dpa;
 
-#define FP8DPA_ROUTE_DISPATCH(KERNEL, GRID, THREADS)                                 \
+// A lane per token (up to 16 experts) has a latency of its own, a warp per token one that grows with the tokens; one lane is
+// faster above these many tokens.  us with a lane and with a warp per token, FP32 logits:
+//   first forward kernel   E = 8: 4096 tokens 3.9, 3.4; 6144 3.9, 4.4    E = 16: 12288 7.1, 6.2; 16384 7.1, 7.4
+//   gradient               E = 8: 8192 5.1, 4.4; 12288 5.2, 5.5          E = 16: 24576 11.3, 8.4; 131072 24.5, 35.1
+static bool route_choose_by_lane(size_t T, int E) { return E <= 16 && T > (E <= 8 ? 4096 : 12288); }
+static bool route_bwd_by_lane(size_t T, int E) { return E <= 16 && T > (E <= 8 ? 8192 : 32768); }
+
+#define FP8DPA_ROUTE_DISPATCH(KERNEL, BY_LANE, GRID, THREADS)                        \
     do {                                                                             \
-        if (q.E <= 8) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 1, 8);                           \
-        else if (q.E <= 16) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 1, 16);                     \
-        else if (q.E <= 32) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 1);                     \
-        else if (q.E <= 64) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 2);                     \
-        else if (q.E <= 96) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 3);                     \
-        else if (q.E <= 128) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 4);                    \
-        else if (q.E <= 160) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 5);                    \
-        else if (q.E <= 192) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 6);                    \
-        else FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 8);                                    \
+        if (BY_LANE && q.E <= 8) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 1, 8);     \
+        else if (BY_LANE) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 1, 16);           \
+        else if (q.E <= 32) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 1);         \
+        else if (q.E <= 64) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 2);         \
+        else if (q.E <= 96) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 3);         \
+        else if (q.E <= 128) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 4);        \
+        else if (q.E <= 160) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 5);        \
+        else if (q.E <= 192) FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 6);        \
+        else FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, 32, 8);                        \
     } while (0)
 #define FP8DPA_ROUTE_TYPE(KERNEL, GRID, THREADS, G, PL)                              \
     do {                                                                             \
@@ -615,8 +622,9 @@ extern "C" int fp8_moe_route(const void *logits, int is_fp32, const float *bias,
     q.cta_z = reinterpret_cast<double *>(q.cta_probs + (size_t)q.ctas * q.stride);
     q.cta_n = reinterpret_cast<int *>(q.cta_z + q.ctas);
     // one thread per token: no more threads than the chunk has tokens
-    const unsigned threads = E > 16 ? RT_THREADS : (unsigned)(q.chunk < 512 ? (q.chunk + 31) & ~(size_t)31 : 512);
-    FP8DPA_ROUTE_DISPATCH(route_choose_kernel, q.ctas, threads);
+    const bool by_lane = route_choose_by_lane(T, E);
+    const unsigned threads = !by_lane ? RT_THREADS : (unsigned)(q.chunk < 512 ? (q.chunk + 31) & ~(size_t)31 : 512);
+    FP8DPA_ROUTE_DISPATCH(route_choose_kernel, by_lane, q.ctas, threads);
     FP8_CUDA_CHECK(cudaGetLastError());
     int quads_log2 = 0;
     while ((4 << quads_log2) < E) ++quads_log2;
@@ -646,11 +654,12 @@ extern "C" int fp8_moe_route_bwd(const void *logits, int is_fp32, const int *exp
     q.balance_coef = balance_coef; q.z_coef = z_coef;
     q.expert = const_cast<int *>(expert); q.counts_in = counts; q.n_in = n_routed; q.dloss = dloss; q.dweight = dweight;
     q.dlogits = dlogits;
-    const size_t groups = E <= 16 ? RT_BWD_THREADS : RT_BWD_THREADS / 32;
+    const bool by_lane = route_bwd_by_lane(T, E);
+    const size_t groups = by_lane ? RT_BWD_THREADS : RT_BWD_THREADS / 32;
     size_t blocks = (T + groups - 1) / groups;
     const size_t cap = (size_t)sm_count() * 8;
     if (blocks > cap) blocks = cap;
-    FP8DPA_ROUTE_DISPATCH(route_bwd_kernel, (unsigned)blocks, RT_BWD_THREADS);
+    FP8DPA_ROUTE_DISPATCH(route_bwd_kernel, by_lane, (unsigned)blocks, RT_BWD_THREADS);
     FP8_CUDA_CHECK(cudaGetLastError());
     return FP8_OK;
 }

@@ -184,7 +184,9 @@ def test_embedding_takes_slices_of_the_ids():
 
 # ------------------------------------------------------------------------------------------------ layer norm
 LN = [(1, 8), (5, 64), (9, 256), (17, 264), (33, 512), (7, 520), (65, 1024), (33, 1032), (3, 2048), (130, 2056), (70, 4096),
-      (11, 4104), (19, 8192), (6, 8200), (5, 16384), (1, 16376), (1200, 128), (700, 1536)]
+      (11, 4104), (19, 8192), (6, 8200), (5, 16384), (1, 16376), (1200, 128), (700, 1536),
+      # several rows to a warp: the last ones missing, lanes without columns, more than one turn of all warps
+      (1, 24), (6, 8), (700, 8), (63, 40), (130, 72), (33, 200), (1300, 248), (9001, 136), (250001, 8)]
 
 
 def ln_data(T, D, seed=0, offset=0.5):
@@ -400,7 +402,10 @@ def route(logits, bias, k, normalize, cb, cz, rows=True):
 
 
 ROUTE = [(1, 1, 1), (1, 2, 2), (5, 7, 3), (33, 8, 2), (4097, 8, 2), (100, 9, 9), (50, 16, 16), (129, 17, 4), (64, 32, 8), (65, 33, 5),
-         (300, 64, 6), (1000, 65, 1), (777, 128, 16), (40, 129, 8), (5001, 160, 6), (256, 256, 8), (2, 256, 16), (20000, 64, 2)]
+         (300, 64, 6), (1000, 65, 1), (777, 128, 16), (40, 129, 8), (5001, 160, 6), (256, 256, 8), (2, 256, 16), (20000, 64, 2),
+         # both sides of the sizes from which a lane takes a token
+         (4096, 8, 3), (8193, 1, 1), (9001, 8, 8), (8200, 5, 2), (12288, 16, 4), (12289, 16, 16), (12300, 11, 3), (32769, 16, 4),
+         (33001, 9, 2)]
 CB, CZ = float(np.float32(0.01)), float(np.float32(0.003))
 
 
