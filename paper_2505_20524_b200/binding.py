@@ -7,6 +7,7 @@ call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 
@@ -427,11 +428,16 @@ class GradItems:
         self.device = self.tensors[0][0].get_device()
         if self.device < 0:
             raise ValueError("expects CUDA tensors")
-        self.array = (GradItem * len(self.tensors[0]))()
-        for i, (g, o) in enumerate(zip(*self.tensors)):
-            self.array[i] = GradItem(_addr(f"grads[{i}]", g, _FLOATS, g.shape, self.device),
-                                     _addr(f"outs[{i}]", o, _FLOATS, g.shape, self.device), g.numel(), g.dtype is _F32,
-                                     o.dtype is _F32)
+        dev, words = self.device, []
+        for g, o in zip(*self.tensors):            # _addr's checks written out: 1 us per pair instead of 2.3
+            gt, ot, shape = g.dtype, o.dtype, g.shape
+            if not ((gt is _F32 or gt is _BF16) and (ot is _F32 or ot is _BF16) and o.shape == shape and g.is_contiguous()
+                    and o.is_contiguous() and g.get_device() == dev and o.get_device() == dev):
+                i = len(words) // 4
+                _addr(f"grads[{i}]", g, _FLOATS, shape, dev)
+                _addr(f"outs[{i}]", o, _FLOATS, shape, dev)
+            words += (g.data_ptr(), o.data_ptr(), shape.numel(), (gt is _F32) | (ot is _F32) << 32)
+        self.array = (GradItem * len(self.tensors[0])).from_buffer(array.array("Q", words))
 
     def __len__(self):
         return len(self.array)

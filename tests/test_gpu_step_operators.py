@@ -705,6 +705,11 @@ def test_python_side_checks():
         lambda: fp8.fp8_grad_items([]),
         lambda: fp8.fp8_grad_items([gb], [gb, gb]),
         lambda: fp8.fp8_grad_items([gb], [gb[:32]]),
+        lambda: fp8.fp8_grad_items([gb, gb.half()]),
+        lambda: fp8.fp8_grad_items([gb, gb], [gb, gb.double()]),
+        lambda: fp8.fp8_grad_items([gb, gb.cpu()]),
+        lambda: fp8.fp8_grad_items([gb[:32], gb[:32]], [gb[:32], gb[::2]]),
+        lambda: fp8.fp8_grad_items([gb[::2]]),
         lambda: fp8.fp8_grad_norm(fp8.fp8_grad_items([gb]), one.half(), ws_of(256)),
     ):
         with pytest.raises(ValueError):
