@@ -253,9 +253,9 @@ struct LnBwd {
 // layernorm_bwd_sum_kernel.  x and dout are read once, dx is written once.  A warp loads mean and rstd of 32 of its rows at a
 // time: when all CTAs read those of neighbouring rows one by one, the few lines that hold them were what bound the kernel
 // (8192 x 4096: 52.7 us).  Up to KG = 2 (8192 columns) xh, g and gamma stay in registers between the sums and dx (4000 x 8192:
-// 37 us, memory's 30); with KG = 4 xh and g are formed again from the ring and gamma lies behind it, and the one CTA per SM
-// that fits waits on its own sums (2048 x 16384: 63 us, memory's 31; a cluster per row, with two groups per thread, loses at
-// its barriers what it gains: 57 to 59, but 3000 x 12288 69 against 61).
+// 37 us, memory's 30); with KG = 4 xh and g are formed again from the ring and gamma lies behind it, with one CTA per SM
+// (2048 x 16384: 46 us, memory's 31; clusters of two and four CTAs per row with two groups per thread: 57 to 59, their
+// barriers cost more than the second look at the row).
 __host__ __device__ constexpr int ln_bwd_stages(int kg) { return kg > 2 ? 2 : 3; }
 constexpr size_t ln_bwd_shared(int kg, unsigned threads) { return (size_t)(ln_bwd_stages(kg) + (kg > 2)) * 2 * kg * 16 * threads; }
 template <int KG, LnUnit UNIT, int MAXT, int MINB>
@@ -346,9 +346,10 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_bwd_kernel(const LnBwd p
                 ring_get(ring_end + (2 * k) * per_k, gm[0][0], gm[0][1]);
                 ring_get(ring_end + (2 * k + 1) * per_k, gm[0][2], gm[0][3]);
             }
+            const uint64_t shift = in[k] ? minus_mu : 0ull;      // columns behind the row's: 0, whatever mean * rstd is
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                xh[kk][e] = mul_f32x2(add_f32x2(xh[kk][e], minus_mu), rs2);
+                xh[kk][e] = mul_f32x2(add_f32x2(xh[kk][e], shift), rs2);
                 ge[kk][e] = mul_f32x2(d[e], gm[kk][e]);
             }
         };

@@ -325,6 +325,24 @@ def test_layernorm_backward(T, D, accumulate):
         assert torch.equal(o, dx)
 
 
+@pytest.mark.parametrize("D", [8, 24, 72, 200, 264, 520, 1032, 4104, 8200])
+def test_layernorm_backward_where_mean_times_rstd_overflows(D):
+    """A constant row far out: x - mean is zero, and nothing of the columns that a row does not have may come in."""
+    g, x, gamma, _ = ln_data(5, D, seed=2)
+    x[1], x[4] = 2.0 ** 120, -2.0 ** 126
+    dout = rnd(g, 5, D, std=1e-2, dtype=BF16)
+    _, mu, rs, _ = ln_reference(x, gamma, gamma, 1e-5)
+    mean, rstd = mu.float(), rs.float()
+    assert mean[1] == 2.0 ** 120 and torch.isinf(mean[1] * rstd[1])
+    want, size, wg, sg, wb, sb = ln_backward_reference(dout, x, gamma, mean, rstd)
+    dx, dg, db = torch.empty_like(x), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    fp8.fp8_layernorm_bwd(dout, x, gamma, mean, rstd, dx, dg, db, ws_of(fp8.fp8_layernorm_bwd_workspace_bytes(5, D)))
+    # as in test_layernorm_backward: row sums of n = 64 terms, five rows
+    within(dx, want, HALF[BF16] * want.abs() + 96 * U * size * (1 + 2 ** -7))
+    within(dg, wg, 261 * U * sg)
+    within(db, wb, 257 * U * sb)
+
+
 def test_layernorm_gradient_against_differences():
     """Directional derivatives of sum(c * out) by central differences of the 64-bit forward, against the kernel's gradients."""
     T, D = 6, 96
