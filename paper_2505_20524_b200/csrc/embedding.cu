@@ -26,15 +26,28 @@ __device__ __forceinline__ int checked_id(const IdT *ids, size_t t, unsigned V)
 // `lanes` (a power of two) threads share a row; a CTA has 256 / lanes row slots with EF_ROWS rows each.  Bound by HBM:
 // every thread keeps EF_ROWS 16-byte loads (32 bytes from an FP32 table) in flight.  8192 tokens x 4096 with codes and amax:
 // 25.1 us (100 MB written, about 45 MB of distinct rows read); 1, 2 and 4 rows and 128 threads are within 4 % of it.
+struct EmbedFwd {
+    const void *table, *ids;
+    size_t T;
+    unsigned V, n8;
+    float scale;
+    uint16_t *out;
+    unsigned int *amax_bits;
+    const float *q_scale;
+    uint8_t *out8;
+    int fmt;
+};
 template <typename IdT, bool F32>
-__global__ void __launch_bounds__(EF_THREADS) embedding_fwd_kernel(const void *__restrict__ table, const IdT *__restrict__ ids,
-                                                                   size_t T, unsigned V, unsigned n8, float scale,
-                                                                   uint16_t *__restrict__ out,
-                                                                   unsigned int *__restrict__ amax_bits,
-                                                                   const float *__restrict__ q_scale,
-                                                                   uint8_t *__restrict__ out8, int fmt, int lanes_log2)
+__global__ void __launch_bounds__(EF_THREADS) embedding_fwd_kernel(const EmbedFwd p, int lanes_log2)
 {
-    const float qs = out8 ? __ldg(q_scale) : 1.0f;
+    const bool alone = amax_begin(p.amax_bits);
+    const void *__restrict__ table = p.table;
+    const IdT *__restrict__ ids = static_cast<const IdT *>(p.ids);
+    uint16_t *__restrict__ out = p.out;
+    uint8_t *__restrict__ out8 = p.out8;
+    const size_t T = p.T;
+    const unsigned V = p.V, n8 = p.n8;
+    const float scale = p.scale, qs = out8 ? __ldg(p.q_scale) : 1.0f;
     const int lane = threadIdx.x & ((1 << lanes_log2) - 1), slot = threadIdx.x >> lanes_log2;
     const int slots = EF_THREADS >> lanes_log2;
     const size_t row0 = (size_t)blockIdx.x * (slots * EF_ROWS) + slot;
@@ -88,11 +101,10 @@ __global__ void __launch_bounds__(EF_THREADS) embedding_fwd_kernel(const void *_
             for (int q = 0; q < 4; ++q) m = absmax2e(m, w[j][q]);
             const size_t at = t * n8 + c;
             if (out) reinterpret_cast<uint4 *>(out)[at] = make_uint4(w[j][0], w[j][1], w[j][2], w[j][3]);
-            if (out8) reinterpret_cast<uint2 *>(out8)[at] = bf16x8_to_fp8x8(w[j], qs, fmt);
+            if (out8) reinterpret_cast<uint2 *>(out8)[at] = bf16x8_to_fp8x8(w[j], qs, p.fmt);
         }
     }
-    cudaGridDependencySynchronize();
-    if (amax_bits) block_max_bf16_to(m, amax_bits);
+    amax_end(m, p.amax_bits, alone);
 }
 
 // ---------------------------------------------------------------- gradient: order of the tokens
@@ -827,11 +839,10 @@ static int embedding_fwd(const char *who, const void *table, int table_is_fp32, 
     const int ll = lanes_log2_for(n8, 8);
     const size_t per_block = (size_t)(EF_THREADS >> ll) * EF_ROWS;
     const unsigned blocks = (unsigned)((T + per_block - 1) / per_block);
-    uint16_t *o = static_cast<uint16_t *>(out_bf16);
-    unsigned int *ab = reinterpret_cast<unsigned int *>(amax_out);
+    const EmbedFwd p = {table, ids, T, (unsigned)V, n8, scale, static_cast<uint16_t *>(out_bf16),
+                        reinterpret_cast<unsigned int *>(amax_out), q_scale, out8, fmt};
 #define FP8DPA_LAUNCH_EF(IdT, F32) \
-    return launch_behind_amax(embedding_fwd_kernel<IdT, F32>, T * D, ab, blocks, EF_THREADS, 0, st, table, \
-                              static_cast<const IdT *>(ids), T, (unsigned)V, n8, scale, o, ab, q_scale, out8, fmt, ll)
+    return launch_behind_amax<embedding_fwd_kernel<IdT, F32>>(T * D, p.amax_bits, blocks, EF_THREADS, 0, st, p, ll)
     if (ids_are_int64) {
         if (table_is_fp32) FP8DPA_LAUNCH_EF(long long, true);
         else FP8DPA_LAUNCH_EF(long long, false);

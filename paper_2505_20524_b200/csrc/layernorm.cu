@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p
     if (UNIT == LN_WARP) lanes_log2 = 5;
     extern __shared__ __align__(16) uint4 ring_mem[];
     __shared__ __align__(16) float red[2][MAXT / 32];
+    const bool alone = amax_begin(p.amax_bits);
     const unsigned span = CTA ? blockDim.x : 1u << lanes_log2, lane = CTA ? threadIdx.x : threadIdx.x & (span - 1);
     const unsigned rows = CTA ? 1 : 32u >> lanes_log2, sub = CTA ? 0 : (threadIdx.x & 31) >> lanes_log2;    // rows at a time
     const size_t units = CTA ? gridDim.x : (size_t)gridDim.x * (blockDim.x >> 5);
@@ -227,8 +228,7 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p
         now += per_stage;
         if (now == ring_end) now = ring;
     }
-    cudaGridDependencySynchronize();
-    if (p.amax_bits) block_max_bf16_to(m, p.amax_bits);
+    amax_end(m, p.amax_bits, alone);
 }
 
 // ---------------------------------------------------------------- backward
@@ -531,7 +531,7 @@ static int ln_launch(const P &p, const LnShape &s, size_t smem, size_t most, uns
         const int rc = allow_shared<Kernel>((int)most);
         if (rc != FP8_OK) return rc;
     }
-    return launch_behind_amax(Kernel, p.T * p.n8 * 8, amax, s.grid, s.threads, smem, st, p, s.lanes_log2);
+    return launch_behind_amax<Kernel>(p.T * p.n8 * 8, amax, s.grid, s.threads, smem, st, p, s.lanes_log2);
 }
 
 template <int KG, LnUnit UNIT, bool RES, int MAXT, int MINB>

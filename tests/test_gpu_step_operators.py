@@ -271,6 +271,42 @@ def test_amax_of_large_outputs():
         assert a.item() == out.float().abs().max().item()
 
 
+@pytest.mark.parametrize("T,D", [(1, 8), (1, 16384), (8, 4096), (9, 4096), (16, 2048), (17, 2048), (8, 16384), (9, 16384), (129, 256),
+                                 (257, 256), (300, 8)])
+def test_amax_of_few_blocks(T, D):
+    """Grids that are one cluster, and those just above: eagerly, on two streams, replayed; stale values ignored, zero for zeros."""
+    g, x, gamma, beta = ln_data(T, D, seed=6)
+    table, ids = rnd(g, 50, D, std=0.02), token_ids(g, T, 50)
+    outs, amax = [torch.empty_like(x) for _ in range(2)], [scalar(1e30), scalar(1e30)]
+    run = [lambda: fp8.fp8_layernorm_fwd(x, gamma, beta, 1e-5, outs[0], amax_out=amax[0]),
+           lambda: fp8.fp8_embedding_fwd(table, ids, 50.0, outs[1], amax[1])]
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for f, s in zip(run, side):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                f()
+        torch.cuda.synchronize()
+        for o, a in zip(outs, amax):
+            assert a.item() == o.float().abs().max().item()
+            a.fill_(1e30)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for f in run:
+            f()
+    for scale in (0.25, 0.0):
+        x.mul_(scale)
+        table.mul_(scale)
+        if scale == 0.0:
+            beta.zero_()
+        for a in amax:
+            a.fill_(1e30)
+        graph.replay()
+        for o, a in zip(outs, amax):
+            assert a.item() == o.float().abs().max().item()
+    assert amax[0].item() == 0.0 and amax[1].item() == 0.0
+
+
 def test_layernorm_constant_rows_and_infinities():
     T, D = 3, 128
     x = torch.full((T, D), 2.5, dtype=BF16, device="cuda")
