@@ -457,6 +457,8 @@ def route(logits, bias, k, normalize, cb, cz, rows=True):
 
 ROUTE = [(1, 1, 1), (1, 2, 2), (5, 7, 3), (33, 8, 2), (4097, 8, 2), (100, 9, 9), (50, 16, 16), (129, 17, 4), (64, 32, 8), (65, 33, 5),
          (300, 64, 6), (1000, 65, 1), (777, 128, 16), (40, 129, 8), (5001, 160, 6), (256, 256, 8), (2, 256, 16), (20000, 64, 2),
+         # one kernel for few tokens, and the first size with two
+         (1, 256, 16), (31, 200, 7), (224, 40, 4), (224, 256, 16), (225, 40, 4), (223, 128, 5),
          # both sides of the sizes from which a lane takes a token
          (4096, 8, 3), (8193, 1, 1), (9001, 8, 8), (8200, 5, 2), (12288, 16, 4), (12289, 16, 16), (12300, 11, 3), (32769, 16, 4),
          (33001, 9, 2)]
