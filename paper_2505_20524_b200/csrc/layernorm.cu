@@ -123,12 +123,10 @@ enum LnUnit { LN_LANES, LN_WARP, LN_CTA };
 // zeros instead of branches, and a kernel without the residual's code took 33.5M elements from 27 to 34 us to 24 to 26.
 // With 50 to 64 KB per SM on their way memory does best, two rows ahead or, with a residual, one (8192 x 4096 with residual
 // and codes: 38.5 us; 42 with two).  rstd by rsqrtf, off by 2 ulp of FP32 at most.
-__host__ __device__ constexpr int ln_fwd_stages(bool res) { return res ? 2 : 3; }
-template <int KG, LnUnit UNIT, bool RES, int MAXT, int MINB>
+template <int KG, LnUnit UNIT, bool RES, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p, int lanes_log2)
 {
     constexpr bool CTA = UNIT == LN_CTA;
-    constexpr int STAGES = ln_fwd_stages(RES);
     if (UNIT == LN_WARP) lanes_log2 = 5;
     extern __shared__ __align__(16) uint4 ring_mem[];
     __shared__ __align__(16) float red[2][MAXT / 32];
@@ -534,23 +532,26 @@ static int ln_launch(const P &p, const LnShape &s, size_t smem, size_t most, uns
     return launch_behind_amax<Kernel>(p.T * p.n8 * 8, amax, s.grid, s.threads, smem, st, p, s.lanes_log2);
 }
 
-template <int KG, LnUnit UNIT, bool RES, int MAXT, int MINB>
+template <int KG, LnUnit UNIT, bool RES, int STAGES, int MAXT, int MINB>
 static int ln_fwd_launch(const LnFwd &p, const LnShape &s, cudaStream_t st)
 {
-    constexpr size_t per_thread = ln_fwd_stages(RES) * (RES ? 2 : 1) * KG * 16;
-    return ln_launch<layernorm_fwd_kernel<KG, UNIT, RES, MAXT, MINB>>(p, s, per_thread * s.threads, per_thread * MAXT,
-                                                                      p.amax_bits, st);
+    constexpr size_t per_thread = STAGES * (RES ? 2 : 1) * KG * 16;
+    return ln_launch<layernorm_fwd_kernel<KG, UNIT, RES, STAGES, MAXT, MINB>>(p, s, per_thread * s.threads, per_thread * MAXT,
+                                                                              p.amax_bits, st);
 }
 template <bool RES>
 static int ln_fwd_run(const LnFwd &p, size_t D, cudaStream_t st)
 {
+    constexpr int STAGES = RES ? 2 : 3;
     const LnShape s = ln_fwd_shape(p.T, D);
-    if (D <= 256) return ln_fwd_launch<2, LN_LANES, RES, 256, 3>(p, s, st);
-    if (D <= 512) return ln_fwd_launch<2, LN_WARP, RES, 256, 3>(p, s, st);
-    if (D <= 1024) return ln_fwd_launch<4, LN_WARP, RES, 256, 2>(p, s, st);
-    if (D <= 4096) return ln_fwd_launch<2, LN_CTA, RES, 256, 3>(p, s, st);
-    if (D <= 8192) return ln_fwd_launch<4, LN_CTA, RES, 256, 2>(p, s, st);
-    return ln_fwd_launch<4, LN_CTA, RES, 512, 1>(p, s, st);
+    if (D <= 256) return ln_fwd_launch<2, LN_LANES, RES, STAGES, 256, 3>(p, s, st);
+    if (D <= 512) return ln_fwd_launch<2, LN_WARP, RES, STAGES, 256, 3>(p, s, st);
+    if (D <= 1024) return ln_fwd_launch<4, LN_WARP, RES, STAGES, 256, 2>(p, s, st);
+    if (D <= 4096) return ln_fwd_launch<2, LN_CTA, RES, STAGES, 256, 3>(p, s, st);
+    if (D <= 8192) return ln_fwd_launch<4, LN_CTA, RES, STAGES, 256, 2>(p, s, st);
+    // one CTA of up to 384 threads per SM: with two stages too little travels (3000 x 10000 with codes: 42.0 us, 38.4 with three)
+    if (RES && D <= 12288) return ln_fwd_launch<4, LN_CTA, RES, 3, 384, 1>(p, s, st);
+    return ln_fwd_launch<4, LN_CTA, RES, STAGES, 512, 1>(p, s, st);
 }
 
 template <int KG, LnUnit UNIT, int MAXT, int MINB>
