@@ -88,8 +88,15 @@ template <int G> __device__ __forceinline__ float group_max(float v)
     return r;
 }
 
-// exp(x) for x <= 0 from the hardware's exp2 (relative error 2^-22, half a step of x log2 e on top)
-__device__ __forceinline__ float exp_neg(float x) { return ex2_approx(x * 1.4426950408889634f); }
+// exp(x) for x <= 0 from the hardware's exp2 (relative error 2^-22).  The rounding of t = x log2 e, and of log2 e itself, moves
+// the result by up to 1.5 |x| 2^-24 of itself: x - t ln 2, which one fma leaves with |x| 2^-28, is put back to first order.
+// Results below 2^-126 are 0; -200 in place of -inf keeps the correction a number.
+__device__ __forceinline__ float exp_neg(float x)
+{
+    x = fmaxf(x, -200.0f);
+    const float t = x * 1.4426950408889634f, e = ex2_approx(t);
+    return fmaf(e, fmaf(t, -0.6931471805599453f, x), e);
+}
 
 // What both passes need of a token: whether it is routed (a finite logit, nothing NaN or +inf), whether it is broken (NaN or
 // +inf), the maximum, the sum of exponentials and the probabilities.
@@ -101,15 +108,12 @@ struct Token {
 
     __device__ __forceinline__ void finish()
     {
-        float mx = -INFINITY;
-        bool bad = false;
+        float mx = l[0];                                   // NaN if a logit is
 #pragma unroll
-        for (int i = 0; i < PL; ++i) {
-            bad |= !(l[i] < INFINITY);
-            mx = fmaxf(mx, l[i]);
-        }
-        broken = G == 1 ? bad : __any_sync(0xffffffffu, bad);
-        top = group_max<G>(mx);
+        for (int i = 1; i < PL; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(mx) : "f"(l[i]));
+        if (G > 1) asm volatile("redux.sync.max.NaN.f32 %0, %0, 0xffffffff;" : "+f"(mx));
+        top = mx;
+        broken = !(top < INFINITY);
         routed = !broken && top > -INFINITY;
         const float from = routed ? top : 0.0f;
         float s = 0.0f;

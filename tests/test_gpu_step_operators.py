@@ -939,3 +939,21 @@ def test_a_training_step_around_the_fp8_products():
     assert c < 1
     for got, ref in zip((dw, dg, db, dtable), plain):
         assert torch.equal(got, ref * torch.tensor(c, device="cuda"))
+
+
+# ------------------------------------------------------------------------------------------------ router: exponentials, sizes
+@pytest.mark.parametrize("T,E", [(150, 2), (150, 8), (300, 40), (5000, 8), (13000, 16)])      # a warp per token in one launch and two; a lane
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("normalize", [False, True])
+def test_router_probabilities_far_below_the_largest(T, E, dt, normalize):
+    """A token's probabilities keep the digits of FP32 however small they are: logits 0 and -x, x up to 80."""
+    k = 2
+    logits = torch.full((T, E), -math.inf, device="cuda", dtype=dt)
+    x = torch.linspace(1.0, 80.0, T, device="cuda").to(dt)
+    logits[:, 0], logits[:, 1] = 0.0, -x
+    o = route(logits, None, k, normalize, 0.0, 0.0)
+    assert (o["expert"][:, 0] == 0).all() and (o["expert"][:, 1] == 1).all()
+    want = torch.softmax(torch.stack([torch.zeros_like(x), -x], 1).to(F64), 1)
+    # The difference from the maximum is exact here.  An exponential: 2^-22 = 4 u of the hardware's exp2, u for the product with
+    # the correction, 0.05 u x for the constants in it; their sum: 5 u and u; the reciprocal and the product: u each
+    within(o["weight"], want, (13 + 0.05 * x.to(F64)[:, None]) * U * want)
