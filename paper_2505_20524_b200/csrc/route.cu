@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(RT_BWD_THREADS, G == 1 ? 2 : 5) route_bwd_kern
 #pragma unroll
         for (int i = 0; i < PL; ++i) {
             g[i] = q.normalize ? fmaf(tok.p[i], u0[i] + shift, add[i]) : tok.p[i] * ((u0[i] + add[i]) + shift);
-            if (tok.broken) g[i] = NAN;
+            if (!tok.routed) g[i] = tok.broken ? NAN : 0.0f;       // 0 whatever dloss is
         }
         if constexpr (G == 1) {
             if (q.E == PL) {

@@ -957,3 +957,15 @@ def test_router_probabilities_far_below_the_largest(T, E, dt, normalize):
     # The difference from the maximum is exact here.  An exponential: 2^-22 = 4 u of the hardware's exp2, u for the product with
     # the correction, 0.05 u x for the constants in it; their sum: 5 u and u; the reciprocal and the product: u each
     within(o["weight"], want, (13 + 0.05 * x.to(F64)[:, None]) * U * want)
+
+
+@pytest.mark.parametrize("T,E,k", [(40, 10, 3), (300, 160, 6), (9001, 8, 2), (33001, 16, 4)])
+@pytest.mark.parametrize("normalize", [False, True])
+@pytest.mark.parametrize("dloss", [math.nan, math.inf])
+def test_router_gradient_of_unrouted_rows_is_zero_whatever_the_loss(T, E, k, normalize, dloss):
+    logits = rnd(gen(T + E), T, E)
+    logits[::7] = -math.inf
+    o = route(logits, None, k, normalize, CB, CZ)
+    dl = torch.full_like(logits, 3.0)
+    fp8.fp8_moe_route_bwd(logits, o["expert"], o["counts"], o["n_routed"], normalize, CB, CZ, scalar(dloss), torch.ones((T, k), device="cuda"), dl)
+    assert (dl[::7] == 0).all() and torch.isnan(dl[1::7]).any()
