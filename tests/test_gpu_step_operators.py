@@ -969,3 +969,16 @@ def test_router_gradient_of_unrouted_rows_is_zero_whatever_the_loss(T, E, k, nor
     dl = torch.full_like(logits, 3.0)
     fp8.fp8_moe_route_bwd(logits, o["expert"], o["counts"], o["n_routed"], normalize, CB, CZ, scalar(dloss), torch.ones((T, k), device="cuda"), dl)
     assert (dl[::7] == 0).all() and torch.isnan(dl[1::7]).any()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("n", [1, 3, 4, 8, 1023, 4095, 4096, 4097, 4100, 148 * 4096 + 13, 20_000_003])
+def test_gradient_clip_in_place_gives_the_bits_of_a_clip_elsewhere(n, dt):
+    g = gen(n)
+    x = rnd(g, n, dtype=dt)
+    other = torch.full_like(x, math.nan)
+    elsewhere, here = fp8.fp8_grad_items([x], [other]), fp8.fp8_grad_items([x])
+    norm = norm_of(here)
+    fp8.fp8_grad_clip(elsewhere, norm, 0.3)
+    fp8.fp8_grad_clip(here, norm, 0.3)
+    assert torch.equal(x, other)
