@@ -59,9 +59,37 @@ __device__ __forceinline__ void amax_end(uint32_t m2, unsigned int *amax, bool a
     if (amax) block_max_bf16_to(m2, amax);
 }
 
+// Whether a cluster of 16 CTAs of up to 256 threads with `smem` bytes each finds room on the current device (clusters of more than
+// 8 need not, on a partition of a GPU for instance).  The runtime is asked once per kernel, device and size of shared memory
+// beyond what is known to fit.
+template <auto Kernel>
+static bool cluster_of_16_fits(int dev, size_t smem)
+{
+    static size_t fits[64] = {0}, fails[64] = {0};        // bytes + 1: the most that fit, the fewest that do not
+    const bool known = dev >= 0 && dev < 64;
+    if (known && smem < fits[dev]) return true;
+    if (known && fails[dev] && smem + 1 >= fails[dev]) return false;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(16);
+    c.blockDim = dim3(256);
+    c.dynamicSmemBytes = smem;
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeClusterDimension;
+    a[0].val.clusterDim.x = 16;
+    a[0].val.clusterDim.y = a[0].val.clusterDim.z = 1;
+    c.attrs = a;
+    c.numAttrs = 1;
+    int clusters = 0;
+    const bool ok = cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&clusters, Kernel, &c) == cudaSuccess && clusters > 0;
+    if (!ok) cudaGetLastError();                          // a refusal is an answer, not an error of the call
+    if (known) (ok ? fits : fails)[dev] = smem + 1;
+    return ok;
+}
+
 // Launches a kernel that raises *amax between amax_begin and amax_end.  A grid of up to 16 CTAs is one cluster (see above), or
-// up to 8 where a CTA may fill an SM: a layer norm of 8 x 4096 takes 3.2 us in a graph and 7.9 us of the host with its binding,
-// 6.2 and 9.3 with a memset in front.  In front of other grids *amax is set to zero by a memset, which has to
+// up to 8 where a CTA may fill an SM or the device has no room for 16: a layer norm of 8 x 4096 takes 3.2 us in a graph and 7.9
+// us of the host with its binding, 6.2 and 9.3 with a memset in front.  In front of other grids *amax is set to zero by a memset, which has to
 // end before the kernel starts; for large tensors by a kernel of one thread, and the main kernel, which waits for it only in
 // front of the atomicMax (cudaGridDependencySynchronize), starts beside it.  The second launch costs the host 2.5 us more, so
 // from 2^24 elements on, where the device is busy longer than the host (8192 x 4096: 43.4 -> 42.7 us for the layer norm
@@ -71,14 +99,13 @@ template <auto Kernel, typename P>
 static int launch_behind_amax(size_t elements, unsigned int *amax, unsigned grid, unsigned threads, size_t smem, cudaStream_t st,
                               const P &p, int n)
 {
-    if (amax && grid > 1 && grid <= (threads <= 256 ? 16u : 8u)) {
-        static unsigned char done[64] = {0};
+    bool cluster = amax && grid > 1 && grid <= (threads <= 256 ? 16u : 8u);
+    if (cluster && grid > 8) {
         int dev = -1;
         FP8_CUDA_CHECK(cudaGetDevice(&dev));
-        if (dev < 0 || dev >= 64 || !done[dev]) {
-            FP8_CUDA_CHECK(cudaFuncSetAttribute(Kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-            if (dev >= 0 && dev < 64) done[dev] = 1;
-        }
+        cluster = cluster_of_16_fits<Kernel>(dev, smem);
+    }
+    if (cluster) {
         cudaLaunchConfig_t c = {};
         c.gridDim = dim3(grid);
         c.blockDim = dim3(threads);
