@@ -437,6 +437,10 @@ class GradItems:
                 _addr(f"grads[{i}]", g, _FLOATS, shape, dev)
                 _addr(f"outs[{i}]", o, _FLOATS, shape, dev)
             words += (g.data_ptr(), o.data_ptr(), shape.numel(), (gt is _F32) | (ot is _F32) << 32)
+        at = words[1::4]
+        if len(set(at)) < len(at) and len(set(at := [o for o, n in zip(at, words[2::4]) if n])) < len(at):
+            # tied weights: the norm would count them twice, and two CTAs scale one element
+            raise ValueError("an output stands in the list twice")
         self.array = (GradItem * len(self.tensors[0])).from_buffer(array.array("Q", words))
 
     def __len__(self):
@@ -444,7 +448,8 @@ class GradItems:
 
 
 def fp8_grad_items(grads, outs=None) -> GradItems:
-    """The list for fp8_grad_norm / fp8_grad_clip: BF16 or FP32 gradients, and where the clipped ones go (None: in place)."""
+    """The list for fp8_grad_norm / fp8_grad_clip: BF16 or FP32 gradients, and where the clipped ones go (None: in place).
+    Every tensor once: a list with an output in it twice is refused."""
     grads = list(grads)
     return GradItems(grads, grads if outs is None else outs)
 

@@ -982,3 +982,12 @@ def test_gradient_clip_in_place_gives_the_bits_of_a_clip_elsewhere(n, dt):
     fp8.fp8_grad_clip(elsewhere, norm, 0.3)
     fp8.fp8_grad_clip(here, norm, 0.3)
     assert torch.equal(x, other)
+
+
+def test_a_gradient_that_is_listed_twice_is_refused():
+    """Tied weights: clipped in place, two CTAs would scale the same elements.  Empty tensors may share their address."""
+    a, b, empty = torch.ones(100, device="cuda"), torch.ones(100, device="cuda"), torch.empty(0, device="cuda")
+    for grads, outs in (([a, b, a], None), ([a, b], [a, a]), ([a, b.view(10, 10)], [b, b.view(10, 10)])):
+        with pytest.raises(ValueError, match="twice"):
+            fp8.fp8_grad_items(grads, outs)
+    assert len(fp8.fp8_grad_items([a, empty, b, empty])) == 4
