@@ -550,7 +550,8 @@ static int ln_fwd_run(const LnFwd &p, size_t D, cudaStream_t st)
     if (D <= 4096) return ln_fwd_launch<2, LN_CTA, RES, STAGES, 256, 3>(p, s, st);
     if (D <= 8192) return ln_fwd_launch<4, LN_CTA, RES, STAGES, 256, 2>(p, s, st);
     // one CTA of up to 384 threads per SM: with two stages too little travels (3000 x 10000 with codes: 42.0 us, 38.4 with three)
-    if (RES && D <= 12288) return ln_fwd_launch<4, LN_CTA, RES, 3, 384, 1>(p, s, st);
+    if constexpr (RES)
+        if (D <= 12288) return ln_fwd_launch<4, LN_CTA, true, 3, 384, 1>(p, s, st);
     return ln_fwd_launch<4, LN_CTA, RES, STAGES, 512, 1>(p, s, st);
 }
 
