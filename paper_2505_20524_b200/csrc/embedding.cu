@@ -763,7 +763,7 @@ static GradWs grad_ws(size_t T, size_t V, size_t D)
     return w;
 }
 
-constexpr int EMB_MAX_SHARED = 160 * 1024;          // the sorts: counts of 32 warps x 1024 digits (68 KB) and the keys
+constexpr int EMB_MAX_SHARED = 160 * 1024;          // of the cluster's sort: counts of 32 warps x 1024 digits and two more rows (72 KB), 64 KB of keys
 template <typename IdT>
 static int launch_cluster_sort(const ClusterSort &p, size_t smem, cudaStream_t st)
 {
@@ -784,16 +784,6 @@ static int launch_cluster_sort(const ClusterSort &p, size_t smem, cudaStream_t s
     c.numAttrs = 1;
     FP8_CUDA_CHECK(cudaLaunchKernelEx(&c, embedding_cluster_sort_kernel<IdT>, p));
     return FP8_OK;
-}
-template <bool F32, bool ACC, int U>
-static int launch_sums(const GradParams &p, unsigned grid, size_t smem, cudaStream_t st)
-{
-    constexpr auto kernel = embedding_sum_kernel<F32, ACC, U>;
-    if (smem > 40 * 1024) {
-        const int rc = allow_shared<embedding_sum_kernel<F32, ACC, U>>(EMB_MAX_SHARED);
-        if (rc != FP8_OK) return rc;
-    }
-    return launch_early(kernel, grid, EG_THREADS, smem, st, p);
 }
 
 static int lanes_log2_for(size_t n8, int most)
@@ -984,12 +974,12 @@ extern "C" int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_a
             FP8_CUDA_CHECK(cudaGetLastError());
         }
     }
-    const size_t smem = ((slots << p.run_log2) * 2 + 2) * sizeof(uint32_t);
+    const size_t smem = ((slots << p.run_log2) * 2 + 2) * sizeof(uint32_t);       // 16 KB at most (8 columns: 256 slots of 8)
     const unsigned blocks = (unsigned)(work + fill);
-    if (p.is_fp32 && p.accumulate) rc = launch_sums<true, true, 4>(p, blocks, smem, st);
-    else if (p.is_fp32) rc = launch_sums<true, false, 8>(p, blocks, smem, st);
-    else if (p.accumulate) rc = launch_sums<false, true, 4>(p, blocks, smem, st);
-    else rc = launch_sums<false, false, 8>(p, blocks, smem, st);
+    if (p.is_fp32 && p.accumulate) rc = launch_early(embedding_sum_kernel<true, true, 4>, blocks, EG_THREADS, smem, st, p);
+    else if (p.is_fp32) rc = launch_early(embedding_sum_kernel<true, false, 8>, blocks, EG_THREADS, smem, st, p);
+    else if (p.accumulate) rc = launch_early(embedding_sum_kernel<false, true, 4>, blocks, EG_THREADS, smem, st, p);
+    else rc = launch_early(embedding_sum_kernel<false, false, 8>, blocks, EG_THREADS, smem, st, p);
     if (rc != FP8_OK || p.items == 1) return rc;
     // narrow rows have a group for (almost) every item that a run reaches, wide ones few groups
     const int jl = lanes_log2_for(p.n8, 7);
