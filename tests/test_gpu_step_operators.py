@@ -971,6 +971,104 @@ def test_router_gradient_of_unrouted_rows_is_zero_whatever_the_loss(T, E, k, nor
     assert (dl[::7] == 0).all() and torch.isnan(dl[1::7]).any()
 
 
+@pytest.mark.parametrize("T,E,k", [(9001, 8, 2), (33001, 16, 4), (33001, 13, 4), (300, 160, 6), (224, 256, 8), (5001, 64, 3)])
+@pytest.mark.parametrize("normalize", [False, True])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_router_broken_rows_in_every_form(T, E, k, normalize, dt):
+    """Rows with NaN or +inf: no expert, NaN weights, losses and row of the gradient; the others are as without them."""
+    g = gen(T + E + 1)
+    logits = rnd(g, T, E, dtype=dt)
+    bad = torch.tensor([0, 7, T // 2, T - 1], device="cuda")
+    logits[bad, torch.tensor([E - 1, 2, 0, E // 2], device="cuda")] = torch.tensor([math.nan, math.inf, math.inf, math.nan], device="cuda", dtype=dt)
+    r = route_reference(logits, None, k, normalize, CB, CZ)
+    o = route(logits, None, k, normalize, CB, CZ)
+    for name in ("expert", "counts", "offsets", "rows"):
+        assert torch.equal(o[name], r[name]), name
+    whole = torch.ones(T, dtype=torch.bool, device="cuda")
+    whole[bad] = False
+    assert o["n_routed"].item() == T == r["n"]
+    assert torch.isnan(o["weight"][bad]).all() and torch.isnan(o["loss"]).all()
+    # as in test_router_forward_and_gradient
+    rel = (4 * logits[whole].float().abs().max().item() + E / 8 + 24) * U
+    within(o["weight"][whole], r["weight"][whole], rel * r["weight"][whole] + 1e-37)
+    dweight, dl = rnd(g, T, k), torch.zeros_like(logits)
+    fp8.fp8_moe_route_bwd(logits, o["expert"], o["counts"], o["n_routed"], normalize, CB, CZ, None, dweight, dl)
+    assert torch.isnan(dl[bad]).all()
+    p, idx, dw = r["p"][whole], r["expert"][whole].long(), dweight[whole].to(F64)
+    u = (CB * E * r["counts"].to(F64) / (k * T * T)).expand(int(whole.sum()), E).clone()
+    if not normalize:
+        u.scatter_add_(1, idx, dw)
+    zterm = CZ * 2 / T * r["lse"][whole][:, None] * p
+    want = p * (u - (u * p).sum(1, keepdim=True)) + zterm
+    size = p * (u.abs() + (u.abs() * p).sum(1, keepdim=True)) + zterm.abs()
+    if normalize:
+        w = r["weight"][whole]
+        want.scatter_add_(1, idx, w * (dw - (dw * w).sum(1, keepdim=True)))
+        size.scatter_add_(1, idx, w * (dw.abs() + (dw.abs() * w).sum(1, keepdim=True)))
+    within(dl[whole], want, HALF[dt] * want.abs() + (4 * rel + (E + 32) * U) * size + 1e-37)
+
+
+@pytest.mark.parametrize("T,E,k", [(100003, 8, 2), (400001, 8, 2), (400001, 13, 3), (200003, 72, 2)])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_router_of_many_tokens(T, E, k, dt):
+    """More tokens than one turn of all lanes takes, forward and backward."""
+    for normalize, with_bias in ((True, True), (False, False)):
+        test_router_forward_and_gradient(T, E, k, dt, normalize, with_bias)
+
+
+# ------------------------------------------------------------------------------------------------ layer norm: rows one after the other
+LONG_ROWS = [(1000, 4104), (1100, 5120), (700, 8192), (700, 8200), (600, 12288), (600, 12296), (500, 16384)]
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("T,D", LONG_ROWS)
+def test_layernorm_forward_of_long_rows_one_after_the_other(T, D, residual):
+    """Rows above 4096 columns, several to a CTA: more than it keeps on the way, and not the same number for each."""
+    test_layernorm_forward(T, D, residual)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("T,D", LONG_ROWS + [(5000, 8200), (9700, 4104), (5000, 6000)])
+def test_layernorm_backward_of_long_rows_one_after_the_other(T, D, accumulate):
+    """The same for the gradient, and more than the 32 rows of a CTA whose statistics travel together."""
+    test_layernorm_backward(T, D, accumulate)
+
+
+# ------------------------------------------------------------------------------------------------ amax of NaN, lists of large gradients
+@pytest.mark.parametrize("T", [1, 8, 300, 4200])
+def test_amax_of_an_output_with_nan_is_nan(T):
+    """Every way in which the amax is set to zero first: a NaN outranks all numbers and infinities."""
+    D = 4096
+    g, x, gamma, beta = ln_data(T, D, seed=8)
+    table = rnd(g, T + 1, D, std=0.02, dtype=BF16)
+    x[T - 1, 17], table[T - 1, 5], table[0, 9] = math.nan, math.nan, math.inf
+    out, a = torch.empty_like(x), scalar(1e30)
+    fp8.fp8_layernorm_fwd(x, gamma, beta, 1e-5, out, amax_out=a)
+    assert math.isnan(a.item()) and torch.isnan(out[T - 1]).all() and torch.isfinite(out[:T - 1]).all()
+    fp8.fp8_embedding_fwd(table, torch.arange(T, device="cuda"), 1.0, out, a)
+    assert math.isnan(a.item())
+    table[T - 1, 5] = 0.0
+    fp8.fp8_embedding_fwd(table, torch.arange(T, device="cuda"), 1.0, out, a)
+    assert math.isinf(a.item())
+
+
+def test_gradient_norm_and_clip_of_many_large_tensors():
+    """More tensors than one launch takes, each of many chunks."""
+    g = gen(78)
+    sizes = [100_000 + 4096 * (i % 7) + i for i in range(1100)]
+    grads = [rnd(g, n, std=0.01 * (1 + i % 5), dtype=BF16 if i % 2 else F32) for i, n in enumerate(sizes)]
+    outs = [torch.full((n,), math.nan, dtype=BF16 if i % 3 else F32, device="cuda") for i, n in enumerate(sizes)]
+    items = fp8.fp8_grad_items(grads, outs)
+    norm = norm_of(items)
+    want = math.sqrt(sum(float(x.to(F64).square().sum()) for x in grads))
+    assert abs(norm.item() - want) <= (17 + 2) * U * want               # as in test_gradient_norm_and_clip
+    fp8.fp8_grad_clip(items, norm, 2.5)
+    c = torch.tensor(np.float32(2.5) / (np.float32(norm.item()) + np.float32(1e-6)), device="cuda")
+    assert c < 1
+    for i, (x, o) in enumerate(zip(grads, outs)):
+        assert torch.equal(o, (x.float() * c).to(o.dtype)), i
+
+
 @pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("n", [1, 3, 4, 8, 1023, 4095, 4096, 4097, 4100, 148 * 4096 + 13, 20_000_003])
 def test_gradient_clip_in_place_gives_the_bits_of_a_clip_elsewhere(n, dt):
