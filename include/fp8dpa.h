@@ -336,7 +336,7 @@ FP8_API int fp8_linear_wgrad_blockwise(const uint8_t *dY8, const uint8_t *X8, co
  * stretches), rounded once: the result is the same from call to call.  Without `accumulate` every row is overwritten (zeros where no token points);
  * with it only the rows that a token points at are read and written.  Ids outside [0, V) contribute nothing.
  * ws: scratch of fp8_embedding_bwd_workspace_bytes(T, V, D), 256-byte aligned, contents need no preparation; calls that
- * share it must be ordered.  D % 8 == 0, D <= 2^20, T and V <= 2^30.  ids need the alignment of their own type only.  Outputs
+ * share it must be ordered.  D % 8 == 0, D <= 2^20, 1 <= T, V <= 2^30.  ids need the alignment of their own type only.  Outputs
  * must not overlap inputs. */
 FP8_API int fp8_embedding_fwd(const void *table, int table_is_fp32, size_t V, size_t D, const void *ids, int ids_are_int64,
                       size_t T, float scale, void *out_bf16, float *amax_out, void *stream);
@@ -350,15 +350,15 @@ FP8_API int fp8_embedding_bwd(const void *dy_bf16, const void *ids, int ids_are_
 /* ---- layer norm ---------------------------------------------------------------------------------------
  * The centred counterpart of fp8_postnorm_residual, with its gradient.  Per row of D columns:
  *   mean = sum(x) / D, rstd = 1 / sqrt(sum((x - mean)^2) / D + eps), out = residual + gamma (x - mean) rstd + beta
- * in FP32 (the squares are of the distances from the mean), rounded once.  x, residual (nullable), out: [T, D] BF16; gamma,
- * beta: D binary32; mean, rstd (nullable): T binary32, what the backward pass reads; *amax_out (nullable) is overwritten with
+ * in FP32 (the squares are of the distances from the mean; rstd by the hardware's reciprocal root, off by 2 ulp at most),
+ * rounded once.  x, residual (nullable), out: [T, D] BF16; gamma, beta: D binary32; mean, rstd (nullable): T binary32, what the backward pass reads; *amax_out (nullable) is overwritten with
  * amax(out).  out may be x or residual itself.  fp8_layernorm_fwd_q also writes out8 = FP8cast(*q_scale * out) of the
  * BF16-rounded values (bit-identical to fp8_cast of out_bf16).
  * fp8_layernorm_bwd: from dout [T, D] BF16 and the forward's x, mean, rstd, with xh = (x - mean) rstd and g = gamma dout:
  *   dx = rstd (g - mean(g) - xh mean(g xh)),  dgamma (+)= sum over rows of dout xh,  dbeta (+)= sum over rows of dout
  * (the residual's gradient is dout).  dx [T, D] BF16, may be dout or x itself; dgamma, dbeta: D binary32, added to with
  * `accumulate`.  The sums over rows are FP32 in a fixed order.  ws: scratch of fp8_layernorm_bwd_workspace_bytes(T, D),
- * 256-byte aligned; calls that share it must be ordered.  D % 8 == 0, D <= 16384, T < 2^31. */
+ * 256-byte aligned; calls that share it must be ordered.  D % 8 == 0, D <= 16384, 1 <= T < 2^31. */
 FP8_API int fp8_layernorm_fwd(const void *x_bf16, const float *gamma, const float *beta, const void *residual_bf16, size_t T,
                       size_t D, float eps, void *out_bf16, float *mean, float *rstd, float *amax_out, void *stream);
 FP8_API int fp8_layernorm_fwd_q(const void *x_bf16, const float *gamma, const float *beta, const void *residual_bf16, size_t T,
@@ -372,12 +372,12 @@ FP8_API int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, const f
 /* ---- router of the grouped products -------------------------------------------------------------------
  * What fp8_grouped_linear_* calls the router's output, and its gradient (Appendix D: sparse FFNs, 8 experts of which 2 are
  * active; balance through an auxiliary loss, z-loss and an expert bias).  logits [T, E] BF16 or FP32 (is_fp32).  For token
- * t, with p = softmax(logits[t]) in FP32 and the score s_e = logits[t, e] + bias[e] (bias: E binary32, nullable; it
- * decides the choice only):
+ * t, with p = softmax(logits[t]) in FP32 (the exponential of the rounded difference from the maximum is good to 2^-22 of itself,
+ * and 0 below 2^-126) and the score s_e = logits[t, e] + bias[e] (bias: E binary32, nullable; it decides the choice only):
  *   expert[t, 0..k)  the experts of the k largest scores in falling order, equal scores in rising order of e
  *   weight[t, j]     p of that expert; with `normalize` the softmax over the k chosen logits
- * Experts of score -inf are never chosen; free slots hold expert -1 and weight 0.  A token whose logits are all -inf (padding)
- * is not routed: it takes no part in the sums below.  A token with a NaN or +inf logit gets expert -1 and weight NaN, and the
+ * Experts of score -inf or NaN (by the bias) are never chosen; free slots hold expert -1 and weight 0.  A token whose logits
+ * are all -inf (padding) is not routed: it takes no part in the sums below.  A token with a NaN or +inf logit gets expert -1 and weight NaN, and the
  * losses become NaN.
  *   counts[e]        chosen slots of expert e;  offsets[0..E]: their running sums (the group_offsets of the products)
  *   rows             (nullable) [T k]: the flat slots t k + j sorted by expert, equal experts in rising order: row r of the
@@ -386,10 +386,10 @@ FP8_API int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, const f
  *   loss[0]          balance_coef * E * sum_e (counts[e] / (k n)) * (sum_t p[t, e] / n)      (1 * balance_coef when even)
  *   loss[1]          z_coef * sum_t logsumexp(logits[t])^2 / n
  * fp8_moe_route_bwd: dlogits [T, E] (type of logits) of dloss * (loss[0] + loss[1]) + sum dweight * weight, the choice and the
- * counts held fixed; dloss (nullable: 1) a device scalar, dweight [T, k] FP32 (nullable: 0).  Rows that are not routed get 0;
- * rows with a NaN or +inf logit get NaN.  expert, counts, n_routed as the forward left them.
+ * counts held fixed; dloss (nullable: 1) a device scalar, dweight [T, k] FP32 (nullable: 0).  Rows that are not routed get 0,
+ * whatever dloss is; rows with a NaN or +inf logit get NaN.  expert, counts, n_routed as the forward left them.
  * ws: scratch of fp8_moe_route_workspace_bytes(T, E), 256-byte aligned; calls that share it must be ordered.
- * E <= 256, k <= min(E, 16), T <= 2^26.  logits and dlogits 16-byte aligned, the others to their own type. */
+ * E <= 256, k <= min(E, 16), 1 <= T <= 2^26.  logits and dlogits 16-byte aligned, the others to their own type. */
 FP8_API size_t fp8_moe_route_workspace_bytes(size_t T, int E);
 FP8_API int fp8_moe_route(const void *logits, int is_fp32, const float *bias, size_t T, int E, int k, int normalize,
                   float balance_coef, float z_coef, int *expert, float *weight, int *counts, int *offsets, int *rows,

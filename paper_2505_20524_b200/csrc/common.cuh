@@ -67,8 +67,9 @@ inline int allow_shared(int bytes)
 }
 
 // Launch of a kernel that may start before the one in front of it on the stream has ended; it calls
-// cudaGridDependencySynchronize() itself before it reads what that one wrote.  Only behind a kernel of the same entry point,
-// itself launched in order: what came before that one has then ended too.
+// cudaGridDependencySynchronize() itself before it reads what that one wrote.  Only behind a kernel of the same entry point that
+// either was launched in order, or does not end before the kernel in front of it has (it waits for that one itself, in one
+// block at least): what came before has then ended too.
 template <typename... P, typename... A>
 inline int launch_early(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t st, A... args)
 {

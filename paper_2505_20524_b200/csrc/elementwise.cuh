@@ -89,11 +89,11 @@ static bool cluster_of_16_fits(int dev, size_t smem)
 
 // Launches a kernel that raises *amax between amax_begin and amax_end.  A grid of up to 16 CTAs is one cluster (see above), or
 // up to 8 where a CTA may fill an SM or the device has no room for 16: a layer norm of 8 x 4096 takes 3.2 us in a graph and 7.9
-// us of the host with its binding, 6.2 and 9.3 with a memset in front.  In front of other grids *amax is set to zero by a memset, which has to
-// end before the kernel starts; for large tensors by a kernel of one thread, and the main kernel, which waits for it only in
-// front of the atomicMax (cudaGridDependencySynchronize), starts beside it.  The second launch costs the host 2.5 us more, so
-// from 2^24 elements on, where the device is busy longer than the host (8192 x 4096: 43.4 -> 42.7 us for the layer norm
-// with residual and codes, 27.6 -> 26.9 us for the embedding).
+// us of the host with its binding, 6.2 and 9.3 with a memset in front.  In front of other grids *amax is set to zero by a
+// memset, which has to end before the kernel starts; for large tensors by a kernel of one thread, and the main kernel, which
+// waits for it only in front of the atomicMax (cudaGridDependencySynchronize), starts beside it.  The second launch costs the
+// host 2.5 us more, so from 2^24 elements on, where the device is busy longer than the host (8192 x 4096: 43.4 -> 42.7 us for
+// the layer norm with residual and codes, 27.6 -> 26.9 us for the embedding).
 constexpr size_t AMAX_EARLY_ELEMENTS = (size_t)1 << 24;
 template <auto Kernel, typename P>
 static int launch_behind_amax(size_t elements, unsigned int *amax, unsigned grid, unsigned threads, size_t smem, cudaStream_t st,

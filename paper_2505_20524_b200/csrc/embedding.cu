@@ -25,7 +25,7 @@ __device__ __forceinline__ int checked_id(const IdT *ids, size_t t, unsigned V)
 
 // `lanes` (a power of two) threads share a row; a CTA has 256 / lanes row slots with EF_ROWS rows each.  Bound by HBM:
 // every thread keeps EF_ROWS 16-byte loads (32 bytes from an FP32 table) in flight.  8192 tokens x 4096 with codes and amax:
-// 25.1 us (100 MB written, about 45 MB of distinct rows read); 1, 2 and 4 rows and 128 threads are within 4 % of it.
+// 25.1 us (100 MB written, 32 MB of distinct rows read); 1, 2 and 4 rows and 128 threads are within 4 % of it.
 struct EmbedFwd {
     const void *table, *ids;
     size_t T;
@@ -541,7 +541,9 @@ __device__ __forceinline__ void fill_rows(const GradParams &p, size_t v0, size_t
 // waits for the sort, so that whoever waits for this kernel has waited for both.
 constexpr unsigned EC_WORDS = 4096;       // 16-byte words per block
 // what is written while the sort takes its 10 us (131072 x 4096 in BF16: 182 us with none, 178.0 with 40 MB, 176.3 with 60 and
-// 80, 178.4 with 100); a table below EC_MIN_BYTES is not worth the launch
+// 80, 178.4 with 100); a table below EC_MIN_BYTES is not worth the launch.  Up to ER_MAX_T positions the order takes 4 to 6 us and
+// less fits beside it, which large tables do not feel (4096 positions: 131072 x 4096 167.6 us with 24 MB, 166.9 with 64; 50257 x
+// 2048 FP32 78 and 77) and one that is cleared whole does (32000 x 1024 BF16: 31.8 with 24 or 40 MB, 33.8 with 64)
 constexpr size_t EC_BYTES = (size_t)64 << 20, EC_MIN_BYTES = (size_t)4 << 20;
 __global__ void __launch_bounds__(EG_THREADS) embedding_clear_kernel(uint4 *__restrict__ out, size_t words)
 {
