@@ -369,6 +369,113 @@ FP8_API int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, const f
                       size_t T, size_t D, void *dx_bf16, float *dgamma, float *dbeta, int accumulate, void *ws,
                       size_t ws_bytes, void *stream);
 
+/* ---- rotary positions on the QKV projection ------------------------------------------------------------
+ * What lies between the QKV projection and the attention, both ways: from the rows of the projection's output to the three
+ * operands of fp8_attention_fwd, and from the gradients of fp8_attention_bwd to the rows that the projection's gradient products
+ * read (Section 3; Appendix B: attnhead = selfattn(N_QK(X W_Q), N_QK(X W_K), X W_V) with rotary position embeddings).
+ *
+ * A row holds Hq heads of Q, Hkv of K and Hkv of V, d values each.  Heads of Q and K go through the regulariser `mode`
+ * (fp8_qk_norm_rope's: FP8_QK_RMS over the d values, FP8_QK_TANH, FP8_QK_NONE), then the first `rot` values of each are rotated:
+ * the pairs (i, i + rot/2), or with `interleaved` (2 i, 2 i + 1), i < rot/2, by the angle of row pos[t] of the tables:
+ *   (a, b) -> (a c - b s, b c + a s).
+ * pos[t] = positions[t], or t mod n_pos without them.  A token whose position lies outside [0, n_pos) is padding: its rows (of Q,
+ * K, V and of the gradient) are zeros, whatever they hold.  rot = 0 rotates nothing and reads neither tables nor positions. */
+typedef struct {
+    int mode;                 /* FP8_QK_RMS / FP8_QK_TANH / FP8_QK_NONE */
+    float alpha, eps;         /* of FP8_QK_TANH, of FP8_QK_RMS (>= 0) */
+    const float *cos_table;   /* device: [n_pos, rot/2] binary32, 16-byte aligned */
+    const float *sin_table;
+    size_t n_pos;             /* rows of the tables, < 2^31 */
+    int rot;                  /* a multiple of 16, at most d */
+    int interleaved;
+    const void *positions;    /* device, nullable: T of int32 or int64 */
+    int positions_are_int64;
+} fp8_rope;
+
+/* The tables: cos and sin (times `magnitude`) of pos * f_i for pos < n_pos, i < rot/2, f_i = base^(-2 i / rot) changed by `scaling`:
+ *   FP8_ROPE_PLAIN     f_i                           FP8_ROPE_LINEAR  f_i / factor
+ *   FP8_ROPE_NTK       base * factor^(rot / (rot - 2)) in place of base
+ *   FP8_ROPE_BY_PARTS  (1 - w) f_i / factor + w f_i with w = (n_i - turns_low) / (turns_high - turns_low) clamped to [0, 1], n_i =
+ *                      original_len f_i / 2 pi: the turns of the pair over the length that the model was trained with
+ * Angles are formed in 64 bits; entries are good to 2 ulp of binary32 for every position.  rot % 16 == 0, rot <= 256. */
+enum { FP8_ROPE_PLAIN = 0, FP8_ROPE_LINEAR = 1, FP8_ROPE_NTK = 2, FP8_ROPE_BY_PARTS = 3 };
+FP8_API int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, double factor, double original_len, double turns_low,
+                   double turns_high, double magnitude, float *cos_table, float *sin_table, void *stream);
+
+/* Forward: qkv BF16, rows `pitch` elements apart (a multiple of 8, at least (Hq + 2 Hkv) d); q [T,Hq,d], k, v [T,Hkv,d] BF16, each
+ * nullable: what is not asked for is not computed.  amax_out (nullable): three floats, overwritten with amax of q, k, v.
+ * _q: the producer form under delayed scaling: codes q8, k8, v8 (each nullable) of the BF16-rounded values under scales[0..2], bit-
+ * identical to fp8_cast of them.  Hkv = 0: rows of Q alone.  With FP8_QK_RMS / NONE, the whole head and halves as partners the results
+ * are those of fp8_qk_norm_rope bit for bit.  d % 16 == 0, d <= 256, 1 <= T < 2^31.  Outputs must not overlap inputs. */
+FP8_API int fp8_rope_qkv_fwd(const void *qkv_bf16, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *rope, void *q_bf16,
+                     void *k_bf16, void *v_bf16, float *amax_out, void *stream);
+FP8_API int fp8_rope_qkv_fwd_q(const void *qkv_bf16, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *rope,
+                       const float *scales, int fmt, void *q_bf16, void *k_bf16, void *v_bf16, uint8_t *q8, uint8_t *k8,
+                       uint8_t *v8, float *amax_out, void *stream);
+
+/* Backward: dq, dk, dv (BF16, shapes of q, k, v; dk, dv may be NULL with Hkv = 0) and the forward's qkv (NULL allowed with
+ * FP8_QK_NONE) -> dqkv BF16, rows dqkv_pitch elements apart.  With u the gradient turned back and xh = x / rms(x): FP8_QK_RMS
+ * (u - xh mean(u xh)) / rms(x), FP8_QK_TANH alpha u (1 - tanh(alpha x)^2).  *amax_out (nullable): amax(dqkv).  _q: the codes
+ * dqkv8 [T, (Hq + 2 Hkv) d] (contiguous rows: the dY8 of the projection's gradient products); dqkv_bf16 may be NULL. */
+FP8_API int fp8_rope_qkv_bwd(const void *dq_bf16, const void *dk_bf16, const void *dv_bf16, const void *qkv_bf16, size_t pitch, size_t T,
+                     int Hq, int Hkv, int d, const fp8_rope *rope, void *dqkv_bf16, size_t dqkv_pitch, float *amax_out,
+                     void *stream);
+FP8_API int fp8_rope_qkv_bwd_q(const void *dq_bf16, const void *dk_bf16, const void *dv_bf16, const void *qkv_bf16, size_t pitch, size_t T,
+                       int Hq, int Hkv, int d, const fp8_rope *rope, const float *scale, int fmt, void *dqkv_bf16,
+                       size_t dqkv_pitch, uint8_t *dqkv8, float *amax_out, void *stream);
+
+/* ---- the joint of two blocks ---------------------------------------------------------------------------
+ * What lies between one block's last product and the next one's first: the norm behind the block, its gate, the residual sum and
+ * the norm in front of the next block, with its gradient (Section 3; Appendix B: X^ = X + (N_post o GQA)(X); pre-norm and sandwich
+ * blocks are the other settings).  Per token row of D columns, in FP32:
+ *   z    = gamma_post y r_post    FP8_NORM_RMS, r_post = 1 / sqrt(mean(y^2) + eps)
+ *          gamma_post y           FP8_NORM_LAYERSCALE
+ *          y                      FP8_NORM_NONE (gamma_post is not read)
+ *   h    = x_scale x + y_scale s z, rounded to BF16;  s = gate (FP8_GATE_LINEAR), sigmoid(gate) (FP8_GATE_SIGMOID), 1 without one
+ *   out  = gamma_pre h r_pre, r_pre = 1 / sqrt(mean(h^2) + eps) of the rounded h, rounded to BF16
+ * The reciprocal roots come from the hardware's, off by 2 ulp at most; a row of zeros without eps gives NaN. */
+enum { FP8_NORM_NONE = 2 };                             /* beside FP8_NORM_RMS and FP8_NORM_LAYERSCALE */
+enum { FP8_GATE_LINEAR = 0, FP8_GATE_SIGMOID = 1 };
+typedef struct {
+    int post;                 /* FP8_NORM_RMS / FP8_NORM_LAYERSCALE / FP8_NORM_NONE */
+    int gate;                 /* FP8_GATE_LINEAR / FP8_GATE_SIGMOID: how a gate is read */
+    float x_scale, y_scale;   /* finite */
+    float eps;                /* >= 0 */
+} fp8_block_norm;
+
+/* Forward: x, y, gate, h, out: [T,D] BF16; gamma_post, gamma_pre: D binary32; r_post, r_pre (nullable): T binary32, what the
+ * backward pass reads.  y NULL: no block in front (h = x_scale x; h may then be NULL where x_scale is 1).  gate NULL: no gate.
+ * gamma_pre NULL: no norm in front of the next block; out is then NULL, and codes and amax are those of h.  *amax_out (nullable) is
+ * overwritten with amax(out).  _q: also out8 = FP8cast(*scale * out) of the BF16-rounded values (bit-identical to fp8_cast); out_bf16
+ * may be NULL.  h may be x or y itself.  D % 8 == 0, D <= 16384, 1 <= T < 2^31. */
+FP8_API int fp8_block_norm_fwd(const void *x_bf16, const void *y_bf16, const void *gate_bf16, const float *gamma_post,
+                       const float *gamma_pre, size_t T, size_t D, const fp8_block_norm *cfg, void *h_bf16, void *out_bf16,
+                       float *r_post, float *r_pre, float *amax_out, void *stream);
+FP8_API int fp8_block_norm_fwd_q(const void *x_bf16, const void *y_bf16, const void *gate_bf16, const float *gamma_post,
+                         const float *gamma_pre, size_t T, size_t D, const fp8_block_norm *cfg, const float *scale, int fmt,
+                         void *h_bf16, void *out_bf16, uint8_t *out8, float *r_post, float *r_pre, float *amax_out,
+                         void *stream);
+
+/* Backward: dout (gradient of out; NULL without gamma_pre) and dh (gradient of h from the residual stream behind; may be NULL with
+ * gamma_pre), with the forward's h, y, gate, r_post, r_pre.  With hh = h r_pre, e = gamma_pre dout, yh = y r_post (y without a norm):
+ *   G = dh + r_pre (e - hh mean(e hh)),  dx = x_scale G,  dgamma_pre (+)= sum over rows of dout hh
+ *   dgate = y_scale G z s',  dz = y_scale G s,  dgamma_post (+)= sum over rows of dz yh
+ *   dy = r_post (f - yh mean(f yh)) with f = gamma_post dz  (FP8_NORM_LAYERSCALE: f;  FP8_NORM_NONE: dz)
+ * dx, dy, dgate: [T,D] BF16; dx may be dh or dout itself, dy may be y, dgate may be gate; dgamma_*: D binary32, added to with
+ * `accumulate`, sums over rows in FP32 in a fixed order.  y NULL: dx alone (dy, dgate NULL).  *amax_out (nullable): amax(dy), the
+ * operand of the block's last gradient products; _q: its codes dy8 (dy_bf16 may be NULL).  ws: scratch of
+ * fp8_block_norm_bwd_workspace_bytes(T, D), 256-byte aligned; calls that share it must be ordered. */
+FP8_API size_t fp8_block_norm_bwd_workspace_bytes(size_t T, size_t D);
+FP8_API int fp8_block_norm_bwd(const void *dout_bf16, const void *dh_bf16, const void *h_bf16, const void *y_bf16, const void *gate_bf16,
+                       const float *gamma_post, const float *gamma_pre, const float *r_post, const float *r_pre, size_t T,
+                       size_t D, const fp8_block_norm *cfg, void *dx_bf16, void *dy_bf16, void *dgate_bf16, float *dgamma_post,
+                       float *dgamma_pre, int accumulate, float *amax_out, void *ws, size_t ws_bytes, void *stream);
+FP8_API int fp8_block_norm_bwd_q(const void *dout_bf16, const void *dh_bf16, const void *h_bf16, const void *y_bf16,
+                         const void *gate_bf16, const float *gamma_post, const float *gamma_pre, const float *r_post,
+                         const float *r_pre, size_t T, size_t D, const fp8_block_norm *cfg, const float *scale, int fmt,
+                         void *dx_bf16, void *dy_bf16, uint8_t *dy8, void *dgate_bf16, float *dgamma_post, float *dgamma_pre,
+                         int accumulate, float *amax_out, void *ws, size_t ws_bytes, void *stream);
+
 /* ---- router of the grouped products -------------------------------------------------------------------
  * What fp8_grouped_linear_* calls the router's output, and its gradient (Appendix D: sparse FFNs, 8 experts of which 2 are
  * active; balance through an auxiliary loss, z-loss and an expert bias).  logits [T, E] BF16 or FP32 (is_fp32).  For token
@@ -419,6 +526,47 @@ typedef struct {
 FP8_API size_t fp8_grad_norm_workspace_bytes(const fp8_grad_item *items, int n_items);
 FP8_API int fp8_grad_norm(const fp8_grad_item *items, int n_items, float *norm, void *ws, size_t ws_bytes, void *stream);
 FP8_API int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *norm, float max_norm, void *stream);
+
+/* ---- optimizer step -------------------------------------------------------------------------------------
+ * AdamW over all tensors of a model, behind fp8_grad_norm and in front of the next step's products.  With t = *step + 1, c = min(1,
+ * max_norm / (*norm + 1e-6)) (1 without norm) and g' = c g, per element in FP32:
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - *lr weight_decay) - *lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * and *step = t.  A norm that is NaN or infinite skips the step: nothing is changed, *step and the outputs neither.  (Without norm
+ * a gradient that is not finite makes its element, and with moments in 8 bits its block of 128, worthless.)
+ * Outputs (nullable): p_bf16 the rounded weights, p8 = FP8cast(*q_scale * p_bf16) in `fmt` (bit-identical to fp8_cast of p_bf16),
+ * *amax = amax(p_bf16): what fp8_quantize_delayed_multi would take another pass for.
+ *
+ * state_bits = 32: m, v: n binary32.  state_bits = 8: m: n E4M3 codes, v: n E4M3 codes of sqrt(v), in blocks of 128 consecutive
+ * elements with a scale 2^(m_exp[i / 128] - 127), 2^(v_exp[i / 128] - 127): the smallest power of two (2^-126 at least) that leaves no
+ * value above 448.  The update uses the values before they are stored.  A stored value is rounded towards zero or away from it
+ * with the probability of the part cut off, from 16 random bits each: the lower (m) and upper (v) half of
+ * mix(mix(mix(K + item) + (i >> 32)) + i) modulo 2^32, K = mix(mix(mix(seed) ^ (seed >> 32)) ^ t), with mix(x): x = (x ^ x >> 16) *
+ * 0x9E3779B9; x = (x ^ x >> 15) * 0x6A09E667; x ^ x >> 16, item the number in the list; the same seed and step give the same
+ * codes.  v above zero is stored as the smallest code at least.  New states: zeros (all bytes).
+ *
+ * `items` is a HOST array, read during the call; its pointers are device pointers, 16-byte aligned (m_exp, v_exp, q_scale, amax to
+ * their own type); items of n = 0 are skipped.  A tensor is listed once.  lr, step (int32), norm (nullable): device scalars, so that the
+ * call can be captured once and replayed.  beta1, beta2 in [0, 1), 1e-30 <= eps <= 1e30, weight_decay >= 0.  ws: scratch of
+ * fp8_adamw_workspace_bytes(items, n_items), 256-byte aligned, contents need no preparation; calls that share it must be ordered. */
+typedef struct {
+    float *p;                 /* device: n binary32 weights, updated */
+    const void *g;            /* device: n gradients, BF16 or FP32 */
+    void *m, *v;              /* device: moments, updated */
+    uint8_t *m_exp, *v_exp;   /* device: (n + 127) / 128 exponents each, with state_bits = 8 */
+    void *p_bf16;             /* device, nullable */
+    uint8_t *p8;              /* device, nullable */
+    const float *q_scale;     /* device scalar, with p8 */
+    float *amax;              /* device scalar, nullable */
+    size_t n;
+    float weight_decay;
+    int g_is_fp32;
+    int state_bits;           /* 32 or 8 */
+    int fmt;                  /* of p8 */
+} fp8_adamw_item;
+FP8_API size_t fp8_adamw_workspace_bytes(const fp8_adamw_item *items, int n_items);
+FP8_API int fp8_adamw(const fp8_adamw_item *items, int n_items, const float *lr, int *step, double beta1, double beta2, double eps,
+              const float *norm, float max_norm, uint64_t seed, void *ws, size_t ws_bytes, void *stream);
 
 /* ---- attention ------------------------------------------------------------------------------------
  * Appendix B, Eq. (P): P = Softmax(s Q K^T + M), output P V, grouped-query heads; Appendix E table: both

@@ -19,4 +19,8 @@ from .binding import (ACT_GELU, ACT_XIELU, E4M3, E5M2, FP8_BLOCK_128x1, NORM_LAY
                       GradItems, fp8_embedding_fwd, fp8_embedding_fwd_q, fp8_embedding_bwd, fp8_embedding_bwd_workspace_bytes,
                       fp8_layernorm_fwd, fp8_layernorm_fwd_q, fp8_layernorm_bwd, fp8_layernorm_bwd_workspace_bytes,
                       fp8_moe_route, fp8_moe_route_bwd, fp8_moe_route_workspace_bytes, fp8_grad_items, fp8_grad_norm,
-                      fp8_grad_norm_workspace_bytes, fp8_grad_clip)
+                      fp8_grad_norm_workspace_bytes, fp8_grad_clip,
+                      GATE_LINEAR, GATE_SIGMOID, NORM_NONE, ROPE_BY_PARTS, ROPE_LINEAR, ROPE_NTK, ROPE_PLAIN, AdamWItems,
+                      fp8_rope_table, fp8_rope_qkv_fwd, fp8_rope_qkv_fwd_q, fp8_rope_qkv_bwd, fp8_rope_qkv_bwd_q,
+                      fp8_block_norm_fwd, fp8_block_norm_fwd_q, fp8_block_norm_bwd, fp8_block_norm_bwd_q,
+                      fp8_block_norm_bwd_workspace_bytes, fp8_adamw, fp8_adamw_items, fp8_adamw_workspace_bytes)

@@ -29,6 +29,9 @@ SYMBOLS = ["fp8_last_error", "fp8_device_status", "fp8_selftest_wait_timeout", "
            "fp8_layernorm_fwd", "fp8_layernorm_fwd_q", "fp8_layernorm_bwd_workspace_bytes", "fp8_layernorm_bwd",
            "fp8_moe_route_workspace_bytes", "fp8_moe_route", "fp8_moe_route_bwd",
            "fp8_grad_norm_workspace_bytes", "fp8_grad_norm", "fp8_grad_clip",
+           "fp8_rope_table", "fp8_rope_qkv_fwd", "fp8_rope_qkv_fwd_q", "fp8_rope_qkv_bwd", "fp8_rope_qkv_bwd_q",
+           "fp8_block_norm_fwd", "fp8_block_norm_fwd_q", "fp8_block_norm_bwd_workspace_bytes", "fp8_block_norm_bwd",
+           "fp8_block_norm_bwd_q", "fp8_adamw_workspace_bytes", "fp8_adamw",
            "fp8_linear_step_host_workspace_bytes", "fp8_linear_step_host", "fp8_attention_step_host_workspace_bytes",
            "fp8_attention_step_host", "fp8_host_sync"]
 
@@ -51,7 +54,7 @@ class AttnScales(C.Structure):
 
 
 # prototypes of the calls whose arguments go through as plain numbers (addresses, sizes, flags)
-_P, _Z, _I, _F = C.c_void_p, C.c_size_t, C.c_int, C.c_float
+_P, _Z, _I, _F, _D = C.c_void_p, C.c_size_t, C.c_int, C.c_float, C.c_double
 _PROTOTYPES = {
     "fp8_embedding_fwd": (_I, [_P, _I, _Z, _Z, _P, _I, _Z, _F, _P, _P, _P]),
     "fp8_embedding_fwd_q": (_I, [_P, _I, _Z, _Z, _P, _I, _Z, _F, _P, _I, _P, _P, _P, _P]),
@@ -67,6 +70,18 @@ _PROTOTYPES = {
     "fp8_grad_norm_workspace_bytes": (_Z, [_P, _I]),
     "fp8_grad_norm": (_I, [_P, _I, _P, _P, _Z, _P]),
     "fp8_grad_clip": (_I, [_P, _I, _P, _F, _P]),
+    "fp8_rope_table": (_I, [_Z, _I, _D, _I, _D, _D, _D, _D, _D, _P, _P, _P]),
+    "fp8_rope_qkv_fwd": (_I, [_P, _Z, _Z, _I, _I, _I, _P, _P, _P, _P, _P, _P]),
+    "fp8_rope_qkv_fwd_q": (_I, [_P, _Z, _Z, _I, _I, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "fp8_rope_qkv_bwd": (_I, [_P, _P, _P, _P, _Z, _Z, _I, _I, _I, _P, _P, _Z, _P, _P]),
+    "fp8_rope_qkv_bwd_q": (_I, [_P, _P, _P, _P, _Z, _Z, _I, _I, _I, _P, _P, _I, _P, _Z, _P, _P, _P]),
+    "fp8_block_norm_fwd": (_I, [_P, _P, _P, _P, _P, _Z, _Z, _P, _P, _P, _P, _P, _P, _P]),
+    "fp8_block_norm_fwd_q": (_I, [_P, _P, _P, _P, _P, _Z, _Z, _P, _P, _I, _P, _P, _P, _P, _P, _P, _P]),
+    "fp8_block_norm_bwd_workspace_bytes": (_Z, [_Z, _Z]),
+    "fp8_block_norm_bwd": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _Z, _P, _P, _P, _P, _P, _P, _I, _P, _P, _Z, _P]),
+    "fp8_block_norm_bwd_q": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _Z, _P, _P, _I, _P, _P, _P, _P, _P, _P, _I, _P, _P, _Z, _P]),
+    "fp8_adamw_workspace_bytes": (_Z, [_P, _I]),
+    "fp8_adamw": (_I, [_P, _I, _P, _P, _D, _D, _D, _P, _F, C.c_uint64, _P, _Z, _P]),
 }
 
 
@@ -476,6 +491,255 @@ def fp8_grad_clip(items, norm, max_norm, stream=None):
     """Every output of `items` = its gradient * min(1, max_norm / (norm + 1e-6)); norm [1] FP32 stays on the device."""
     dev, st = _here(stream)
     _check(load().fp8_grad_clip(*_items(items, dev), _addr("norm", norm, _F32, _ONE, dev), max_norm, st))
+
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BY_PARTS = 0, 1, 2, 3
+NORM_NONE = 2                 # beside NORM_RMS and NORM_LAYERSCALE
+GATE_LINEAR, GATE_SIGMOID = 0, 1
+
+
+class Rope(C.Structure):
+    _fields_ = [("mode", C.c_int), ("alpha", C.c_float), ("eps", C.c_float), ("cos_table", C.c_void_p), ("sin_table", C.c_void_p),
+                ("n_pos", C.c_size_t), ("rot", C.c_int), ("interleaved", C.c_int), ("positions", C.c_void_p),
+                ("positions_are_int64", C.c_int)]
+
+
+def fp8_rope_table(cos, sin, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, original_len=1.0, turns_low=1.0, turns_high=32.0,
+                   magnitude=1.0, stream=None):
+    """cos, sin [n_pos, rot / 2] FP32 = magnitude * cos / sin of position times frequency, the frequencies changed by `scaling` (ROPE_*)."""
+    N, half = _matrix("cos", cos)
+    dev, st = _here(stream)
+    _check(load().fp8_rope_table(N, 2 * half, base, scaling, factor, original_len, turns_low, turns_high, magnitude,
+                                 _addr("cos", cos, _F32, cos.shape, dev), _addr("sin", sin, _F32, cos.shape, dev), st))
+
+
+def _rope(mode, alpha, eps, cos, sin, positions, interleaved, T, dev):
+    if cos is None:
+        return Rope(mode, alpha, eps, None, None, 0, 0, bool(interleaved), None, 0)
+    N, half = _matrix("cos", cos)
+    return Rope(mode, alpha, eps, _addr("cos", cos, _F32, cos.shape, dev), _addr("sin", sin, _F32, cos.shape, dev), N, 2 * half,
+                bool(interleaved), _opt("positions", positions, _INTS, (T,), dev),
+                positions is not None and positions.dtype is torch.int64)
+
+
+def _pitched(name, t, T, W, dev):
+    """(address, elements from row to row) of a BF16 matrix whose rows are contiguous."""
+    if t.dtype is _BF16 and t.shape == (T, W) and (W < 2 or t.stride(1) == 1) and (T < 2 or t.stride(0) >= W) and t.get_device() == dev:
+        return t.data_ptr(), t.stride(0) if T > 1 else W
+    raise ValueError(f"{name}: expects a bfloat16 matrix of shape {(T, W)} with contiguous rows on the current device, cuda:{dev}; got "
+                     f"{t.dtype} of shape {tuple(t.shape)} and strides {t.stride()} on {t.device}")
+
+
+def _heads(qkv, Hq, Hkv):
+    T, W = _matrix("qkv", qkv)
+    if Hq <= 0 or Hkv < 0 or W == 0 or W % (Hq + 2 * Hkv):
+        raise ValueError(f"qkv: rows of {W} values are not {Hq} + 2 * {Hkv} heads")
+    return T, W, W // (Hq + 2 * Hkv)
+
+
+def _rope_fwd_args(qkv, Hq, Hkv, rope, q, k, v, q8, k8, v8, stream):
+    (T, W, d), (dev, st) = _heads(qkv, Hq, Hkv), _here(stream)
+    heads = ((T, Hq, d), (T, Hkv, d), (T, Hkv, d))
+    return (dev, st, (*_pitched("qkv", qkv, T, W, dev), T, Hq, Hkv, d, C.byref(_rope(*rope, T, dev))),
+            [_opt(n, t, _BF16, s, dev) for n, t, s in zip("qkv", (q, k, v), heads)],
+            [_opt(n + "8", t, _U8, s, dev) for n, t, s in zip("qkv", (q8, k8, v8), heads)])
+
+
+def fp8_rope_qkv_fwd(qkv, Hq, Hkv, mode, alpha, eps, cos, sin, positions, interleaved, q, k, v, amax_out=None, stream=None):
+    """Rows of the QKV projection [T, (Hq + 2 Hkv) d] BF16 (rows may be strided) -> q [T, Hq, d], k, v [T, Hkv, d] BF16 (each may be
+    None): regulariser `mode` (QK_*) and rotation of Q and K by the tables cos, sin [n_pos, rot / 2] (None: no rotation) at positions
+    [T] int32 / int64 (None: t mod n_pos; outside the table: a token of zeros); amax_out [3] FP32: amax of q, k, v."""
+    dev, st, ins, outs, _ = _rope_fwd_args(qkv, Hq, Hkv, (mode, alpha, eps, cos, sin, positions, interleaved), q, k, v, None, None, None,
+                                           stream)
+    _check(load().fp8_rope_qkv_fwd(*ins, *outs, _opt("amax_out", amax_out, _F32, (3,), dev), st))
+
+
+def fp8_rope_qkv_fwd_q(qkv, Hq, Hkv, mode, alpha, eps, cos, sin, positions, interleaved, scales, fmt, q8, k8, v8, q=None, k=None,
+                       v=None, amax_out=None, stream=None):
+    """fp8_rope_qkv_fwd that also writes the FP8 codes q8, k8, v8 (each may be None) of its (BF16-rounded) results under the delayed
+    scales [3] FP32."""
+    dev, st, ins, outs, codes = _rope_fwd_args(qkv, Hq, Hkv, (mode, alpha, eps, cos, sin, positions, interleaved), q, k, v, q8, k8, v8,
+                                               stream)
+    _check(load().fp8_rope_qkv_fwd_q(*ins, _addr("scales", scales, _F32, (3,), dev), fmt, *outs, *codes,
+                                     _opt("amax_out", amax_out, _F32, (3,), dev), st))
+
+
+def _rope_bwd_args(dq, dk, dv, qkv, rope, stream):
+    if dq.dim() != 3:
+        raise ValueError(f"dq: expects [T, Hq, d], got shape {tuple(dq.shape)}")
+    (T, Hq, d), Hkv = dq.shape, 0 if dk is None else dk.shape[1]
+    dev, st = _here(stream)
+    W = (Hq + 2 * Hkv) * d
+    kv = (T, Hkv, d)
+    if (dk is None) != (dv is None):
+        raise ValueError("dk and dv come together")
+    saved = (None, 0) if qkv is None else _pitched("qkv", qkv, T, W, dev)
+    return dev, st, T, W, (_addr("dq", dq, _BF16, dq.shape, dev), _opt("dk", dk, _BF16, kv, dev), _opt("dv", dv, _BF16, kv, dev), *saved,
+                           T, Hq, Hkv, d, C.byref(_rope(*rope, T, dev)))
+
+
+def fp8_rope_qkv_bwd(dq, dk, dv, qkv, mode, alpha, eps, cos, sin, positions, interleaved, dqkv, amax_out=None, stream=None):
+    """Gradient of fp8_rope_qkv_fwd: dq [T, Hq, d], dk, dv [T, Hkv, d] BF16 (None without K and V) and the forward's qkv (None with
+    QK_NONE) -> dqkv [T, (Hq + 2 Hkv) d] BF16 (rows may be strided); amax of dqkv optional."""
+    dev, st, T, W, ins = _rope_bwd_args(dq, dk, dv, qkv, (mode, alpha, eps, cos, sin, positions, interleaved), stream)
+    _check(load().fp8_rope_qkv_bwd(*ins, *_pitched("dqkv", dqkv, T, W, dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_rope_qkv_bwd_q(dq, dk, dv, qkv, mode, alpha, eps, cos, sin, positions, interleaved, scale, fmt, dqkv8, dqkv=None, amax_out=None,
+                       stream=None):
+    """fp8_rope_qkv_bwd that writes the FP8 codes dqkv8 [T, (Hq + 2 Hkv) d] of its (BF16-rounded) result under the delayed `scale`
+    (and the result itself where dqkv is given)."""
+    dev, st, T, W, ins = _rope_bwd_args(dq, dk, dv, qkv, (mode, alpha, eps, cos, sin, positions, interleaved), stream)
+    out = (None, 0) if dqkv is None else _pitched("dqkv", dqkv, T, W, dev)
+    _check(load().fp8_rope_qkv_bwd_q(*ins, _addr("scale", scale, _F32, _ONE, dev), fmt, *out, _addr("dqkv8", dqkv8, _U8, (T, W), dev),
+                                     _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+class BlockNorm(C.Structure):
+    _fields_ = [("post", C.c_int), ("gate", C.c_int), ("x_scale", C.c_float), ("y_scale", C.c_float), ("eps", C.c_float)]
+
+
+def _block_norm_ins(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, dev):
+    T, D = _matrix("x", x)
+    return (_addr("x", x, _BF16, x.shape, dev), _opt("y", y, _BF16, x.shape, dev), _opt("gate", gate, _BF16, x.shape, dev),
+            _opt("gamma_post", gamma_post, _F32, (D,), dev), _opt("gamma_pre", gamma_pre, _F32, (D,), dev), T, D,
+            C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, eps)))
+
+
+def fp8_block_norm_fwd(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, h, out, r_post=None, r_pre=None,
+                       amax_out=None, stream=None):
+    """h = x_scale x + y_scale s z with z = gamma_post y / rms(y) (post = NORM_RMS), gamma_post y (NORM_LAYERSCALE) or y (NORM_NONE), s =
+    gate (GATE_LINEAR) or its sigmoid (GATE_SIGMOID); out = gamma_pre h / rms(h).  All [T, D] BF16 with gammas [D] FP32; y, gate, gamma_pre
+    (then out) may be None; r_post, r_pre [T] FP32 for the backward pass; amax of out (of h without gamma_pre) optional."""
+    dev, st = _here(stream)
+    s, T = x.shape, (x.shape[0],)
+    _check(load().fp8_block_norm_fwd(*_block_norm_ins(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, dev),
+                                     _opt("h", h, _BF16, s, dev), _opt("out", out, _BF16, s, dev), _opt("r_post", r_post, _F32, T, dev),
+                                     _opt("r_pre", r_pre, _F32, T, dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_block_norm_fwd_q(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, scale, fmt, h, out, out8,
+                         r_post=None, r_pre=None, amax_out=None, stream=None):
+    """fp8_block_norm_fwd that also writes the FP8 codes out8 of its (BF16-rounded) result under the delayed `scale` (out may be None)."""
+    dev, st = _here(stream)
+    s, T = x.shape, (x.shape[0],)
+    _check(load().fp8_block_norm_fwd_q(*_block_norm_ins(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, dev),
+                                       _addr("scale", scale, _F32, _ONE, dev), fmt, _opt("h", h, _BF16, s, dev),
+                                       _opt("out", out, _BF16, s, dev), _addr("out8", out8, _U8, s, dev),
+                                       _opt("r_post", r_post, _F32, T, dev), _opt("r_pre", r_pre, _F32, T, dev),
+                                       _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+
+
+def fp8_block_norm_bwd_workspace_bytes(T, D) -> int:
+    return load().fp8_block_norm_bwd_workspace_bytes(T, D)
+
+
+def _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dev):
+    s = T, D = _matrix("dx", dx)
+    return s, (_opt("dout", dout, _BF16, s, dev), _opt("dh", dh, _BF16, s, dev), _opt("h", h, _BF16, s, dev), _opt("y", y, _BF16, s, dev),
+               _opt("gate", gate, _BF16, s, dev), _opt("gamma_post", gamma_post, _F32, (D,), dev),
+               _opt("gamma_pre", gamma_pre, _F32, (D,), dev), _opt("r_post", r_post, _F32, (T,), dev),
+               _opt("r_pre", r_pre, _F32, (T,), dev), T, D, C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, 0.0)))
+
+
+def fp8_block_norm_bwd(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dy, dgate,
+                       dgamma_post, dgamma_pre, ws, accumulate=False, amax_out=None, stream=None):
+    """Gradient of fp8_block_norm_fwd from dout (None without gamma_pre) and dh (the residual stream's; None with gamma_pre alone), both
+    [T, D] BF16, and the forward's h, y, gate, r_post, r_pre: dx, dy, dgate [T, D] BF16, dgamma_post, dgamma_pre [D] FP32 (added to
+    with `accumulate`); None where there is nothing; amax of dy optional; ws: a uint8 CUDA tensor of
+    fp8_block_norm_bwd_workspace_bytes(T, D)."""
+    dev, st = _here(stream)
+    s, ins = _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dev)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_block_norm_bwd(*ins, _addr("dx", dx, _BF16, s, dev), _opt("dy", dy, _BF16, s, dev),
+                                     _opt("dgate", dgate, _BF16, s, dev), _opt("dgamma_post", dgamma_post, _F32, (s[1],), dev),
+                                     _opt("dgamma_pre", dgamma_pre, _F32, (s[1],), dev), bool(accumulate),
+                                     _opt("amax_out", amax_out, _F32, _ONE, dev), w, nw, st))
+
+
+def fp8_block_norm_bwd_q(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, scale, fmt, dx,
+                         dy, dy8, dgate, dgamma_post, dgamma_pre, ws, accumulate=False, amax_out=None, stream=None):
+    """fp8_block_norm_bwd that also writes the FP8 codes dy8 of the (BF16-rounded) dy under the delayed `scale` (dy may be None)."""
+    dev, st = _here(stream)
+    s, ins = _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dev)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_block_norm_bwd_q(*ins, _addr("scale", scale, _F32, _ONE, dev), fmt, _addr("dx", dx, _BF16, s, dev),
+                                       _opt("dy", dy, _BF16, s, dev), _addr("dy8", dy8, _U8, s, dev),
+                                       _opt("dgate", dgate, _BF16, s, dev), _opt("dgamma_post", dgamma_post, _F32, (s[1],), dev),
+                                       _opt("dgamma_pre", dgamma_pre, _F32, (s[1],), dev), bool(accumulate),
+                                       _opt("amax_out", amax_out, _F32, _ONE, dev), w, nw, st))
+
+
+class AdamWItem(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_exp", C.c_void_p),
+                ("v_exp", C.c_void_p), ("p_bf16", C.c_void_p), ("p8", C.c_void_p), ("q_scale", C.c_void_p), ("amax", C.c_void_p),
+                ("n", C.c_size_t), ("weight_decay", C.c_float), ("g_is_fp32", C.c_int), ("state_bits", C.c_int), ("fmt", C.c_int)]
+
+
+class AdamWItems:
+    """The tensors of a model as fp8_adamw takes them: built once, used every step (it keeps the tensors alive; they have to stay
+    where they are)."""
+
+    def __init__(self, params, grads, ms, vs, decays, m_exps, v_exps, params16, params8, q_scales, amaxes, fmt):
+        n = len(params)
+        lists = [params, grads, ms, vs, decays, m_exps, v_exps, params16, params8]
+        if n == 0 or any(x is not None and len(x) != n for x in lists):
+            raise ValueError(f"lists of {[None if x is None else len(x) for x in lists]} tensors")
+        dev = self.device = params[0].get_device()
+        if dev < 0:
+            raise ValueError("expects CUDA tensors")
+        if params8 is not None and q_scales is None:
+            raise ValueError("FP8 copies need their scales")
+        self.tensors = [None if x is None else list(x) for x in lists] + [q_scales, amaxes]
+        scales, maxima = _opt("q_scales", q_scales, _F32, (n,), dev), _opt("amaxes", amaxes, _F32, (n,), dev)
+        self.array = (AdamWItem * n)()
+        for i in range(n):
+            p, g, m, v = params[i], grads[i], ms[i], vs[i]
+            shape, numel, eight = p.shape, p.numel(), m.dtype is _U8
+            blocks, state = (-(-numel // 128),), _U8 if eight else _F32
+            if eight and (m_exps is None or v_exps is None):
+                raise ValueError(f"ms[{i}]: moments in 8 bits need their exponents")
+            at = lambda name, t, dt, sh: _addr(f"{name}[{i}]", t, dt, sh, dev)  # noqa: E731
+            it = self.array[i]
+            it.p, it.g = at("params", p, _F32, shape), at("grads", g, _FLOATS, shape)
+            it.m, it.v = at("ms", m, state, shape), at("vs", v, state, shape)
+            if eight:
+                it.m_exp, it.v_exp = at("m_exps", m_exps[i], _U8, blocks), at("v_exps", v_exps[i], _U8, blocks)
+            if params16 is not None and params16[i] is not None:
+                it.p_bf16 = at("params16", params16[i], _BF16, shape)
+            if params8 is not None and params8[i] is not None:
+                it.p8, it.q_scale = at("params8", params8[i], _U8, shape), scales + 4 * i
+            if maxima is not None:
+                it.amax = maxima + 4 * i
+            it.n, it.weight_decay, it.g_is_fp32, it.state_bits, it.fmt = numel, decays[i], g.dtype is _F32, 8 if eight else 32, fmt
+        written = [a for it in self.array if it.n for a in (it.p, it.m, it.v, it.m_exp, it.v_exp, it.p_bf16, it.p8) if a]
+        if len(set(written)) < len(written):
+            raise ValueError("a tensor that is written stands in the lists twice")     # tied weights would take two steps at once
+
+    def __len__(self):
+        return len(self.array)
+
+
+def fp8_adamw_items(params, grads, ms, vs, decays, m_exps=None, v_exps=None, params16=None, params8=None, q_scales=None, amaxes=None,
+                    fmt=E4M3) -> AdamWItems:
+    """The list for fp8_adamw: params FP32, grads BF16 / FP32, moments ms, vs FP32, or uint8 with exponents m_exps, v_exps (uint8, one
+    per 128 elements; all zeros to begin with), decays numbers; what the next step's products read: params16 BF16, params8 uint8
+    codes in `fmt` under q_scales [n] FP32 (each tensor or the list may be None), amaxes [n] FP32.  Every tensor once."""
+    return AdamWItems(params, grads, ms, vs, decays, m_exps, v_exps, params16, params8, q_scales, amaxes, fmt)
+
+
+def fp8_adamw_workspace_bytes(items) -> int:
+    return load().fp8_adamw_workspace_bytes(items.array, len(items.array))
+
+
+def fp8_adamw(items, lr, step, beta1, beta2, eps, ws, norm=None, max_norm=1.0, seed=0, stream=None):
+    """One AdamW step of all tensors of `items`: lr [1] FP32 and step [1] int32 (the steps taken so far; counted on) stay on the device;
+    norm [1] FP32 (of fp8_grad_norm): gradients are scaled by min(1, max_norm / (norm + 1e-6)), and a norm that is not finite skips
+    the step; seed: of the random rounding of moments in 8 bits; ws: a uint8 CUDA tensor of fp8_adamw_workspace_bytes(items)."""
+    dev, st = _here(stream)
+    w, nw = _scratch(ws, dev)
+    _check(load().fp8_adamw(*_items(items, dev), _addr("lr", lr, _F32, _ONE, dev), _addr("step", step, _I32, _ONE, dev), beta1, beta2,
+                            eps, _opt("norm", norm, _F32, _ONE, dev), max_norm, seed, w, nw, st))
 
 
 def _is_fp32(t):

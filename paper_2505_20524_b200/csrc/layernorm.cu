@@ -4,97 +4,9 @@
 
 #include "common.cuh"
 #include "elementwise.cuh"
+#include "rows.cuh"
 
 namespace fp8dpa {
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// Rows travel through a private ring in shared memory: every thread copies what it alone reads, so it needs no barrier.
-__device__ __forceinline__ uint4 ring_get(uint32_t at)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-__device__ __forceinline__ void ring_put_zero(uint32_t at)
-{
-    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
-}
-__device__ __forceinline__ void ring_put(uint32_t at, uint64_t lo, uint64_t hi)
-{
-    asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(at), "l"(lo), "l"(hi) : "memory");
-}
-__device__ __forceinline__ void ring_get(uint32_t at, uint64_t &lo, uint64_t &hi)
-{
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(lo), "=l"(hi) : "r"(at) : "memory");
-}
-
-// Eight BF16 values as four pairs for the packed FP32 instructions (two lanes each).
-__device__ __forceinline__ void unpack4x2(const uint4 v, uint64_t (&f)[4])
-{
-    f[0] = pack_u32x2(v.x << 16, v.x & 0xFFFF0000u);
-    f[1] = pack_u32x2(v.y << 16, v.y & 0xFFFF0000u);
-    f[2] = pack_u32x2(v.z << 16, v.z & 0xFFFF0000u);
-    f[3] = pack_u32x2(v.w << 16, v.w & 0xFFFF0000u);
-}
-__device__ __forceinline__ void load4x2(const float *p, uint64_t (&f)[4])
-{
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-    f[0] = pack_f32x2(a.x, a.y);
-    f[1] = pack_f32x2(a.z, a.w);
-    f[2] = pack_f32x2(b.x, b.y);
-    f[3] = pack_f32x2(b.z, b.w);
-}
-__device__ __forceinline__ uint64_t both(float v) { return pack_f32x2(v, v); }
-__device__ __forceinline__ float add_halves(uint64_t v)
-{
-    float lo, hi;
-    unpack_f32x2(v, lo, hi);
-    return lo + hi;
-}
-__device__ __forceinline__ float4 quad(uint64_t a, uint64_t b)
-{
-    float4 v;
-    unpack_f32x2(a, v.x, v.y);
-    unpack_f32x2(b, v.z, v.w);
-    return v;
-}
-__device__ __forceinline__ uint32_t round2(uint64_t v)
-{
-    float lo, hi;
-    unpack_f32x2(v, lo, hi);
-    return pack_bf16x2(lo, hi);
-}
-
-// Sum over the threads that share a row: 2^lanes_log2 neighbouring lanes, or the whole CTA of up to WARPS warps through `red` (a
-// buffer that this call alone uses until the next barrier; entries behind the CTA's warps are zero).
-template <bool CTA, int WARPS>
-__device__ __forceinline__ float row_sum(float v, int lanes_log2, float *red)
-{
-    switch (CTA ? 5 : lanes_log2) {
-    case 5: v += __shfl_xor_sync(0xffffffffu, v, 16);
-    case 4: v += __shfl_xor_sync(0xffffffffu, v, 8);
-    case 3: v += __shfl_xor_sync(0xffffffffu, v, 4);
-    case 2: v += __shfl_xor_sync(0xffffffffu, v, 2);
-    case 1: v += __shfl_xor_sync(0xffffffffu, v, 1);
-    }
-    if (CTA) {
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WARPS; w += 4) {
-            const float4 q = *reinterpret_cast<const float4 *>(red + w);
-            v += (q.x + q.y) + (q.z + q.w);
-        }
-    }
-    return v;
-}
 
 // ---------------------------------------------------------------- forward
 struct LnFwd {
@@ -112,9 +24,6 @@ struct LnFwd {
     int fmt;
 };
 
-// Who takes a row: 2^lanes_log2 lanes of a warp, a warp, or the CTA.
-enum LnUnit { LN_LANES, LN_WARP, LN_CTA };
-
 // A thread holds KG groups of eight columns of its unit's row, gamma and beta of them in registers for all the rows that the unit
 // comes by (every n-th of n units': neighbours read neighbouring rows, 38.5 us against 41.8 with a contiguous share each at
 // 8192 x 4096 with residual and codes), and the row itself between the two sums (the mean, then the squared distances from it:
@@ -123,11 +32,11 @@ enum LnUnit { LN_LANES, LN_WARP, LN_CTA };
 // zeros instead of branches, and a kernel without the residual's code took 33.5M elements from 27 to 34 us to 24 to 26.
 // With 50 to 64 KB per SM on their way memory does best, two rows ahead or, with a residual, one (8192 x 4096 with residual
 // and codes: 38.5 us; 42 with two).  rstd by rsqrtf, off by 2 ulp of FP32 at most.
-template <int KG, LnUnit UNIT, bool RES, int STAGES, int MAXT, int MINB>
+template <int KG, RowUnit UNIT, bool RES, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p, int lanes_log2)
 {
-    constexpr bool CTA = UNIT == LN_CTA;
-    if (UNIT == LN_WARP) lanes_log2 = 5;
+    constexpr bool CTA = UNIT == ROW_CTA;
+    if (UNIT == ROW_WARP) lanes_log2 = 5;
     extern __shared__ __align__(16) uint4 ring_mem[];
     __shared__ __align__(16) float red[2][MAXT / 32];
     const bool alone = amax_begin(p.amax_bits);
@@ -202,7 +111,7 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p
         }
         const float rstd = rsqrtf(fmaf(row_sum<CTA, MAXT / 32>(add_halves(ss), lanes_log2, red[1]), inv_d, p.eps));
         const uint64_t rstd2 = both(rstd);
-        const bool live = UNIT != LN_LANES || t < p.T;
+        const bool live = UNIT != ROW_LANES || t < p.T;
         if (live && lane == 0) {
             if (p.mean) p.mean[t] = mean;
             if (p.rstd) p.rstd[t] = rstd;
@@ -230,12 +139,6 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_fwd_kernel(const LnFwd p
 }
 
 // ---------------------------------------------------------------- backward
-// The rows of unit u of n: a contiguous share.
-struct Rows {
-    size_t begin, end;
-};
-__device__ __forceinline__ Rows rows_of(size_t u, size_t n, size_t T) { return {T * u / n, T * (u + 1) / n}; }
-
 struct LnBwd {
     const uint16_t *dout, *x;
     const float *gamma, *mean, *rstd;
@@ -248,7 +151,7 @@ struct LnBwd {
 // With xh = (x - mean) rstd and g = gamma dout:  dx = rstd (g - mean(g) - xh mean(g xh)), dgamma = sum over rows of dout xh,
 // dbeta = sum over rows of dout.  Persistent, rows and columns on threads as in the forward; a thread keeps its columns'
 // dgamma and dbeta in registers over all its rows, and the CTA leaves them in `partial` [CTA][2][D] for
-// layernorm_bwd_sum_kernel.  x and dout are read once, dx is written once.  A warp loads mean and rstd of 32 of its rows at a
+// column_sums_kernel.  x and dout are read once, dx is written once.  A warp loads mean and rstd of 32 of its rows at a
 // time: when all CTAs read those of neighbouring rows one by one, the few lines that hold them were what bound the kernel
 // (8192 x 4096: 52.7 us).  Up to KG = 2 (8192 columns) xh, g and gamma stay in registers between the sums and dx (4000 x 8192:
 // 37 us, memory's 30); with KG = 4 xh and g are formed again from the ring and gamma lies behind it, with one CTA per SM
@@ -256,13 +159,13 @@ struct LnBwd {
 // barriers cost more than the second look at the row).
 __host__ __device__ constexpr int ln_bwd_stages(int kg) { return kg > 2 ? 2 : 3; }
 constexpr size_t ln_bwd_shared(int kg, unsigned threads) { return (size_t)(ln_bwd_stages(kg) + (kg > 2)) * 2 * kg * 16 * threads; }
-template <int KG, LnUnit UNIT, int MAXT, int MINB>
+template <int KG, RowUnit UNIT, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) layernorm_bwd_kernel(const LnBwd p, int lanes_log2)
 {
     cudaTriggerProgrammaticLaunchCompletion();
-    constexpr bool CTA = UNIT == LN_CTA, KEEP = KG <= 2;
+    constexpr bool CTA = UNIT == ROW_CTA, KEEP = KG <= 2;
     constexpr int STAGES = ln_bwd_stages(KG);
-    if (UNIT == LN_WARP) lanes_log2 = 5;
+    if (UNIT == ROW_WARP) lanes_log2 = 5;
     extern __shared__ __align__(16) uint4 ring_mem[];
     __shared__ __align__(16) float2 red[2][MAXT / 32];
     const unsigned span = CTA ? blockDim.x : 1u << lanes_log2, lane = CTA ? threadIdx.x : threadIdx.x & (span - 1);
@@ -320,7 +223,7 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_bwd_kernel(const LnBwd p
         rs_ahead = __ldg(p.rstd + rows.begin + (threadIdx.x & 31));
     }
     for (size_t first = rows.begin; first < rows.end; first += at_once, at += pitch, flip ^= 1) {
-        const bool live = UNIT != LN_LANES || first + sub < rows.end;
+        const bool live = UNIT != ROW_LANES || first + sub < rows.end;
         cp_async_wait<STAGES - 2>();
         fetch(fill);                             // the stage of the row before this one
         fill = now;
@@ -366,7 +269,7 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_bwd_kernel(const LnBwd p
             }
         }
         float s1 = add_halves(a1), s2 = add_halves(a2);
-        for (int off = UNIT != LN_LANES ? 16 : (1 << lanes_log2) >> 1; off > 0; off >>= 1) {
+        for (int off = UNIT != ROW_LANES ? 16 : (1 << lanes_log2) >> 1; off > 0; off >>= 1) {
             s1 += __shfl_xor_sync(0xffffffffu, s1, off);
             s2 += __shfl_xor_sync(0xffffffffu, s2, off);
         }
@@ -450,43 +353,11 @@ __global__ void __launch_bounds__(MAXT, MINB) layernorm_bwd_kernel(const LnBwd p
     }
 }
 
-// dgamma and dbeta from the CTAs' sums: 32 columns per CTA, a warp takes every 32nd of the sums, then the warps in order.
-__global__ void __launch_bounds__(1024) layernorm_bwd_sum_kernel(const float *__restrict__ partial, int parts, unsigned D,
-                                                                 float *__restrict__ dgamma, float *__restrict__ dbeta,
-                                                                 int accumulate)
-{
-    cudaGridDependencySynchronize();
-    __shared__ float red[32][33];
-    const unsigned j = blockIdx.x * 32 + (threadIdx.x & 31);      // over [2][D]
-    const int r = threadIdx.x >> 5;
-    float s = 0.0f;
-    if (j < 2 * D) {
-#pragma unroll 8
-        for (int c = r; c < parts; c += 32) s += __ldcg(partial + (size_t)c * 2 * D + j);
-    }
-    red[r][threadIdx.x & 31] = s;
-    __syncthreads();
-    s = red[threadIdx.x & 31][r];                                 // transposed: warp r adds the 32 sums of column r
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    const unsigned col = blockIdx.x * 32 + r;
-    if ((threadIdx.x & 31) == 0 && col < 2 * D) {
-        float *o = col < D ? dgamma + col : dbeta + (col - D);
-        *o = accumulate ? *o + s : s;
-    }
-}
-
 struct LnShape {
     bool cta;
     int lanes_log2;
     unsigned threads, grid;
 };
-static int log2_at_least(unsigned n)
-{
-    int l = 0;
-    while ((1u << l) < n) ++l;
-    return l;
-}
 // Forward: two groups of columns per thread on lanes of a warp up to 256 columns (65536 x 64: 5.0 us where a warp per row took
 // 16.5, x 256: 14.1 where it took 17.2), on a warp up to 512, on the CTA between 1032 and 4096; four on a warp up to 1024
 // and on the CTA above 4096.
@@ -532,7 +403,7 @@ static int ln_launch(const P &p, const LnShape &s, size_t smem, size_t most, uns
     return launch_behind_amax<Kernel>(p.T * p.n8 * 8, amax, s.grid, s.threads, smem, st, p, s.lanes_log2);
 }
 
-template <int KG, LnUnit UNIT, bool RES, int STAGES, int MAXT, int MINB>
+template <int KG, RowUnit UNIT, bool RES, int STAGES, int MAXT, int MINB>
 static int ln_fwd_launch(const LnFwd &p, const LnShape &s, cudaStream_t st)
 {
     constexpr size_t per_thread = STAGES * (RES ? 2 : 1) * KG * 16;
@@ -544,18 +415,18 @@ static int ln_fwd_run(const LnFwd &p, size_t D, cudaStream_t st)
 {
     constexpr int STAGES = RES ? 2 : 3;
     const LnShape s = ln_fwd_shape(p.T, D);
-    if (D <= 256) return ln_fwd_launch<2, LN_LANES, RES, STAGES, 256, 3>(p, s, st);
-    if (D <= 512) return ln_fwd_launch<2, LN_WARP, RES, STAGES, 256, 3>(p, s, st);
-    if (D <= 1024) return ln_fwd_launch<4, LN_WARP, RES, STAGES, 256, 2>(p, s, st);
-    if (D <= 4096) return ln_fwd_launch<2, LN_CTA, RES, STAGES, 256, 3>(p, s, st);
-    if (D <= 8192) return ln_fwd_launch<4, LN_CTA, RES, STAGES, 256, 2>(p, s, st);
+    if (D <= 256) return ln_fwd_launch<2, ROW_LANES, RES, STAGES, 256, 3>(p, s, st);
+    if (D <= 512) return ln_fwd_launch<2, ROW_WARP, RES, STAGES, 256, 3>(p, s, st);
+    if (D <= 1024) return ln_fwd_launch<4, ROW_WARP, RES, STAGES, 256, 2>(p, s, st);
+    if (D <= 4096) return ln_fwd_launch<2, ROW_CTA, RES, STAGES, 256, 3>(p, s, st);
+    if (D <= 8192) return ln_fwd_launch<4, ROW_CTA, RES, STAGES, 256, 2>(p, s, st);
     // one CTA of up to 384 threads per SM: with two stages too little travels (3000 x 10000 with codes: 42.0 us, 38.4 with three)
     if constexpr (RES)
-        if (D <= 12288) return ln_fwd_launch<4, LN_CTA, true, 3, 384, 1>(p, s, st);
-    return ln_fwd_launch<4, LN_CTA, RES, STAGES, 512, 1>(p, s, st);
+        if (D <= 12288) return ln_fwd_launch<4, ROW_CTA, true, 3, 384, 1>(p, s, st);
+    return ln_fwd_launch<4, ROW_CTA, RES, STAGES, 512, 1>(p, s, st);
 }
 
-template <int KG, LnUnit UNIT, int MAXT, int MINB>
+template <int KG, RowUnit UNIT, int MAXT, int MINB>
 static int ln_bwd_launch(const LnBwd &p, const LnShape &s, cudaStream_t st)
 {
     return ln_launch<layernorm_bwd_kernel<KG, UNIT, MAXT, MINB>>(p, s, ln_bwd_shared(KG, s.threads), ln_bwd_shared(KG, MAXT),
@@ -652,13 +523,13 @@ extern "C" int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, cons
     float *partial = static_cast<float *>(ws);
     LnBwd p = {static_cast<const uint16_t *>(dout_bf16), static_cast<const uint16_t *>(x_bf16), gamma, mean, rstd, T,
                (unsigned)(D / 8), static_cast<uint16_t *>(dx_bf16), partial};
-    if (D <= 128) rc = ln_bwd_launch<1, LN_LANES, 256, 3>(p, s, st);
-    else if (D <= 256) rc = ln_bwd_launch<1, LN_WARP, 256, 3>(p, s, st);
-    else if (D <= 512) rc = ln_bwd_launch<2, LN_WARP, 256, 2>(p, s, st);
-    else if (D <= 4096) rc = ln_bwd_launch<2, LN_CTA, 256, 2>(p, s, st);
-    else if (D <= 8192) rc = ln_bwd_launch<2, LN_CTA, 512, 1>(p, s, st);
-    else rc = ln_bwd_launch<4, LN_CTA, 512, 1>(p, s, st);
+    if (D <= 128) rc = ln_bwd_launch<1, ROW_LANES, 256, 3>(p, s, st);
+    else if (D <= 256) rc = ln_bwd_launch<1, ROW_WARP, 256, 3>(p, s, st);
+    else if (D <= 512) rc = ln_bwd_launch<2, ROW_WARP, 256, 2>(p, s, st);
+    else if (D <= 4096) rc = ln_bwd_launch<2, ROW_CTA, 256, 2>(p, s, st);
+    else if (D <= 8192) rc = ln_bwd_launch<2, ROW_CTA, 512, 1>(p, s, st);
+    else rc = ln_bwd_launch<4, ROW_CTA, 512, 1>(p, s, st);
     if (rc != FP8_OK) return rc;
-    return launch_early(layernorm_bwd_sum_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, partial, (int)s.grid,
+    return launch_early(column_sums_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, partial, (int)s.grid,
                         (unsigned)D, dgamma, dbeta, accumulate ? 1 : 0);
 }

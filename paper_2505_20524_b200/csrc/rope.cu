@@ -1,0 +1,527 @@
+// Rotary positions on the heads of the fused QKV projection, with the QK regulariser in front of them, the amax and FP8 codes of
+// the attention's three operands behind them, the gradient of all that, and the table of angles for long contexts.
+#include <math.h>
+
+#include "common.cuh"
+#include "elementwise.cuh"
+
+namespace fp8dpa {
+
+// ---------------------------------------------------------------- table
+constexpr int ROPE_MAX_PAIRS = 128;
+struct RopeTable {
+    double turns[ROPE_MAX_PAIRS];        // turns of each pair per position
+    float *cos_t, *sin_t;
+    size_t rows;
+    int pairs;
+    float magnitude;
+};
+
+// The angle in turns is a product in 64 bits, good to 2^-52 of itself; what is left of it next to the nearest quarter turn is
+// rounded to FP32, so that cos and sin are good to 2 ulp wherever the position lies, next to their zeros too.
+__global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__ RopeTable t)
+{
+    const unsigned quads = t.pairs / 4;
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t pos = i / quads;
+    const unsigned q = (unsigned)(i - pos * quads);
+    if (pos >= t.rows) return;
+    float c[4], s[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const double turns = (double)pos * t.turns[4 * q + e];
+        const double quarter = rint(4.0 * turns);
+        const float rest = (float)fma(-0.25, quarter, turns);                    // in [-1/8, 1/8]
+        const int k = (int)((long long)quarter & 3);
+        float sn, cs;
+        sincospif(2.0f * rest, &sn, &cs);
+        const float x = k & 1 ? -sn : cs, y = k & 1 ? cs : sn;
+        c[e] = (k & 2 ? -x : x) * t.magnitude;
+        s[e] = (k & 2 ? -y : y) * t.magnitude;
+    }
+    reinterpret_cast<float4 *>(t.cos_t)[i] = make_float4(c[0], c[1], c[2], c[3]);
+    reinterpret_cast<float4 *>(t.sin_t)[i] = make_float4(s[0], s[1], s[2], s[3]);
+}
+
+// ---------------------------------------------------------------- heads
+struct RopeArgs {
+    const uint16_t *qkv;                 // rows of (Hq + 2 Hkv) heads, `pitch` elements apart (NULL: the gradient without a regulariser)
+    size_t pitch;
+    size_t T;
+    int heads[3];                        // Hq, Hkv, Hkv
+    int d, rot;                          // rot = 0: no rotation
+    float alpha, eps, inv_d;
+    const float *cos_t, *sin_t;
+    size_t n_pos;
+    const void *positions;
+    int wide_positions;
+    const uint16_t *grad[3];             // backward: gradients of q, k, v
+    uint16_t *out[3];                    // forward: q, k, v; backward: out[0] = dqkv with rows `out_pitch` elements apart
+    size_t out_pitch;
+    uint8_t *out8[3];                    // forward: codes of q, k, v; backward: out8[0] = codes of dqkv, contiguous rows
+    const float *scales;
+    unsigned int *amax_bits;             // forward: three; backward: one
+    int fmt;
+    int lanes_log2;                      // lanes per head: a power of two, at least d / 16
+    int chunks[3];                       // pieces of ROPE_HEADS heads of each of q, k, v
+    int tokens;                          // tokens per CTA
+};
+constexpr int ROPE_HEADS = 4;
+
+__device__ __forceinline__ void unpack8(const uint4 w, float (&f)[8])
+{
+    f[0] = bf16_lo(w.x); f[1] = bf16_hi(w.x); f[2] = bf16_lo(w.y); f[3] = bf16_hi(w.y);
+    f[4] = bf16_lo(w.z); f[5] = bf16_hi(w.z); f[6] = bf16_lo(w.w); f[7] = bf16_hi(w.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8])
+{
+    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+
+// The rotation of a lane's two groups of eight: partners are the same places of the two groups, or neighbours in each.
+template <bool PAIRS, bool BACK>
+__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&sn)[8])
+{
+    if (PAIRS) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float s0 = BACK ? -sn[e] : sn[e], s1 = BACK ? -sn[4 + e] : sn[4 + e];
+            const float x = a[2 * e], y = a[2 * e + 1], z = b[2 * e], w = b[2 * e + 1];
+            a[2 * e] = x * c[e] - y * s0;
+            a[2 * e + 1] = y * c[e] + x * s0;
+            b[2 * e] = z * c[4 + e] - w * s1;
+            b[2 * e + 1] = w * c[4 + e] + z * s1;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float s = BACK ? -sn[e] : sn[e];
+            const float ra = a[e] * c[e] - b[e] * s, rb = b[e] * c[e] + a[e] * s;
+            a[e] = ra;
+            b[e] = rb;
+        }
+    }
+}
+
+// 1 - tanh(x)^2 = 4 e / (1 + e)^2 with e = exp(-2 |x|): no cancellation where tanh is near 1.
+__device__ __forceinline__ float sech2(float x)
+{
+    const float e = ex2_approx(-2.8853900817779268f * fabsf(x));
+    return __fdividef(4.0f * e, (1.0f + e) * (1.0f + e));
+}
+
+template <int N>
+__device__ __forceinline__ void block_max_each(const uint32_t (&m2)[N], unsigned int *amax_bits, bool alone)
+{
+    __shared__ uint32_t warp_max[N][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t m = __reduce_max_sync(0xffffffffu, max(m2[i] & 0xFFFFu, m2[i] >> 16));
+        if (lane == 0) warp_max[i][warp] = m;
+    }
+    __syncthreads();
+    const int nwarps = blockDim.x >> 5;
+    for (int i = warp; i < N; i += nwarps) {
+        const uint32_t m = __reduce_max_sync(0xffffffffu, lane < nwarps ? warp_max[i][lane] : 0u);
+        if (lane == 0) {
+            if (alone) amax_bits[i] = m << 16;
+            else if (m != 0u) atomicMax(amax_bits + i, m << 16);
+        }
+    }
+}
+
+// A head is on 2^lanes_log2 neighbouring lanes, 16 elements each: below `rot` lane j holds elements [8 j, 8 j + 8) and the same
+// of the rotated part's second half, so that both kinds of partners are in one lane; behind it 16 in a row, which pass through.
+// A group of lanes takes up to ROPE_HEADS heads of one token and tensor with the token's angles in registers; a CTA takes whole
+// tokens.  Bytes bind: every element is read once and written once.
+template <int MODE, bool PAIRS, bool BACK>
+__global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeArgs p)
+{
+    const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log2;
+    const int groups = blockDim.x >> p.lanes_log2;
+    const int slots = p.d / 16, turned = p.rot / 16;
+    const int per_token = p.chunks[0] + p.chunks[1] + p.chunks[2], items = per_token * p.tokens;
+    const bool here = j < slots, turns = j < turned;
+    const int lo = turns ? 8 * j : p.rot + 16 * (j - turned), hi = turns ? p.rot / 2 + 8 * j : lo + 8;
+    const int row = p.heads[0] + p.heads[1] + p.heads[2];
+    uint32_t m[BACK ? 1 : 3];
+#pragma unroll
+    for (int i = 0; i < (BACK ? 1 : 3); ++i) m[i] = 0u;
+    for (int first = 0; first < items; first += groups) {     // the same trip count for every lane: shuffles below
+        const int item = first + group, local = min(item, items - 1) / per_token;
+        int piece = min(item, items - 1) - local * per_token;
+        const size_t t = (size_t)blockIdx.x * p.tokens + local;
+        const bool live = here && item < items && t < p.T;
+        const int part = piece < p.chunks[0] ? 0 : piece < p.chunks[0] + p.chunks[1] ? 1 : 2;
+        if (part > 0) piece -= p.chunks[0];
+        if (part > 1) piece -= p.chunks[1];
+        const int h0 = piece * ROPE_HEADS, n_heads = p.heads[part];
+        const int before = (part > 0 ? p.heads[0] : 0) + (part > 1 ? p.heads[1] : 0);       // heads of the row in front
+        size_t pos = 0;
+        bool known = true;
+        if (live) {
+            if (p.positions) {
+                const long long at = p.wide_positions ? static_cast<const long long *>(p.positions)[t]
+                                                      : (long long)static_cast<const int *>(p.positions)[t];
+                known = at >= 0 && (unsigned long long)at < p.n_pos;
+                pos = known ? (size_t)at : 0;
+            } else if (p.rot) {
+                pos = t % p.n_pos;
+            }
+        }
+        float c[8], sn[8];
+        if (live && turns && known && part < 2) {
+            const float *pc = p.cos_t + pos * (p.rot / 2), *ps = p.sin_t + pos * (p.rot / 2);
+            const int i0 = PAIRS ? 4 * j : 8 * j, i1 = PAIRS ? p.rot / 4 + 4 * j : 8 * j + 4;
+            const float4 c0 = __ldg(reinterpret_cast<const float4 *>(pc + i0)), c1 = __ldg(reinterpret_cast<const float4 *>(pc + i1));
+            const float4 s0 = __ldg(reinterpret_cast<const float4 *>(ps + i0)), s1 = __ldg(reinterpret_cast<const float4 *>(ps + i1));
+            c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
+            sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
+        }
+        const float qs = p.scales ? __ldg(p.scales + (BACK ? 0 : part)) : 1.0f;
+#pragma unroll
+        for (int hh = 0; hh < ROPE_HEADS; ++hh) {
+            const int h = h0 + hh;
+            const bool valid = live && known && h < n_heads, regular = valid && part < 2;
+            float a[8], b[8], x[8], y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[e] = b[e] = x[e] = y[e] = 0.0f;
+            const size_t in_row = t * p.pitch + (size_t)(before + h) * p.d, in_head = (t * n_heads + h) * p.d;
+            if (valid) {
+                const uint16_t *src = BACK ? p.grad[part] + in_head : p.qkv + in_row;
+                unpack8(__ldg(reinterpret_cast<const uint4 *>(src + lo)), a);
+                unpack8(__ldg(reinterpret_cast<const uint4 *>(src + hi)), b);
+            }
+            if (BACK && MODE != FP8_QK_NONE && regular) {
+                unpack8(__ldg(reinterpret_cast<const uint4 *>(p.qkv + in_row + lo)), x);
+                unpack8(__ldg(reinterpret_cast<const uint4 *>(p.qkv + in_row + hi)), y);
+            }
+            float r = 1.0f;
+            if (MODE == FP8_QK_RMS) {
+                float ss = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = BACK ? fmaf(x[e], x[e], fmaf(y[e], y[e], ss)) : fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+                for (int off = lanes >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                r = rsqrtf(fmaf(ss, p.inv_d, p.eps));
+            }
+            if (!BACK && regular) {
+                if (MODE == FP8_QK_RMS) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { a[e] *= r; b[e] *= r; }
+                } else if (MODE == FP8_QK_TANH) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { a[e] = tanhf(p.alpha * a[e]); b[e] = tanhf(p.alpha * b[e]); }
+                }
+            }
+            if (regular && turns) rotate<PAIRS, BACK>(a, b, c, sn);
+            if (BACK && MODE == FP8_QK_RMS) {
+                float s = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { x[e] *= r; y[e] *= r; s = fmaf(a[e], x[e], fmaf(b[e], y[e], s)); }
+                if (!regular) s = 0.0f;                        // r is without meaning there
+                for (int off = lanes >> 1; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                s *= p.inv_d;
+                if (regular) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { a[e] = r * fmaf(-s, x[e], a[e]); b[e] = r * fmaf(-s, y[e], b[e]); }
+                }
+            }
+            if (BACK && MODE == FP8_QK_TANH && regular) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { a[e] *= p.alpha * sech2(p.alpha * x[e]); b[e] *= p.alpha * sech2(p.alpha * y[e]); }
+            }
+            const uint4 oa = pack8(a), ob = pack8(b);
+            const uint32_t wa[4] = {oa.x, oa.y, oa.z, oa.w}, wb[4] = {ob.x, ob.y, ob.z, ob.w};
+            if (valid) {
+                uint32_t most = 0u;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) most = absmax2e(absmax2e(most, wa[q]), wb[q]);
+                if (BACK) {
+                    m[0] = __vmaxu2(m[0], most);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) m[i % (BACK ? 1 : 3)] = __vmaxu2(m[i % (BACK ? 1 : 3)], part == i ? most : 0u);
+                }
+            }
+            if (live && h < n_heads) {                         // a token outside the table: zeros
+                uint16_t *o = BACK ? p.out[0] : p.out[part];
+                uint8_t *o8 = BACK ? p.out8[0] : p.out8[part];
+                if (o) {
+                    o += BACK ? t * p.out_pitch + (size_t)(before + h) * p.d : in_head;
+                    *reinterpret_cast<uint4 *>(o + lo) = oa;
+                    *reinterpret_cast<uint4 *>(o + hi) = ob;
+                }
+                if (o8) {
+                    o8 += BACK ? (t * row + before + h) * p.d : in_head;
+                    *reinterpret_cast<uint2 *>(o8 + lo) = bf16x8_to_fp8x8(wa, qs, p.fmt);
+                    *reinterpret_cast<uint2 *>(o8 + hi) = bf16x8_to_fp8x8(wb, qs, p.fmt);
+                }
+            }
+        }
+    }
+    if (p.amax_bits) block_max_each(m, p.amax_bits, gridDim.x == 1);
+}
+
+template <bool BACK>
+static int rope_launch(RopeArgs &p, int mode, bool pairs, cudaStream_t st)
+{
+    const int slots = p.d / 16;
+    p.lanes_log2 = 0;
+    while ((1 << p.lanes_log2) < slots) ++p.lanes_log2;
+    int per_token = 0;
+    for (int i = 0; i < 3; ++i) {
+        // the forward leaves out what is not asked for
+        const bool wanted = BACK || p.out[i] || p.out8[i] || p.amax_bits;
+        p.chunks[i] = wanted ? (p.heads[i] + ROPE_HEADS - 1) / ROPE_HEADS : 0;
+        per_token += p.chunks[i];
+    }
+    const int threads_per_token = per_token << p.lanes_log2;
+    p.tokens = threads_per_token >= 256 ? 1 : 256 / threads_per_token;
+    if ((size_t)p.tokens > p.T) p.tokens = (int)p.T;
+    int threads = (threads_per_token * p.tokens + 31) & ~31;
+    if (threads > 512) threads = 512;
+    const size_t grid = (p.T + p.tokens - 1) / p.tokens;
+    if (p.amax_bits && grid > 1) FP8_CUDA_CHECK(cudaMemsetAsync(p.amax_bits, 0, (BACK ? 1 : 3) * sizeof(float), st));
+#define FP8DPA_LAUNCH_ROPE(MODE) \
+    do { \
+        if (pairs) rope_kernel<MODE, true, BACK><<<(unsigned)grid, threads, 0, st>>>(p); \
+        else rope_kernel<MODE, false, BACK><<<(unsigned)grid, threads, 0, st>>>(p); \
+    } while (0)
+    if (mode == FP8_QK_RMS) FP8DPA_LAUNCH_ROPE(FP8_QK_RMS);
+    else if (mode == FP8_QK_TANH) FP8DPA_LAUNCH_ROPE(FP8_QK_TANH);
+    else FP8DPA_LAUNCH_ROPE(FP8_QK_NONE);
+#undef FP8DPA_LAUNCH_ROPE
+    FP8_CUDA_CHECK(cudaGetLastError());
+    return FP8_OK;
+}
+
+// What both directions check of an fp8_rope; 0 or a status.
+static int rope_check(const char *who, size_t T, int Hq, int Hkv, int d, const fp8_rope *r)
+{
+    if (!r) {
+        set_error("%s: NULL rope", who);
+        return FP8_ERR_NULL;
+    }
+    if (r->mode < FP8_QK_RMS || r->mode > FP8_QK_NONE) {
+        set_error("%s: mode %d is not FP8_QK_RMS / FP8_QK_TANH / FP8_QK_NONE", who, r->mode);
+        return FP8_ERR_ENUM;
+    }
+    if (T == 0 || T > 0x7FFFFFFFull || Hq <= 0 || Hkv < 0 || Hq > 65536 || Hkv > 65536 || d <= 0 || d % 16 || d > 256) {
+        set_error("%s: unsupported shape T=%zu Hq=%d Hkv=%d d=%d (d %% 16 == 0, d <= 256, up to 65536 heads)", who, T, Hq, Hkv, d);
+        return FP8_ERR_SHAPE;
+    }
+    if (r->rot < 0 || r->rot > d || r->rot % 16 || (r->rot && (r->n_pos == 0 || r->n_pos > 0x7FFFFFFFull)) || !(r->eps >= 0.0f) ||
+        !(r->alpha - r->alpha == 0.0f)) {
+        set_error("%s: unsupported rot=%d (rot %% 16 == 0, rot <= d) or n_pos=%zu, eps < 0 or alpha not finite", who, r->rot, r->n_pos);
+        return FP8_ERR_SHAPE;
+    }
+    if (r->rot && (!r->cos_table || !r->sin_table)) {
+        set_error("%s: NULL table", who);
+        return FP8_ERR_NULL;
+    }
+    if (!aligned16(r->cos_table) || !aligned16(r->sin_table) || !aligned_to(r->positions, r->positions_are_int64 ? 8 : 4)) {
+        set_error("%s: tables must be 16-byte aligned, positions to their own type", who);
+        return FP8_ERR_ALIGN;
+    }
+    return FP8_OK;
+}
+
+static void rope_fill(RopeArgs &p, size_t T, int Hq, int Hkv, int d, const fp8_rope *r, int fmt)
+{
+    p.T = T;
+    p.heads[0] = Hq;
+    p.heads[1] = p.heads[2] = Hkv;
+    p.d = d;
+    p.rot = r->rot;
+    p.alpha = r->alpha;
+    p.eps = r->eps;
+    p.inv_d = 1.0f / (float)d;
+    p.cos_t = r->cos_table;
+    p.sin_t = r->sin_table;
+    p.n_pos = r->n_pos;
+    p.positions = r->rot ? r->positions : nullptr;
+    p.wide_positions = r->positions_are_int64;
+    p.fmt = fmt;
+}
+
+static int rope_fwd(const char *who, const void *qkv, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *r,
+                    const float *scales, int fmt, void *q, void *k, void *v, uint8_t *q8, uint8_t *k8, uint8_t *v8, float *amax_out,
+                    void *stream)
+{
+    int rc = rope_check(who, T, Hq, Hkv, d, r);
+    if (rc != FP8_OK) return rc;
+    if (!qkv || !(q || k || v || q8 || k8 || v8)) {
+        set_error("%s: NULL qkv, or nothing to write", who);
+        return FP8_ERR_NULL;
+    }
+    const size_t row = ((size_t)Hq + 2 * (size_t)Hkv) * d;
+    if (pitch < row || pitch % 8 || pitch > ((size_t)1 << 40)) {
+        set_error("%s: pitch of %zu elements (rows of %zu, multiples of 8)", who, pitch, row);
+        return FP8_ERR_SHAPE;
+    }
+    if (Hkv == 0 && (k || v || k8 || v8)) {
+        set_error("%s: outputs of K or V without heads of them", who);
+        return FP8_ERR_SHAPE;
+    }
+    if (!aligned16(qkv) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q8) || !aligned16(k8) || !aligned16(v8)) {
+        set_error("%s: tensor pointers must be 16-byte aligned", who);
+        return FP8_ERR_ALIGN;
+    }
+    rc = check_arch();
+    if (rc != FP8_OK) return rc;
+    RopeArgs p = {};
+    p.qkv = static_cast<const uint16_t *>(qkv);
+    p.pitch = pitch;
+    rope_fill(p, T, Hq, Hkv, d, r, fmt);
+    void *const out[3] = {q, k, v};
+    uint8_t *const out8[3] = {q8, k8, v8};
+    for (int i = 0; i < 3; ++i) {
+        p.out[i] = static_cast<uint16_t *>(out[i]);
+        p.out8[i] = out8[i];
+    }
+    p.scales = scales;
+    p.amax_bits = reinterpret_cast<unsigned int *>(amax_out);
+    return rope_launch<false>(p, r->mode, r->interleaved != 0, static_cast<cudaStream_t>(stream));
+}
+
+static int rope_bwd(const char *who, const void *dq, const void *dk, const void *dv, const void *qkv, size_t pitch, size_t T,
+                    int Hq, int Hkv, int d, const fp8_rope *r, const float *scale, int fmt, void *dqkv, size_t out_pitch,
+                    uint8_t *dqkv8, float *amax_out, void *stream)
+{
+    int rc = rope_check(who, T, Hq, Hkv, d, r);
+    if (rc != FP8_OK) return rc;
+    if (!dq || (Hkv && (!dk || !dv)) || (!qkv && r->mode != FP8_QK_NONE)) {
+        set_error("%s: NULL pointer (qkv may be missing with FP8_QK_NONE alone)", who);
+        return FP8_ERR_NULL;
+    }
+    const size_t row = ((size_t)Hq + 2 * (size_t)Hkv) * d;
+    if ((qkv && (pitch < row || pitch % 8 || pitch > ((size_t)1 << 40))) ||
+        (dqkv && (out_pitch < row || out_pitch % 8 || out_pitch > ((size_t)1 << 40)))) {
+        set_error("%s: pitches of %zu and %zu elements (rows of %zu, multiples of 8)", who, pitch, out_pitch, row);
+        return FP8_ERR_SHAPE;
+    }
+    if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(qkv) || !aligned16(dqkv) || !aligned16(dqkv8)) {
+        set_error("%s: tensor pointers must be 16-byte aligned", who);
+        return FP8_ERR_ALIGN;
+    }
+    rc = check_arch();
+    if (rc != FP8_OK) return rc;
+    RopeArgs p = {};
+    p.qkv = static_cast<const uint16_t *>(qkv);
+    p.pitch = pitch;
+    rope_fill(p, T, Hq, Hkv, d, r, fmt);
+    const void *const grad[3] = {dq, dk, dv};
+    for (int i = 0; i < 3; ++i) p.grad[i] = static_cast<const uint16_t *>(grad[i]);
+    p.out[0] = static_cast<uint16_t *>(dqkv);
+    p.out_pitch = out_pitch;
+    p.out8[0] = dqkv8;
+    p.scales = scale;
+    p.amax_bits = reinterpret_cast<unsigned int *>(amax_out);
+    return rope_launch<true>(p, r->mode, r->interleaved != 0, static_cast<cudaStream_t>(stream));
+}
+
+static int check_codes(const char *who, const void *scale, int fmt, bool any)
+{
+    if (!scale || !any) {
+        set_error("%s: NULL scale or codes", who);
+        return FP8_ERR_NULL;
+    }
+    if (fmt != FP8_E4M3 && fmt != FP8_E5M2) {
+        set_error("%s: fmt %d is not FP8_E4M3 / FP8_E5M2", who, fmt);
+        return FP8_ERR_ENUM;
+    }
+    return FP8_OK;
+}
+
+}  // namespace fp8dpa
+
+using namespace fp8dpa;
+
+extern "C" int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, double factor, double original_len, double turns_low,
+                              double turns_high, double magnitude, float *cos_table, float *sin_table, void *stream)
+{
+    if (!cos_table || !sin_table) {
+        set_error("fp8_rope_table: NULL table");
+        return FP8_ERR_NULL;
+    }
+    if (scaling < FP8_ROPE_PLAIN || scaling > FP8_ROPE_BY_PARTS) {
+        set_error("fp8_rope_table: scaling %d is not a known enum value", scaling);
+        return FP8_ERR_ENUM;
+    }
+    const bool scaled = scaling != FP8_ROPE_PLAIN, parts = scaling == FP8_ROPE_BY_PARTS;
+    if (n_pos == 0 || n_pos > 0x7FFFFFFFull || rot <= 0 || rot % 16 || rot > 2 * ROPE_MAX_PAIRS || !(base > 0.0) || isinf(base) ||
+        !(magnitude > 0.0) || isinf(magnitude) || (scaled && (!(factor > 0.0) || isinf(factor))) ||
+        (parts && (!(original_len > 0.0) || isinf(original_len) || !(turns_high > turns_low) || isinf(turns_high) || isinf(turns_low)))) {
+        set_error("fp8_rope_table: unsupported n_pos=%zu rot=%d (rot %% 16 == 0, rot <= 256) or a parameter that is not a positive "
+                  "number", n_pos, rot);
+        return FP8_ERR_SHAPE;
+    }
+    if (!aligned16(cos_table) || !aligned16(sin_table)) {
+        set_error("fp8_rope_table: tables must be 16-byte aligned");
+        return FP8_ERR_ALIGN;
+    }
+    int rc = check_arch();
+    if (rc != FP8_OK) return rc;
+    RopeTable t = {};
+    const double full_turn = 6.283185307179586477;
+    if (scaling == FP8_ROPE_NTK) base *= pow(factor, rot / (rot - 2.0));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot);
+        if (scaling == FP8_ROPE_LINEAR) f /= factor;
+        if (parts) {
+            double w = (original_len * f / full_turn - turns_low) / (turns_high - turns_low);
+            w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+            f = (1.0 - w) * f / factor + w * f;
+        }
+        t.turns[i] = f / full_turn;
+    }
+    t.cos_t = cos_table;
+    t.sin_t = sin_table;
+    t.rows = n_pos;
+    t.pairs = rot / 2;
+    t.magnitude = (float)magnitude;
+    const size_t threads = n_pos * (size_t)(rot / 8);
+    rope_table_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(t);
+    FP8_CUDA_CHECK(cudaGetLastError());
+    return FP8_OK;
+}
+
+extern "C" int fp8_rope_qkv_fwd(const void *qkv_bf16, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *rope,
+                                void *q_bf16, void *k_bf16, void *v_bf16, float *amax_out, void *stream)
+{
+    return rope_fwd("fp8_rope_qkv_fwd", qkv_bf16, pitch, T, Hq, Hkv, d, rope, nullptr, 0, q_bf16, k_bf16, v_bf16, nullptr, nullptr,
+                    nullptr, amax_out, stream);
+}
+
+extern "C" int fp8_rope_qkv_fwd_q(const void *qkv_bf16, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *rope,
+                                  const float *scales, int fmt, void *q_bf16, void *k_bf16, void *v_bf16, uint8_t *q8, uint8_t *k8,
+                                  uint8_t *v8, float *amax_out, void *stream)
+{
+    const int rc = check_codes("fp8_rope_qkv_fwd_q", scales, fmt, q8 || k8 || v8);
+    if (rc != FP8_OK) return rc;
+    return rope_fwd("fp8_rope_qkv_fwd_q", qkv_bf16, pitch, T, Hq, Hkv, d, rope, scales, fmt, q_bf16, k_bf16, v_bf16, q8, k8, v8,
+                    amax_out, stream);
+}
+
+extern "C" int fp8_rope_qkv_bwd(const void *dq_bf16, const void *dk_bf16, const void *dv_bf16, const void *qkv_bf16, size_t pitch,
+                                size_t T, int Hq, int Hkv, int d, const fp8_rope *rope, void *dqkv_bf16, size_t dqkv_pitch,
+                                float *amax_out, void *stream)
+{
+    if (!dqkv_bf16) {
+        set_error("fp8_rope_qkv_bwd: NULL dqkv");
+        return FP8_ERR_NULL;
+    }
+    return rope_bwd("fp8_rope_qkv_bwd", dq_bf16, dk_bf16, dv_bf16, qkv_bf16, pitch, T, Hq, Hkv, d, rope, nullptr, 0, dqkv_bf16,
+                    dqkv_pitch, nullptr, amax_out, stream);
+}
+
+extern "C" int fp8_rope_qkv_bwd_q(const void *dq_bf16, const void *dk_bf16, const void *dv_bf16, const void *qkv_bf16, size_t pitch,
+                                  size_t T, int Hq, int Hkv, int d, const fp8_rope *rope, const float *scale, int fmt,
+                                  void *dqkv_bf16, size_t dqkv_pitch, uint8_t *dqkv8, float *amax_out, void *stream)
+{
+    const int rc = check_codes("fp8_rope_qkv_bwd_q", scale, fmt, dqkv8 != nullptr);
+    if (rc != FP8_OK) return rc;
+    return rope_bwd("fp8_rope_qkv_bwd_q", dq_bf16, dk_bf16, dv_bf16, qkv_bf16, pitch, T, Hq, Hkv, d, rope, scale, fmt, dqkv_bf16,
+                    dqkv_pitch, dqkv8, amax_out, stream);
+}
