@@ -37,17 +37,17 @@ __device__ __forceinline__ uint2 bf16x8_to_fp8x8(const uint32_t (&w)[4], float s
     return make_uint2(cvt_f32x4_to_fp8x4<1>(v0, v1, v2, v3), cvt_f32x4_to_fp8x4<1>(v4, v5, v6, v7));
 }
 
-static __global__ void zero_word_kernel(unsigned int *word) { *word = 0u; }
+static __global__ void zero_word_kernel(unsigned int *word) { word[threadIdx.x] = 0u; }
 
 // A grid that is one cluster sets *amax to zero itself: its first thread at the start, before a cluster barrier that everybody
-// passes in front of the atomicMax.  Both calls by all threads.
-__device__ __forceinline__ bool amax_begin(unsigned int *amax)
+// passes in front of the atomicMax.  Both calls by all threads.  `words`: amax values behind one another.
+__device__ __forceinline__ bool amax_begin(unsigned int *amax, unsigned words = 1)
 {
     uint32_t ctas;
     asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
     const bool alone = amax && ctas == gridDim.x;
     if (alone) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) *amax = 0u;
+        if (blockIdx.x == 0 && threadIdx.x < words) amax[threadIdx.x] = 0u;
         asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     }
     return alone;
@@ -97,7 +97,7 @@ static bool cluster_of_16_fits(int dev, size_t smem)
 constexpr size_t AMAX_EARLY_ELEMENTS = (size_t)1 << 24;
 template <auto Kernel, typename P>
 static int launch_behind_amax(size_t elements, unsigned int *amax, unsigned grid, unsigned threads, size_t smem, cudaStream_t st,
-                              const P &p, int n)
+                              const P &p, int n, unsigned words = 1)
 {
     bool cluster = amax && grid > 1 && grid <= (threads <= 256 ? 16u : 8u);
     if (cluster && grid > 8) {
@@ -121,11 +121,11 @@ static int launch_behind_amax(size_t elements, unsigned int *amax, unsigned grid
         return FP8_OK;
     }
     if (amax && grid > 1 && elements >= AMAX_EARLY_ELEMENTS) {
-        zero_word_kernel<<<1, 1, 0, st>>>(amax);
+        zero_word_kernel<<<1, words, 0, st>>>(amax);
         FP8_CUDA_CHECK(cudaGetLastError());
         return launch_early(Kernel, grid, threads, smem, st, p, n);
     }
-    if (amax && grid > 1) FP8_CUDA_CHECK(cudaMemsetAsync(amax, 0, sizeof(float), st));
+    if (amax && grid > 1) FP8_CUDA_CHECK(cudaMemsetAsync(amax, 0, words * sizeof(float), st));
     Kernel<<<grid, threads, smem, st>>>(p, n);
     FP8_CUDA_CHECK(cudaGetLastError());
     return FP8_OK;

@@ -4,6 +4,7 @@
 
 #include "common.cuh"
 #include "elementwise.cuh"
+#include "rows.cuh"
 
 namespace fp8dpa {
 
@@ -17,30 +18,63 @@ struct RopeTable {
     float magnitude;
 };
 
+// sin and cos of two angles of at most pi / 4 in size: their Taylor series up to the powers 9 and 10, of which the next terms
+// are 1.8e-9 and 1.1e-10 there.
+__device__ __forceinline__ void sincos2(uint64_t x, uint64_t &sn, uint64_t &cs)
+{
+    const auto k = [](float v) { return pack_f32x2(v, v); };
+    const uint64_t q = mul_f32x2(x, x);
+    uint64_t s = fma_f32x2(q, k(1.0f / 362880.0f), k(-1.0f / 5040.0f));
+    s = fma_f32x2(s, q, k(1.0f / 120.0f));
+    s = fma_f32x2(s, q, k(-1.0f / 6.0f));
+    sn = fma_f32x2(mul_f32x2(s, q), x, x);
+    uint64_t c = fma_f32x2(q, k(-1.0f / 3628800.0f), k(1.0f / 40320.0f));
+    c = fma_f32x2(c, q, k(-1.0f / 720.0f));
+    c = fma_f32x2(c, q, k(1.0f / 24.0f));
+    c = fma_f32x2(c, q, k(-0.5f));
+    cs = fma_f32x2(c, q, k(1.0f));
+}
+
 // The angle in turns is a product in 64 bits, good to 2^-52 of itself; what is left of it next to the nearest quarter turn is
-// rounded to FP32, so that cos and sin are good to 2 ulp wherever the position lies, next to their zeros too.
+// rounded to FP32, so that cos and sin are good to 2 ulp wherever the position lies, next to their zeros too.  Adding 1.5 * 2^52
+// leaves the nearest whole number of quarters in the low bits (2^31 turns at most).
+// A thread keeps four frequencies and walks over the positions.
 __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__ RopeTable t)
 {
-    const unsigned quads = t.pairs / 4;
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const size_t pos = i / quads;
-    const unsigned q = (unsigned)(i - pos * quads);
-    if (pos >= t.rows) return;
-    float c[4], s[4];
+    const unsigned quads = t.pairs / 4, wide = 256 / quads, q = threadIdx.x % quads;
+    if (threadIdx.x >= wide * quads) return;
+    double f[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const double turns = (double)pos * t.turns[4 * q + e];
-        const double quarter = rint(4.0 * turns);
-        const float rest = (float)fma(-0.25, quarter, turns);                    // in [-1/8, 1/8]
-        const int k = (int)((long long)quarter & 3);
-        float sn, cs;
-        sincospif(2.0f * rest, &sn, &cs);
-        const float x = k & 1 ? -sn : cs, y = k & 1 ? cs : sn;
-        c[e] = (k & 2 ? -x : x) * t.magnitude;
-        s[e] = (k & 2 ? -y : y) * t.magnitude;
+    for (int e = 0; e < 4; ++e) f[e] = t.turns[4 * q + e];
+    const unsigned step = gridDim.x * wide;
+#pragma unroll 2
+    for (unsigned pos = blockIdx.x * wide + threadIdx.x / quads; pos < t.rows; pos += step) {
+        const double at = (double)pos;
+        float c[4], s[4], x[4];
+        int k[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double turns = at * f[e], shifted = fma(4.0, turns, 6755399441055744.0);
+            k[e] = __double2loint(shifted);
+            x[e] = (float)fma(-0.25, shifted - 6755399441055744.0, turns) * 6.2831853071795865f;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            uint64_t sn, cs;
+            sincos2(pack_f32x2(x[e], x[e + 1]), sn, cs);
+            unpack_f32x2(sn, s[e], s[e + 1]);
+            unpack_f32x2(cs, c[e], c[e + 1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float u = k[e] & 1 ? -s[e] : c[e], v = k[e] & 1 ? c[e] : s[e];
+            c[e] = (k[e] & 2 ? -u : u) * t.magnitude;
+            s[e] = (k[e] & 2 ? -v : v) * t.magnitude;
+        }
+        const size_t i = (size_t)pos * quads + q;
+        __stcs(reinterpret_cast<float4 *>(t.cos_t) + i, make_float4(c[0], c[1], c[2], c[3]));
+        __stcs(reinterpret_cast<float4 *>(t.sin_t) + i, make_float4(s[0], s[1], s[2], s[3]));
     }
-    reinterpret_cast<float4 *>(t.cos_t)[i] = make_float4(c[0], c[1], c[2], c[3]);
-    reinterpret_cast<float4 *>(t.sin_t)[i] = make_float4(s[0], s[1], s[2], s[3]);
 }
 
 // ---------------------------------------------------------------- heads
@@ -61,10 +95,12 @@ struct RopeArgs {
     uint8_t *out8[3];                    // forward: codes of q, k, v; backward: out8[0] = codes of dqkv, contiguous rows
     const float *scales;
     unsigned int *amax_bits;             // forward: three; backward: one
+    unsigned words;                      // how many
     int fmt;
     int lanes_log2;                      // lanes per head: a power of two, at least d / 16
     int chunks[3];                       // pieces of ROPE_HEADS heads of each of q, k, v
-    int tokens;                          // tokens per CTA
+    int per_cta, blocks;                 // pieces of a token on one CTA, and CTAs that share a token
+    int tokens;                          // tokens of a CTA at a time (1 where CTAs share them)
 };
 constexpr int ROPE_HEADS = 4;
 
@@ -94,15 +130,20 @@ __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float s = BACK ? -sn[e] : sn[e];
-            const float ra = a[e] * c[e] - b[e] * s, rb = b[e] * c[e] + a[e] * s;
-            a[e] = ra;
-            b[e] = rb;
+        for (int e = 0; e < 8; e += 2) {                       // two places at a time with the packed instructions
+            const uint64_t x = pack_f32x2(a[e], a[e + 1]), y = pack_f32x2(b[e], b[e + 1]), c2 = pack_f32x2(c[e], c[e + 1]);
+            const uint64_t up = pack_f32x2(sn[e], sn[e + 1]), down = pack_f32x2(-sn[e], -sn[e + 1]);
+            unpack_f32x2(fma_f32x2(x, c2, mul_f32x2(y, BACK ? up : down)), a[e], a[e + 1]);
+            unpack_f32x2(fma_f32x2(y, c2, mul_f32x2(x, BACK ? down : up)), b[e], b[e + 1]);
         }
     }
 }
-
+__device__ __forceinline__ void scale8(float (&a)[8], float r)
+{
+    const uint64_t r2 = pack_f32x2(r, r);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) unpack_f32x2(mul_f32x2(pack_f32x2(a[e], a[e + 1]), r2), a[e], a[e + 1]);
+}
 // 1 - tanh(x)^2 = 4 e / (1 + e)^2 with e = exp(-2 |x|): no cancellation where tanh is near 1.
 __device__ __forceinline__ float sech2(float x)
 {
@@ -111,162 +152,208 @@ __device__ __forceinline__ float sech2(float x)
 }
 
 template <int N>
-__device__ __forceinline__ void block_max_each(const uint32_t (&m2)[N], unsigned int *amax_bits, bool alone)
+__device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int *amax_bits)
 {
     __shared__ uint32_t warp_max[N][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const uint32_t m = __reduce_max_sync(0xffffffffu, max(m2[i] & 0xFFFFu, m2[i] >> 16));
-        if (lane == 0) warp_max[i][warp] = m;
+        const uint32_t most = __reduce_max_sync(0xffffffffu, pack_bf16x2(m[i], 0.0f) & 0xFFFFu);
+        if (lane == 0) warp_max[i][warp] = most;
     }
     __syncthreads();
     const int nwarps = blockDim.x >> 5;
     for (int i = warp; i < N; i += nwarps) {
-        const uint32_t m = __reduce_max_sync(0xffffffffu, lane < nwarps ? warp_max[i][lane] : 0u);
-        if (lane == 0) {
-            if (alone) amax_bits[i] = m << 16;
-            else if (m != 0u) atomicMax(amax_bits + i, m << 16);
-        }
+        const uint32_t most = __reduce_max_sync(0xffffffffu, lane < nwarps ? warp_max[i][lane] : 0u);
+        if (lane == 0 && most != 0u) atomicMax(amax_bits + i, most << 16);
     }
 }
 
 // A head is on 2^lanes_log2 neighbouring lanes, 16 elements each: below `rot` lane j holds elements [8 j, 8 j + 8) and the same
 // of the rotated part's second half, so that both kinds of partners are in one lane; behind it 16 in a row, which pass through.
-// A group of lanes takes up to ROPE_HEADS heads of one token and tensor with the token's angles in registers; a CTA takes whole
-// tokens.  Bytes bind: every element is read once and written once.
-template <int MODE, bool PAIRS, bool BACK>
-__global__ void __launch_bounds__(512) rope_kernel(const __grid_constant__ RopeArgs p)
+// A group of lanes takes up to ROPE_HEADS heads of one tensor of one token with the token's angles in registers.  Persistent: a
+// group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
+// bind: every element is read once and written once.
+template <int MODE, bool BACK>
+constexpr int rope_slots() { return ROPE_HEADS * (BACK && MODE != FP8_QK_NONE ? 4 : 2); }
+template <int MODE, bool PAIRS, bool BACK, int STAGES>
+__global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs p, int slots)
 {
+    extern __shared__ __align__(16) uint4 ring_mem[];
+    constexpr bool SAVED = BACK && MODE != FP8_QK_NONE;
+    constexpr int N = BACK ? 1 : 3;
+    const bool alone = amax_begin(p.amax_bits, N);
     const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log2;
-    const int groups = blockDim.x >> p.lanes_log2;
-    const int slots = p.d / 16, turned = p.rot / 16;
-    const int per_token = p.chunks[0] + p.chunks[1] + p.chunks[2], items = per_token * p.tokens;
-    const bool here = j < slots, turns = j < turned;
-    const int lo = turns ? 8 * j : p.rot + 16 * (j - turned), hi = turns ? p.rot / 2 + 8 * j : lo + 8;
-    const int row = p.heads[0] + p.heads[1] + p.heads[2];
-    uint32_t m[BACK ? 1 : 3];
+    const int turned = p.rot / 16, per_token = p.chunks[0] + p.chunks[1] + p.chunks[2];
+    const unsigned share = blockIdx.x % p.blocks, first = blockIdx.x / p.blocks, ctas = gridDim.x / p.blocks;
+    const int local = group / p.per_cta;
+    int piece = share * p.per_cta + group - local * p.per_cta;
+    const bool mine = j < p.d / 16 && local < p.tokens && piece < per_token, turns = j < turned;
+    piece = min(piece, per_token - 1);
+    const int part = piece < p.chunks[0] ? 0 : piece < p.chunks[0] + p.chunks[1] ? 1 : 2;
+    if (part > 0) piece -= p.chunks[0];
+    if (part > 1) piece -= p.chunks[1];
+    const int h0 = piece * ROPE_HEADS, n_heads = p.heads[part], here = min(ROPE_HEADS, n_heads - h0);
+    const int before = (part > 0 ? p.heads[0] : 0) + (part > 1 ? p.heads[1] : 0) + h0;       // heads of the row in front
+    const int lo = turns ? 8 * j : p.rot + 16 * (j - turned), hi = turns ? p.rot / 2 + 8 * j : lo + 8, d = p.d;
+    const size_t in_row = (size_t)before * d + lo, in_part = (size_t)h0 * d + lo;
+    const int other = hi - lo;
+    const size_t step = (size_t)ctas * p.tokens;
+    const size_t part_pitch = (size_t)n_heads * d, row_pitch = (size_t)(p.heads[0] + p.heads[1] + p.heads[2]) * d;
+    size_t t = (size_t)first * p.tokens + local, ahead = t;
+    // places in shared memory: [stage][slot][thread]; slots 2 hh, 2 hh + 1 are a head's groups, behind them those of what is saved
+    const uint32_t ring = smem_u32(ring_mem + threadIdx.x), per_slot = blockDim.x * 16u, per_stage = per_slot * (unsigned)slots;
+    const uint32_t ring_end = ring + STAGES * per_stage;
+    const auto fetch = [&](uint32_t to) {
+        if (mine && ahead < p.T) {
+            const uint16_t *src = BACK ? p.grad[part] + ahead * part_pitch + in_part : p.qkv + ahead * p.pitch + in_row;
+            const uint16_t *saved = p.qkv + ahead * p.pitch + in_row;
 #pragma unroll
-    for (int i = 0; i < (BACK ? 1 : 3); ++i) m[i] = 0u;
-    for (int first = 0; first < items; first += groups) {     // the same trip count for every lane: shuffles below
-        const int item = first + group, local = min(item, items - 1) / per_token;
-        int piece = min(item, items - 1) - local * per_token;
-        const size_t t = (size_t)blockIdx.x * p.tokens + local;
-        const bool live = here && item < items && t < p.T;
-        const int part = piece < p.chunks[0] ? 0 : piece < p.chunks[0] + p.chunks[1] ? 1 : 2;
-        if (part > 0) piece -= p.chunks[0];
-        if (part > 1) piece -= p.chunks[1];
-        const int h0 = piece * ROPE_HEADS, n_heads = p.heads[part];
-        const int before = (part > 0 ? p.heads[0] : 0) + (part > 1 ? p.heads[1] : 0);       // heads of the row in front
+            for (int hh = 0; hh < ROPE_HEADS; ++hh) {
+                if (hh < here) {
+                    cp_async16(to + (2 * hh) * per_slot, src + hh * d);
+                    cp_async16(to + (2 * hh + 1) * per_slot, src + hh * d + other);
+                    if (SAVED && part < 2) {
+                        cp_async16(to + (2 * ROPE_HEADS + 2 * hh) * per_slot, saved + hh * d);
+                        cp_async16(to + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot, saved + hh * d + other);
+                    }
+                }
+            }
+        }
+        cp_async_commit();
+        ahead += step;
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) fetch(ring + s * per_stage);
+    const float qs = p.scales ? __ldg(p.scales + (BACK ? 0 : part)) : 1.0f;
+    const uint64_t qs2 = both(qs);
+    uint16_t *const out = BACK ? p.out[0] : p.out[part];
+    uint8_t *const out8 = BACK ? p.out8[0] : p.out8[part];
+    const size_t out_pitch = BACK ? p.out_pitch : part_pitch, out8_pitch = BACK ? row_pitch : part_pitch, out_at = BACK ? in_row : in_part;
+    const int i0 = PAIRS ? 4 * j : 8 * j, i1 = PAIRS ? p.rot / 4 + 4 * j : 8 * j + 4;
+    float m = 0.0f;
+    uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage;
+    for (size_t base = (size_t)first * p.tokens; base < p.T; base += step, t += step) {
         size_t pos = 0;
         bool known = true;
+        const bool live = mine && t < p.T;
         if (live) {
             if (p.positions) {
-                const long long at = p.wide_positions ? static_cast<const long long *>(p.positions)[t]
-                                                      : (long long)static_cast<const int *>(p.positions)[t];
+                const long long at = p.wide_positions ? __ldg(static_cast<const long long *>(p.positions) + t)
+                                                      : (long long)__ldg(static_cast<const int *>(p.positions) + t);
                 known = at >= 0 && (unsigned long long)at < p.n_pos;
-                pos = known ? (size_t)at : 0;
+                pos = known ? (size_t)at : 0;                  // row 0 for a token outside the table
             } else if (p.rot) {
-                pos = t % p.n_pos;
+                pos = (unsigned)t % (unsigned)p.n_pos;         // both are below 2^31
             }
         }
         float c[8], sn[8];
-        if (live && turns && known && part < 2) {
+        if (turns && part < 2) {
             const float *pc = p.cos_t + pos * (p.rot / 2), *ps = p.sin_t + pos * (p.rot / 2);
-            const int i0 = PAIRS ? 4 * j : 8 * j, i1 = PAIRS ? p.rot / 4 + 4 * j : 8 * j + 4;
             const float4 c0 = __ldg(reinterpret_cast<const float4 *>(pc + i0)), c1 = __ldg(reinterpret_cast<const float4 *>(pc + i1));
             const float4 s0 = __ldg(reinterpret_cast<const float4 *>(ps + i0)), s1 = __ldg(reinterpret_cast<const float4 *>(ps + i1));
             c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
             sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
         }
-        const float qs = p.scales ? __ldg(p.scales + (BACK ? 0 : part)) : 1.0f;
+        cp_async_wait<STAGES - 2>();
+        fetch(fill);                                           // the stage of the token before this one
+        fill = now;
+        uint16_t *o = out + t * out_pitch + out_at;
+        uint8_t *o8 = out8 + t * out8_pitch + out_at;
 #pragma unroll
-        for (int hh = 0; hh < ROPE_HEADS; ++hh) {
-            const int h = h0 + hh;
-            const bool valid = live && known && h < n_heads, regular = valid && part < 2;
+        for (int hh = 0; hh < ROPE_HEADS; ++hh, o += d, o8 += d) {
+            if (hh > 0 && __all_sync(0xffffffffu, hh >= here)) break;
             float a[8], b[8], x[8], y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a[e] = b[e] = x[e] = y[e] = 0.0f;
-            const size_t in_row = t * p.pitch + (size_t)(before + h) * p.d, in_head = (t * n_heads + h) * p.d;
-            if (valid) {
-                const uint16_t *src = BACK ? p.grad[part] + in_head : p.qkv + in_row;
-                unpack8(__ldg(reinterpret_cast<const uint4 *>(src + lo)), a);
-                unpack8(__ldg(reinterpret_cast<const uint4 *>(src + hi)), b);
-            }
-            if (BACK && MODE != FP8_QK_NONE && regular) {
-                unpack8(__ldg(reinterpret_cast<const uint4 *>(p.qkv + in_row + lo)), x);
-                unpack8(__ldg(reinterpret_cast<const uint4 *>(p.qkv + in_row + hi)), y);
+            unpack8(ring_get(now + (2 * hh) * per_slot), a);
+            unpack8(ring_get(now + (2 * hh + 1) * per_slot), b);
+            if (SAVED && part < 2) {
+                unpack8(ring_get(now + (2 * ROPE_HEADS + 2 * hh) * per_slot), x);
+                unpack8(ring_get(now + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot), y);
             }
             float r = 1.0f;
             if (MODE == FP8_QK_RMS) {
                 float ss = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ss = BACK ? fmaf(x[e], x[e], fmaf(y[e], y[e], ss)) : fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+                if (!mine) ss = 0.0f;
                 for (int off = lanes >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
                 r = rsqrtf(fmaf(ss, p.inv_d, p.eps));
             }
-            if (!BACK && regular) {
+            if (!BACK && part < 2) {
                 if (MODE == FP8_QK_RMS) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { a[e] *= r; b[e] *= r; }
+                    scale8(a, r);
+                    scale8(b, r);
                 } else if (MODE == FP8_QK_TANH) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) { a[e] = tanhf(p.alpha * a[e]); b[e] = tanhf(p.alpha * b[e]); }
                 }
             }
-            if (regular && turns) rotate<PAIRS, BACK>(a, b, c, sn);
+            if (turns && part < 2) rotate<PAIRS, BACK>(a, b, c, sn);
             if (BACK && MODE == FP8_QK_RMS) {
                 float s = 0.0f;
+                scale8(x, r);
+                scale8(y, r);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { x[e] *= r; y[e] *= r; s = fmaf(a[e], x[e], fmaf(b[e], y[e], s)); }
-                if (!regular) s = 0.0f;                        // r is without meaning there
+                for (int e = 0; e < 8; ++e) s = fmaf(a[e], x[e], fmaf(b[e], y[e], s));
+                if (!mine) s = 0.0f;
                 for (int off = lanes >> 1; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-                s *= p.inv_d;
-                if (regular) {
+                if (part < 2) {
+                    s *= -p.inv_d;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { a[e] = r * fmaf(-s, x[e], a[e]); b[e] = r * fmaf(-s, y[e], b[e]); }
+                    for (int e = 0; e < 8; ++e) { a[e] = fmaf(s, x[e], a[e]); b[e] = fmaf(s, y[e], b[e]); }
+                    scale8(a, r);
+                    scale8(b, r);
                 }
             }
-            if (BACK && MODE == FP8_QK_TANH && regular) {
+            if (BACK && MODE == FP8_QK_TANH && part < 2) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) { a[e] *= p.alpha * sech2(p.alpha * x[e]); b[e] *= p.alpha * sech2(p.alpha * y[e]); }
             }
-            const uint4 oa = pack8(a), ob = pack8(b);
-            const uint32_t wa[4] = {oa.x, oa.y, oa.z, oa.w}, wb[4] = {ob.x, ob.y, ob.z, ob.w};
-            if (valid) {
-                uint32_t most = 0u;
+            if (!live || hh >= here) continue;
+            if (!known) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) most = absmax2e(absmax2e(most, wa[q]), wb[q]);
-                if (BACK) {
-                    m[0] = __vmaxu2(m[0], most);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) m[i % (BACK ? 1 : 3)] = __vmaxu2(m[i % (BACK ? 1 : 3)], part == i ? most : 0u);
-                }
+                for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.0f;
             }
-            if (live && h < n_heads) {                         // a token outside the table: zeros
-                uint16_t *o = BACK ? p.out[0] : p.out[part];
-                uint8_t *o8 = BACK ? p.out8[0] : p.out8[part];
-                if (o) {
-                    o += BACK ? t * p.out_pitch + (size_t)(before + h) * p.d : in_head;
-                    *reinterpret_cast<uint4 *>(o + lo) = oa;
-                    *reinterpret_cast<uint4 *>(o + hi) = ob;
-                }
-                if (o8) {
-                    o8 += BACK ? (t * row + before + h) * p.d : in_head;
-                    *reinterpret_cast<uint2 *>(o8 + lo) = bf16x8_to_fp8x8(wa, qs, p.fmt);
-                    *reinterpret_cast<uint2 *>(o8 + hi) = bf16x8_to_fp8x8(wb, qs, p.fmt);
-                }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = absmax3(m, a[e], b[e]);
+            const uint4 oa = pack8(a), ob = pack8(b);
+            if (out) {
+                *reinterpret_cast<uint4 *>(o) = oa;
+                *reinterpret_cast<uint4 *>(o + other) = ob;
+            }
+            if (out8) {
+                *reinterpret_cast<uint2 *>(o8) = codes8(oa, qs2, p.fmt);
+                *reinterpret_cast<uint2 *>(o8 + other) = codes8(ob, qs2, p.fmt);
             }
         }
+        now += per_stage;
+        if (now == ring_end) now = ring;
     }
-    if (p.amax_bits) block_max_each(m, p.amax_bits, gridDim.x == 1);
+    cudaGridDependencySynchronize();
+    if (alone) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    if (p.amax_bits) {
+        float each[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) each[i] = BACK || part == i ? m : 0.0f;
+        block_max_each(each, p.amax_bits);
+    }
+}
+
+template <auto Kernel>
+static int rope_run(const RopeArgs &p, int slots, unsigned grid, unsigned threads, size_t per_thread, size_t elements, cudaStream_t st)
+{
+    if (256 * per_thread > 40 * 1024) {
+        const int rc = allow_shared<Kernel>((int)(256 * per_thread));
+        if (rc != FP8_OK) return rc;
+    }
+    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, threads * per_thread, st, p, slots, p.words);
 }
 
 template <bool BACK>
 static int rope_launch(RopeArgs &p, int mode, bool pairs, cudaStream_t st)
 {
     const int slots = p.d / 16;
+    p.words = BACK ? 1 : 3;
     p.lanes_log2 = 0;
     while ((1 << p.lanes_log2) < slots) ++p.lanes_log2;
     int per_token = 0;
@@ -276,24 +363,29 @@ static int rope_launch(RopeArgs &p, int mode, bool pairs, cudaStream_t st)
         p.chunks[i] = wanted ? (p.heads[i] + ROPE_HEADS - 1) / ROPE_HEADS : 0;
         per_token += p.chunks[i];
     }
-    const int threads_per_token = per_token << p.lanes_log2;
-    p.tokens = threads_per_token >= 256 ? 1 : 256 / threads_per_token;
+    // CTAs of up to 256 threads take whole tokens, or several share one token's heads
+    const int groups = 256 >> p.lanes_log2;
+    p.blocks = (per_token + groups - 1) / groups;
+    p.per_cta = (per_token + p.blocks - 1) / p.blocks;
+    p.tokens = p.blocks > 1 ? 1 : groups / p.per_cta;
     if ((size_t)p.tokens > p.T) p.tokens = (int)p.T;
-    int threads = (threads_per_token * p.tokens + 31) & ~31;
-    if (threads > 512) threads = 512;
-    const size_t grid = (p.T + p.tokens - 1) / p.tokens;
-    if (p.amax_bits && grid > 1) FP8_CUDA_CHECK(cudaMemsetAsync(p.amax_bits, 0, (BACK ? 1 : 3) * sizeof(float), st));
+    const unsigned threads = (unsigned)((p.tokens * p.per_cta << p.lanes_log2) + 31) & ~31u;
+    const size_t want = (p.T + p.tokens - 1) / p.tokens, most = 148 * (size_t)((BACK ? 512 : 768) / threads);
+    size_t ctas = want * p.blocks <= most ? want : most / p.blocks;
+    if (ctas == 0) ctas = 1;
+    const unsigned grid = (unsigned)(ctas * p.blocks);
+    const size_t elements = p.T * (size_t)(p.heads[0] + p.heads[1] + p.heads[2]) * p.d;
 #define FP8DPA_LAUNCH_ROPE(MODE) \
     do { \
-        if (pairs) rope_kernel<MODE, true, BACK><<<(unsigned)grid, threads, 0, st>>>(p); \
-        else rope_kernel<MODE, false, BACK><<<(unsigned)grid, threads, 0, st>>>(p); \
+        constexpr int STAGES = 2, SLOTS = rope_slots<MODE, BACK>(); \
+        constexpr size_t per_thread = (size_t)STAGES * SLOTS * 16; \
+        if (pairs) return rope_run<rope_kernel<MODE, true, BACK, STAGES>>(p, SLOTS, grid, threads, per_thread, elements, st); \
+        return rope_run<rope_kernel<MODE, false, BACK, STAGES>>(p, SLOTS, grid, threads, per_thread, elements, st); \
     } while (0)
     if (mode == FP8_QK_RMS) FP8DPA_LAUNCH_ROPE(FP8_QK_RMS);
     else if (mode == FP8_QK_TANH) FP8DPA_LAUNCH_ROPE(FP8_QK_TANH);
     else FP8DPA_LAUNCH_ROPE(FP8_QK_NONE);
 #undef FP8DPA_LAUNCH_ROPE
-    FP8_CUDA_CHECK(cudaGetLastError());
-    return FP8_OK;
 }
 
 // What both directions check of an fp8_rope; 0 or a status.
@@ -481,8 +573,8 @@ extern "C" int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, d
     t.rows = n_pos;
     t.pairs = rot / 2;
     t.magnitude = (float)magnitude;
-    const size_t threads = n_pos * (size_t)(rot / 8);
-    rope_table_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, static_cast<cudaStream_t>(stream)>>>(t);
+    const size_t wide = 256 / (rot / 8), want = (n_pos + wide - 1) / wide;       // positions of a CTA at a time
+    rope_table_kernel<<<(unsigned)(want < 148 * 8 ? want : 148 * 8), 256, 0, static_cast<cudaStream_t>(stream)>>>(t);
     FP8_CUDA_CHECK(cudaGetLastError());
     return FP8_OK;
 }

@@ -72,6 +72,32 @@ __device__ __forceinline__ uint32_t round2(uint64_t v)
     return pack_bf16x2(lo, hi);
 }
 
+// max(m, |a|, |b|); NaN stays.  Rounding to BF16 keeps the order, so that an amax can be taken of the values before it and be
+// rounded once: half the instructions of the maximum of the packed results.
+__device__ __forceinline__ float absmax3(float m, float a, float b)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float absmax3(float m, uint64_t v)
+{
+    float lo, hi;
+    unpack_f32x2(v, lo, hi);
+    return absmax3(m, lo, hi);
+}
+// Eight BF16 values to eight FP8 codes under the scale in both halves of `scale2`: fp8_cast's (binary32 product, one rounding).
+__device__ __forceinline__ uint2 codes8(const uint4 w, uint64_t scale2, int fmt)
+{
+    uint64_t f[4];
+    float v[8];
+    unpack4x2(w, f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) unpack_f32x2(mul_f32x2(f[e], scale2), v[2 * e], v[2 * e + 1]);
+    if (fmt == 0) return make_uint2(cvt_f32x4_to_fp8x4<0>(v[0], v[1], v[2], v[3]), cvt_f32x4_to_fp8x4<0>(v[4], v[5], v[6], v[7]));
+    return make_uint2(cvt_f32x4_to_fp8x4<1>(v[0], v[1], v[2], v[3]), cvt_f32x4_to_fp8x4<1>(v[4], v[5], v[6], v[7]));
+}
+
 // Sum over the threads that share a row: 2^lanes_log2 neighbouring lanes, or the whole CTA of up to WARPS warps through `red` (a
 // buffer that this call alone uses until the next barrier; entries behind the CTA's warps are zero).
 template <bool CTA, int WARPS>
