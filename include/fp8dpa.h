@@ -405,8 +405,7 @@ FP8_API int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, doub
 /* Forward: qkv BF16, rows `pitch` elements apart (a multiple of 8, at least (Hq + 2 Hkv) d); q [T,Hq,d], k, v [T,Hkv,d] BF16, each
  * nullable: what is not asked for is not computed.  amax_out (nullable): three floats, overwritten with amax of q, k, v.
  * _q: the producer form under delayed scaling: codes q8, k8, v8 (each nullable) of the BF16-rounded values under scales[0..2], bit-
- * identical to fp8_cast of them.  Hkv = 0: rows of Q alone.  With FP8_QK_RMS / NONE, the whole head and halves as partners the results
- * are those of fp8_qk_norm_rope bit for bit.  d % 16 == 0, d <= 256, 1 <= T < 2^31.  Outputs must not overlap inputs. */
+ * identical to fp8_cast of them.  Hkv = 0: rows of Q alone.  d % 16 == 0, d <= 256, 1 <= T < 2^31.  Outputs must not overlap inputs. */
 FP8_API int fp8_rope_qkv_fwd(const void *qkv_bf16, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *rope, void *q_bf16,
                      void *k_bf16, void *v_bf16, float *amax_out, void *stream);
 FP8_API int fp8_rope_qkv_fwd_q(const void *qkv_bf16, size_t pitch, size_t T, int Hq, int Hkv, int d, const fp8_rope *rope,

@@ -4,6 +4,7 @@
 
 #include "common.cuh"
 #include "elementwise.cuh"
+#include "rows.cuh"
 
 namespace fp8dpa {
 
@@ -144,7 +145,8 @@ __device__ __forceinline__ void store8(uint8_t *p, int left, uint2 v)
     }
 }
 
-__device__ __forceinline__ void decode8(uint2 codes, float scale, float (&f)[8])
+// Four of these per eight values: the packed instructions work on two at a time.
+__device__ __forceinline__ void decode8(uint2 codes, float scale, uint64_t (&f)[4])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -153,131 +155,246 @@ __device__ __forceinline__ void decode8(uint2 codes, float scale, float (&f)[8])
         asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(two));
         float lo, hi;
         asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(h));
-        f[2 * i] = lo * scale;
-        f[2 * i + 1] = hi * scale;
+        f[i] = mul_f32x2(pack_f32x2(lo, hi), both(scale));
     }
 }
-
-// The codes of a block's values under the smallest power of two that leaves none above 448.  A value is rounded up in size with
-// the probability of the part that is cut off (16 bits of it), so that a change far below a step is not lost over many steps but
-// comes through on average.  FLOOR: values above zero get the smallest code at least (a root of zero in the update's denominator
-// would let it through unchecked).  A value that is not finite gets the code of NaN.
-template <bool FLOOR>
-__device__ __forceinline__ uint2 encode8(const float (&f)[8], const uint32_t (&bits)[8], uint32_t &exponent)
+__device__ __forceinline__ uint64_t add_ftz2(uint64_t a, uint64_t b)
 {
-    float most = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[e]));
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));   // the block's 16 lanes
-    const int up = (int)((__float_as_uint(most) + 0x1FFFFFu) >> 23) - 8;
-    exponent = (uint32_t)max(up, 1);
-    const float inv = __uint_as_float((254u - exponent) << 23);
-    float z[8];
+    uint64_t r;
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Square roots of two values that are 0 or normal numbers: the hardware's reciprocal root and one step of Newton's iteration on
+// r^2 = v, r - (r^2 - v) / (2 r), with the difference exact: the correctly rounded root but where that lies within 2^-44 of the
+// middle of two values.
+__device__ __forceinline__ uint64_t root2(uint64_t v)
+{
+    float a, b, qa, qb;
+    unpack_f32x2(v, a, b);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(qa) : "f"(fmaxf(a, 1.17549435e-38f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(qb) : "f"(fmaxf(b, 1.17549435e-38f)));
+    const uint64_t q = pack_f32x2(qa, qb), r = mul_f32x2(v, q);
+    return fma_f32x2(fma_f32x2(r, r, mul_f32x2(v, both(-1.0f))), mul_f32x2(q, both(-0.5f)), r);
+}
+__device__ __forceinline__ float reciprocal(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t half_bits(uint64_t v, int i)
+{
+    float lo, hi;
+    unpack_f32x2(v, lo, hi);
+    return __float_as_uint(i ? hi : lo);
+}
+
+// The biased exponent of the smallest power of two that leaves none of a block's values above 448, from its largest one: 448 is
+// 1.75 * 2^8, and a mantissa above 1.75 carries into the exponent.
+__device__ __forceinline__ uint32_t exponent_of(float most) { return (__float_as_uint(most) + 0x1FFFFFu) >> 23; }
+
+// A block's values as codes.  E4M3 with a fixed bias is FP32 with fewer bits: the value over its power of two and over 2^120 has
+// its code in bits 20 to 26, down to the smallest, FP32's own denormal numbers being its too.  Rounding with random bits is then
+// an addition below bit 20: away from zero with the probability of the part that is cut off (16 bits of it), so that a change far
+// below a step is not lost over many steps but comes through on average.  ROOT: not negative, and values above zero get the
+// smallest code at least (a root of zero in the update's denominator would let it through unchecked).
+template <bool ROOT>
+__device__ __forceinline__ uint2 encode8(const uint64_t (&f)[4], const uint32_t (&bits)[8], uint32_t exponent)
+{
+    const uint64_t inv = both(__uint_as_float((254u - exponent) << 23)), down = both(7.5231638e-37f);       // 2^-120
+    uint32_t z[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float y = fabsf(f[e]) * inv, off = y < 0.015625f ? 0.015625f : 0.0f;     // below the normal numbers the step stays 2^-9
-        const uint32_t rnd = FLOOR ? (bits[e] >> 16) << 4 : (bits[e] & 0xFFFFu) << 4;
-        float q = __uint_as_float((__float_as_uint(y + off) + rnd) & 0xFFF00000u) - off;
-        if (FLOOR && q == 0.0f && f[e] > 0.0f) q = 0.001953125f;
-        q = y <= 448.0f ? q : __uint_as_float(0x7FC00000u);
-        z[e] = FLOOR ? q : copysignf(q, f[e]);
+        const uint64_t y = mul_f32x2(mul_f32x2(f[e >> 1], inv), down);
+        const uint32_t cut = ROOT ? bits[e] >> 16 : bits[e] & 0xFFFFu;
+        z[e] = half_bits(y, e & 1) + (cut << 4);
+        if (ROOT) z[e] = max(z[e], min(half_bits(f[e >> 1], e & 1), 0x100000u)) << 4;
+        else z[e] = ((z[e] << 4) & 0x7FFFFFFFu) | (z[e] & 0x80000000u);
     }
-    return make_uint2(cvt_f32x4_to_fp8x4<0>(z[0], z[1], z[2], z[3]), cvt_f32x4_to_fp8x4<0>(z[4], z[5], z[6], z[7]));
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(z[4 * i], z[4 * i + 1], 0x0073), __byte_perm(z[4 * i + 2], z[4 * i + 3], 0x0073), 0x5410);
+    return make_uint2(w[0], w[1]);
+}
+// The same for a block with values that are not finite: they get the code of NaN, the others are scaled by the largest of theirs.
+// By all lanes of a warp together.
+template <bool ROOT>
+__device__ __noinline__ uint2 encode8_broken(uint64_t f0, uint64_t f1, uint64_t f2, uint64_t f3, uint32_t key, uint32_t &exponent)
+{
+    uint64_t f[4] = {f0, f1, f2, f3};
+    uint32_t bits[8], broken = 0u;
+    float most = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        bits[e] = mix32(key + e);
+        const float v = fabsf(__uint_as_float(half_bits(f[e >> 1], e & 1)));
+        if (v < INFINITY) most = fmaxf(most, v);
+        else broken |= 1u << e;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float lo, hi;
+        unpack_f32x2(f[e], lo, hi);
+        f[e] = pack_f32x2(broken >> (2 * e) & 1u ? 0.0f : lo, broken >> (2 * e + 1) & 1u ? 0.0f : hi);
+    }
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+    exponent = (uint32_t)max((int)exponent_of(most) - 8, 1);
+    uint2 c = encode8<ROOT>(f, bits, exponent);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (broken >> e & 1u) (e < 4 ? c.x : c.y) |= 0x7Fu << (8 * (e & 3));
+    return c;
 }
 
 struct AdamRates {
     float beta1, rest1, beta2, rest2, eps;                // rest = 1 - beta
 };
 
+// What a thread reads of eight elements.
 template <typename G, bool EIGHT>
-__device__ __forceinline__ uint32_t adamw_chunk(const AdamTable &t, int k, unsigned long long i, int left, const AdamStep &s,
-                                               const AdamRates &a)
-{
-    const float keep = 1.0f - s.lr * t.decay[k], qs = t.p8[k] ? __ldg(t.q_scale[k]) : 1.0f;
-    float *const p = t.p[k];
-    const G *const g = static_cast<const G *>(t.g[k]);
-    uint32_t m2 = 0u;
-    i += threadIdx.x * 8;
-    left -= threadIdx.x * 8;
-#pragma unroll
-    for (int u = 0; u < AW_PER_THREAD / 8; ++u, i += AW_THREADS * 8, left -= AW_THREADS * 8) {
-        float w[8], d[8], m[8], v[8], r[8];
-        const int some = max(left, 0);
-        load8(p + i, some, w);
-        load8(g + i, some, d);
-        if (EIGHT) {
-            const uint2 mc = load8(static_cast<const uint8_t *>(t.m[k]) + i, some), vc = load8(static_cast<const uint8_t *>(t.v[k]) + i, some);
-            uint32_t me = 0u, ve = 0u;
-            if (some) {
-                me = t.m_exp[k][i / AW_BLOCK];
-                ve = t.v_exp[k][i / AW_BLOCK];
-            }
-            decode8(mc, __uint_as_float(me << 23), m);
-            decode8(vc, __uint_as_float(ve << 23), v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= v[e];
+struct AdamIn {
+    float w[8], g[8], m[EIGHT ? 1 : 8], v[EIGHT ? 1 : 8];
+    uint2 mc, vc;
+    uint32_t me, ve;
+    __device__ __forceinline__ void load(const AdamTable &t, int k, unsigned long long i, int some)
+    {
+        load8(t.p[k] + i, some, w);
+        load8(static_cast<const G *>(t.g[k]) + i, some, g);
+        if constexpr (EIGHT) {
+            mc = load8(static_cast<const uint8_t *>(t.m[k]) + i, some);
+            vc = load8(static_cast<const uint8_t *>(t.v[k]) + i, some);
+            me = some ? t.m_exp[k][i / AW_BLOCK] : 0u;
+            ve = some ? t.v_exp[k][i / AW_BLOCK] : 0u;
         } else {
             load8(static_cast<const float *>(t.m[k]) + i, some, m);
             load8(static_cast<const float *>(t.v[k]) + i, some, v);
         }
+    }
+};
+
+// The element's new weight and moments, two elements at a time.  The moments take one rounding per operation, in this order: the
+// codes that random bits give are the same wherever they are worked out.
+template <typename G, bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned long long i, int left, const AdamStep *step,
+                                            const AdamRates &a)
+{
+    i += threadIdx.x * 8;
+    left -= threadIdx.x * 8;
+    constexpr int U = AW_PER_THREAD / 8, STEP = AW_THREADS * 8;
+    AdamIn<G, EIGHT> in[EIGHT ? U : 1];
+    const float scale = t.p8[k] ? __ldg(t.q_scale[k]) : 1.0f;
+    // on their way before the step's numbers are there
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = __fmul_rn(d[e], s.factor);
-            // one rounding per operation, in this order: the codes that random bits give are the same wherever they are worked out
-            m[e] = __fadd_rn(__fmul_rn(a.beta1, m[e]), __fmul_rn(a.rest1, x));
-            v[e] = __fadd_rn(__fmul_rn(a.beta2, v[e]), __fmul_rn(__fmul_rn(a.rest2, x), x));
-            if (EIGHT) r[e] = __fsqrt_rn(v[e]);
-            else asm("sqrt.approx.f32 %0, %1;" : "=f"(r[e]) : "f"(v[e]));
-            w[e] = fmaf(-s.rate, __fdividef(m[e], fmaf(r[e], s.inv_root, a.eps)), w[e] * keep);
+    for (int u = 0; u < (EIGHT ? U : 1); ++u) in[u].load(t, k, i + u * STEP, WHOLE ? 8 : max(left - u * STEP, 0));
+    cudaGridDependencySynchronize();
+    const AdamStep s = *step;
+    if (s.skip) return;
+    const uint64_t keep = both(1.0f - s.lr * t.decay[k]), qs = both(scale);
+    float most = 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u, i += STEP, left -= STEP) {
+        const int some = WHOLE ? 8 : max(left, 0);
+        AdamIn<G, EIGHT> &x = in[EIGHT ? u : 0];
+        if (!EIGHT && u > 0) x.load(t, k, i, some);
+        uint64_t m[4], v[4], r[4], w[4];
+        if constexpr (EIGHT) {
+            decode8(x.mc, __uint_as_float(x.me << 23), m);
+            decode8(x.vc, __uint_as_float(x.ve << 23), v);
         }
-        store8(p + i, some, w);
-        if (EIGHT) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (EIGHT) {
+                v[e] = mul_f32x2(v[e], v[e]);
+            } else {
+                m[e] = pack_f32x2(x.m[2 * e], x.m[2 * e + 1]);
+                v[e] = pack_f32x2(x.v[2 * e], x.v[2 * e + 1]);
+            }
+            const uint64_t g = mul_f32x2(pack_f32x2(x.g[2 * e], x.g[2 * e + 1]), both(s.factor));
+            m[e] = add_f32x2(mul_f32x2(both(a.beta1), m[e]), mul_f32x2(both(a.rest1), g));
+            const uint64_t old = mul_f32x2(both(a.beta2), v[e]), more = mul_f32x2(mul_f32x2(both(a.rest2), g), g);
+            if constexpr (EIGHT) {
+                v[e] = add_ftz2(old, more);                  // below the normal numbers: 0
+                r[e] = root2(v[e]);
+            } else {
+                v[e] = add_f32x2(old, more);
+                float lo, hi;
+                unpack_f32x2(v[e], lo, hi);
+                asm("sqrt.approx.f32 %0, %1;" : "=f"(lo) : "f"(lo));
+                asm("sqrt.approx.f32 %0, %1;" : "=f"(hi) : "f"(hi));
+                r[e] = pack_f32x2(lo, hi);
+            }
+            float lo, hi;
+            unpack_f32x2(fma_f32x2(r[e], both(s.inv_root), both(a.eps)), lo, hi);
+            w[e] = fma_f32x2(mul_f32x2(m[e], pack_f32x2(reciprocal(lo), reciprocal(hi))), both(-s.rate),
+                             mul_f32x2(pack_f32x2(x.w[2 * e], x.w[2 * e + 1]), keep));
+            most = absmax3(most, w[e]);
+            unpack_f32x2(w[e], x.w[2 * e], x.w[2 * e + 1]);
+        }
+        store8(t.p[k] + i, some, x.w);
+        if constexpr (EIGHT) {
             const unsigned long long at = t.done[k] + i;
             const uint32_t key = mix32(mix32(s.key + (uint32_t)(t.number + k)) + (uint32_t)(at >> 32)) + (uint32_t)at;
-            uint32_t bits[8], me, ve;
+            float top_m = 0.0f, top_r = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) bits[e] = mix32(key + e);
-            const uint2 mc = encode8<false>(m, bits, me), vc = encode8<true>(r, bits, ve);
+            for (int e = 0; e < 4; ++e) {
+                top_m = absmax3(top_m, m[e]);
+                top_r = absmax3(top_r, r[e]);
+            }
+            uint32_t up = exponent_of(top_m) << 16 | exponent_of(top_r);
+#pragma unroll
+            for (int off = 8; off > 0; off >>= 1) up = __vmaxu2(up, __shfl_xor_sync(0xffffffffu, up, off));   // the block's 16 lanes
+            uint32_t me = (uint32_t)max((int)(up >> 16) - 8, 1), ve = (uint32_t)max((int)(up & 0xFFFFu) - 8, 1);
+            uint2 mc, vc;
+            if (__any_sync(0xffffffffu, max(up >> 16, up & 0xFFFFu) >= 255u)) {
+                mc = encode8_broken<false>(m[0], m[1], m[2], m[3], key, me);
+                vc = encode8_broken<true>(r[0], r[1], r[2], r[3], key, ve);
+            } else {
+                uint32_t bits[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) bits[e] = mix32(key + e);
+                mc = encode8<false>(m, bits, me);
+                vc = encode8<true>(r, bits, ve);
+            }
             store8(static_cast<uint8_t *>(t.m[k]) + i, some, mc);
             store8(static_cast<uint8_t *>(t.v[k]) + i, some, vc);
-            if (some && (threadIdx.x & 15) == 0) {
+            if ((threadIdx.x & 15) == 0 && some) {
                 t.m_exp[k][i / AW_BLOCK] = (uint8_t)me;
                 t.v_exp[k][i / AW_BLOCK] = (uint8_t)ve;
             }
         } else {
-            store8(static_cast<float *>(t.m[k]) + i, some, m);
-            store8(static_cast<float *>(t.v[k]) + i, some, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                unpack_f32x2(m[e], x.m[2 * e], x.m[2 * e + 1]);
+                unpack_f32x2(v[e], x.v[2 * e], x.v[2 * e + 1]);
+            }
+            store8(static_cast<float *>(t.m[k]) + i, some, x.m);
+            store8(static_cast<float *>(t.v[k]) + i, some, x.v);
         }
-        uint32_t o[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = pack_bf16x2(w[2 * q], w[2 * q + 1]);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            m2 = absmax2e(m2, o[q] & (2 * q + 1 < some ? 0xFFFFFFFFu : 2 * q < some ? 0xFFFFu : 0u));
+        const uint32_t o[4] = {round2(w[0]), round2(w[1]), round2(w[2]), round2(w[3])};
         if (t.p16[k]) store8(t.p16[k] + i, some, o);
-        if (t.p8[k]) store8(t.p8[k] + i, some, bf16x8_to_fp8x8(o, qs, t.types[k] >> 2));
+        if (t.p8[k]) store8(t.p8[k] + i, some, codes8(make_uint4(o[0], o[1], o[2], o[3]), qs, t.types[k] >> 2));
     }
-    return m2;
+    if (t.amax[k]) block_max_bf16_to(pack_bf16x2(most, 0.0f), t.amax[k]);
 }
 
-__global__ void __launch_bounds__(AW_THREADS) adamw_kernel(const __grid_constant__ AdamTable t, const AdamStep *step, const AdamRates a)
+__global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ AdamTable t, const AdamStep *step, const AdamRates a)
 {
     const unsigned c = blockIdx.x;
     const int k = item_of_chunk(t, c);
     const unsigned long long i = (unsigned long long)(c - t.first[k]) * AW_CHUNK, rest = t.n[k] - i;
     const int left = rest < AW_CHUNK ? (int)rest : AW_CHUNK;
-    cudaGridDependencySynchronize();
-    const AdamStep s = *step;
-    if (s.skip) return;
-    uint32_t m2;
+    const bool whole = left == AW_CHUNK;
+#define FP8DPA_ADAMW_CHUNK(G, EIGHT) \
+    whole ? adamw_chunk<G, EIGHT, true>(t, k, i, left, step, a) : adamw_chunk<G, EIGHT, false>(t, k, i, left, step, a)
     switch (t.types[k] & 3) {
-    case 0: m2 = adamw_chunk<uint16_t, false>(t, k, i, left, s, a); break;
-    case 1: m2 = adamw_chunk<float, false>(t, k, i, left, s, a); break;
-    case 2: m2 = adamw_chunk<uint16_t, true>(t, k, i, left, s, a); break;
-    default: m2 = adamw_chunk<float, true>(t, k, i, left, s, a); break;
+    case 0: return FP8DPA_ADAMW_CHUNK(uint16_t, false);
+    case 1: return FP8DPA_ADAMW_CHUNK(float, false);
+    case 2: return FP8DPA_ADAMW_CHUNK(uint16_t, true);
+    default: return FP8DPA_ADAMW_CHUNK(float, true);
     }
-    if (t.amax[k]) block_max_bf16_to(m2, t.amax[k]);
+#undef FP8DPA_ADAMW_CHUNK
 }
 
 static int adamw_check_items(const fp8_adamw_item *items, int n_items)

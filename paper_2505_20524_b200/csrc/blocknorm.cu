@@ -10,12 +10,25 @@ namespace fp8dpa {
 
 constexpr uint64_t TWO_ONES = 0x3F8000003F800000ull;
 
-// sigmoid(v) of two values by the hardware's exp2 and reciprocal (good to 2^-22 of itself, then rounded to BF16 with the rest)
-__device__ __forceinline__ uint64_t sigmoid2(uint64_t v)
+// sigmoid(v) of two values, s = 1 / (1 + e) with e = exp(-v), and 1 - s = e s (no cancellation where s is near 1); e stops at
+// 2^126, where the sigmoid is 2^-126.
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t v, uint64_t &rest)
 {
     float a, b;
     unpack_f32x2(mul_f32x2(v, both(-1.4426950408889634f)), a, b);
-    return pack_f32x2(__fdividef(1.0f, 1.0f + ex2_approx(a)), __fdividef(1.0f, 1.0f + ex2_approx(b)));
+    const uint64_t e = pack_f32x2(ex2_approx(fminf(a, 126.0f)), ex2_approx(fminf(b, 126.0f)));
+    unpack_f32x2(add_f32x2(e, both(1.0f)), a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    const uint64_t s = pack_f32x2(a, b);
+    rest = mul_f32x2(e, s);
+    return s;
+}
+// by the hardware's exp2 and reciprocal (good to 2^-22 of itself, then rounded to BF16 with the rest)
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t v)
+{
+    uint64_t unused;
+    return sigmoid2(v, unused);
 }
 
 // ---------------------------------------------------------------- forward
@@ -56,7 +69,7 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd 
             red[0][0][threadIdx.x] = red[0][1][threadIdx.x] = red[1][0][threadIdx.x] = red[1][1][threadIdx.x] = 0.0f;
         __syncthreads();
     }
-    const float qs = p.out8 ? __ldg(p.q_scale) : 1.0f;
+    const uint64_t qs = both(p.out8 ? __ldg(p.q_scale) : 1.0f);
     const float inv_d = 1.0f / (float)(p.n8 * 8);
     const uint64_t a2 = both(p.a), b2 = both(p.b);
     // places in shared memory of this thread's groups: [stage][tensor][k][thread]
@@ -95,7 +108,8 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd 
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) fetch(ring + s * per_stage);
-    uint32_t m = 0, now = ring, fill = ring + (STAGES - 1) * per_stage;
+    float m = 0.0f;
+    uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage;
     int flip = 0;
     for (size_t base = unit * rows; base < p.T; base += step, t += step, at += pitch, flip ^= 1) {
         cp_async_wait<STAGES - 2>();
@@ -155,22 +169,23 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd 
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
             if (!live || !in[k]) continue;
-            uint32_t o[4] = {hw[k].x, hw[k].y, hw[k].z, hw[k].w};
+            uint64_t f[4];
+            uint4 o = hw[k];
+            unpack4x2(o, f);
             if (PRE) {
-                uint64_t f[4];
-                unpack4x2(hw[k], f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = round2(mul_f32x2(mul_f32x2(f[e], r2), gp[k][e]));
-                if (p.out) reinterpret_cast<uint4 *>(p.out)[at + k * span] = make_uint4(o[0], o[1], o[2], o[3]);
+                for (int e = 0; e < 4; ++e) f[e] = mul_f32x2(mul_f32x2(f[e], r2), gp[k][e]);
+                o = make_uint4(round2(f[0]), round2(f[1]), round2(f[2]), round2(f[3]));
+                if (p.out) reinterpret_cast<uint4 *>(p.out)[at + k * span] = o;
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) m = absmax2e(m, o[e]);
-            if (p.out8) reinterpret_cast<uint2 *>(p.out8)[at + k * span] = bf16x8_to_fp8x8(o, qs, p.fmt);
+            for (int e = 0; e < 4; ++e) m = absmax3(m, f[e]);
+            if (p.out8) reinterpret_cast<uint2 *>(p.out8)[at + k * span] = codes8(o, qs, p.fmt);
         }
         now += per_stage;
         if (now == ring_end) now = ring;
     }
-    amax_end(m, p.amax_bits, alone);
+    amax_end(pack_bf16x2(m, 0.0f), p.amax_bits, alone);
 }
 
 // ---------------------------------------------------------------- backward
@@ -211,7 +226,7 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
     const unsigned at_once = CTA ? 1 : 32u >> lanes_log2, sub = CTA ? 0 : (threadIdx.x & 31) >> lanes_log2;   // rows of a warp
     const Rows rows = rows_of((size_t)blockIdx.x * groups + group, (size_t)gridDim.x * groups, p.T);
     const float inv_d = 1.0f / (float)(p.n8 * 8);
-    const float qs = p.dy8 ? __ldg(p.q_scale) : 1.0f;
+    const uint64_t qs = both(p.dy8 ? __ldg(p.q_scale) : 1.0f);
     if (CTA) {
         if (threadIdx.x < MAXT / 32)
             red[0][0][threadIdx.x] = red[0][1][threadIdx.x] = red[1][0][threadIdx.x] = red[1][1][threadIdx.x] = 0.0f;
@@ -263,7 +278,8 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
         fetch_first(ring + s * per_stage);
         fetch_second(ring + s * per_stage);
     }
-    uint32_t m = 0, now = ring, fill = ring + (STAGES - 1) * per_stage;
+    float m = 0.0f;
+    uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage;
     int flip = 0;
     const uint64_t a2 = both(p.a), b2 = both(p.b);
     float rp32 = 1.0f, rq32 = 1.0f, rp_ahead = 1.0f, rq_ahead = 1.0f;      // lane l: the statistics of row l of a batch of 32
@@ -346,10 +362,10 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     uint64_t slope = mul_f32x2(D[e], mul_f32x2(y[e], gq[e]));
-                    if (p.sigmoid) {                          // 1 - s = sigmoid(-g): no cancellation where s is near 1
-                        const uint64_t s = sigmoid2(g[e]);
-                        slope = mul_f32x2(slope, mul_f32x2(s, sigmoid2(mul_f32x2(g[e], both(-1.0f)))));
-                        g[e] = s;
+                    if (p.sigmoid) {
+                        uint64_t rest;
+                        g[e] = sigmoid2(g[e], rest);
+                        slope = mul_f32x2(slope, mul_f32x2(g[e], rest));
                     }
                     o[e] = round2(slope);
                     D[e] = mul_f32x2(D[e], g[e]);
@@ -380,17 +396,17 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 o[e] = round2(f[k][e]);
-                m = absmax2e(m, o[e]);
+                m = absmax3(m, f[k][e]);
             }
             if (p.dy) reinterpret_cast<uint4 *>(p.dy)[at + k * span] = make_uint4(o[0], o[1], o[2], o[3]);
-            if (p.dy8) reinterpret_cast<uint2 *>(p.dy8)[at + k * span] = bf16x8_to_fp8x8(o, qs, p.fmt);
+            if (p.dy8) reinterpret_cast<uint2 *>(p.dy8)[at + k * span] = codes8(make_uint4(o[0], o[1], o[2], o[3]), qs, p.fmt);
         }
         if (STAGES == 1) fetch_second(ring);
         now += per_stage;
         if (now == ring_end) now = ring;
     }
     cp_async_wait<0>();
-    amax_end(m, p.amax_bits, alone);
+    amax_end(pack_bf16x2(m, 0.0f), p.amax_bits, alone);
     if (!p.partial) return;
     const size_t D = (size_t)p.n8 * 8;
     float *mine = p.partial + (size_t)blockIdx.x * 2 * D;

@@ -104,46 +104,80 @@ struct RopeArgs {
 };
 constexpr int ROPE_HEADS = 4;
 
-__device__ __forceinline__ void unpack8(const uint4 w, float (&f)[8])
-{
-    f[0] = bf16_lo(w.x); f[1] = bf16_hi(w.x); f[2] = bf16_lo(w.y); f[3] = bf16_hi(w.y);
-    f[4] = bf16_lo(w.z); f[5] = bf16_hi(w.z); f[6] = bf16_lo(w.w); f[7] = bf16_hi(w.w);
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8])
-{
-    return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-}
-
-// The rotation of a lane's two groups of eight: partners are the same places of the two groups, or neighbours in each.
-template <bool PAIRS, bool BACK>
-__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&sn)[8])
-{
-    if (PAIRS) {
+// A lane's cos and sin of a token, as the packed instructions take them: of partners in two groups (cos, sin, -sin of four pairs
+// of places), or of neighbours (cos cos, -sin sin of each of eight pairs).
+template <bool PAIRS>
+struct Angles {
+    uint64_t c[PAIRS ? 8 : 4], up[PAIRS ? 1 : 4], down[PAIRS ? 8 : 4];
+    __device__ __forceinline__ void load(const float *pc, const float *ps, int i0, int i1, bool back)
+    {
+        const float4 c0 = __ldg(reinterpret_cast<const float4 *>(pc + i0)), c1 = __ldg(reinterpret_cast<const float4 *>(pc + i1));
+        const float4 s0 = __ldg(reinterpret_cast<const float4 *>(ps + i0)), s1 = __ldg(reinterpret_cast<const float4 *>(ps + i1));
+        const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+        float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float s0 = BACK ? -sn[e] : sn[e], s1 = BACK ? -sn[4 + e] : sn[4 + e];
-            const float x = a[2 * e], y = a[2 * e + 1], z = b[2 * e], w = b[2 * e + 1];
-            a[2 * e] = x * c[e] - y * s0;
-            a[2 * e + 1] = y * c[e] + x * s0;
-            b[2 * e] = z * c[4 + e] - w * s1;
-            b[2 * e + 1] = w * c[4 + e] + z * s1;
-        }
-    } else {
+        for (int e = 0; e < 8; ++e) sn[e] = back ? -sn[e] : sn[e];
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {                       // two places at a time with the packed instructions
-            const uint64_t x = pack_f32x2(a[e], a[e + 1]), y = pack_f32x2(b[e], b[e + 1]), c2 = pack_f32x2(c[e], c[e + 1]);
-            const uint64_t up = pack_f32x2(sn[e], sn[e + 1]), down = pack_f32x2(-sn[e], -sn[e + 1]);
-            unpack_f32x2(fma_f32x2(x, c2, mul_f32x2(y, BACK ? up : down)), a[e], a[e + 1]);
-            unpack_f32x2(fma_f32x2(y, c2, mul_f32x2(x, BACK ? down : up)), b[e], b[e + 1]);
+        for (int e = 0; e < (PAIRS ? 8 : 4); ++e) {
+            if (PAIRS) {
+                c[e] = both(cs[e]);
+                down[e] = pack_f32x2(-sn[e], sn[e]);
+            } else {
+                c[e] = pack_f32x2(cs[2 * e], cs[2 * e + 1]);
+                up[PAIRS ? 0 : e] = pack_f32x2(sn[2 * e], sn[2 * e + 1]);
+                down[e] = pack_f32x2(-sn[2 * e], -sn[2 * e + 1]);
+            }
         }
     }
-}
-__device__ __forceinline__ void scale8(float (&a)[8], float r)
-{
-    const uint64_t r2 = pack_f32x2(r, r);
+    // The rotation of a lane's two groups of eight: partners are the same places of the two groups, or neighbours in each.
+    __device__ __forceinline__ void turn(uint64_t (&a)[4], uint64_t (&b)[4]) const
+    {
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) unpack_f32x2(mul_f32x2(pack_f32x2(a[e], a[e + 1]), r2), a[e], a[e + 1]);
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t x = a[e], y = b[e];
+            if (PAIRS) {
+                a[e] = fma_f32x2(x, c[e], mul_f32x2(swapped(x), down[e]));
+                b[e] = fma_f32x2(y, c[PAIRS ? 4 + e : 0], mul_f32x2(swapped(y), down[PAIRS ? 4 + e : 0]));
+            } else {
+                a[e] = fma_f32x2(x, c[e], mul_f32x2(y, down[e]));
+                b[e] = fma_f32x2(y, c[e], mul_f32x2(x, up[PAIRS ? 0 : e]));
+            }
+        }
+    }
+    static __device__ __forceinline__ uint64_t swapped(uint64_t v)
+    {
+        float lo, hi;
+        unpack_f32x2(v, lo, hi);
+        return pack_f32x2(hi, lo);
+    }
+};
+__device__ __forceinline__ void scale8(uint64_t (&a)[4], float r)
+{
+    const uint64_t r2 = both(r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] = mul_f32x2(a[e], r2);
 }
+__device__ __forceinline__ float dot16(const uint64_t (&a)[4], const uint64_t (&b)[4], const uint64_t (&x)[4], const uint64_t (&y)[4])
+{
+    uint64_t s = mul_f32x2(a[0], x[0]), t = mul_f32x2(b[0], y[0]);
+#pragma unroll
+    for (int e = 1; e < 4; ++e) {
+        s = fma_f32x2(a[e], x[e], s);
+        t = fma_f32x2(b[e], y[e], t);
+    }
+    return add_halves(add_f32x2(s, t));
+}
+template <typename F>
+__device__ __forceinline__ void each8(uint64_t (&a)[4], F f)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float lo, hi;
+        unpack_f32x2(a[e], lo, hi);
+        a[e] = pack_f32x2(f(lo), f(hi));
+    }
+}
+
 // 1 - tanh(x)^2 = 4 e / (1 + e)^2 with e = exp(-2 |x|): no cancellation where tanh is near 1.
 __device__ __forceinline__ float sech2(float x)
 {
@@ -175,7 +209,7 @@ __device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int
 // group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
 // bind: every element is read once and written once.
 template <int MODE, bool BACK>
-constexpr int rope_slots() { return ROPE_HEADS * (BACK && MODE != FP8_QK_NONE ? 4 : 2); }
+__host__ __device__ constexpr int rope_slots() { return ROPE_HEADS * (BACK && MODE != FP8_QK_NONE ? 4 : 2); }
 template <int MODE, bool PAIRS, bool BACK, int STAGES>
 __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs p, int slots)
 {
@@ -202,8 +236,8 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
     const size_t part_pitch = (size_t)n_heads * d, row_pitch = (size_t)(p.heads[0] + p.heads[1] + p.heads[2]) * d;
     size_t t = (size_t)first * p.tokens + local, ahead = t;
     // places in shared memory: [stage][slot][thread]; slots 2 hh, 2 hh + 1 are a head's groups, behind them those of what is saved
-    const uint32_t ring = smem_u32(ring_mem + threadIdx.x), per_slot = blockDim.x * 16u, per_stage = per_slot * (unsigned)slots;
-    const uint32_t ring_end = ring + STAGES * per_stage;
+    constexpr uint32_t per_slot = 256u * 16u, per_stage = per_slot * rope_slots<MODE, BACK>();
+    const uint32_t ring = smem_u32(ring_mem + threadIdx.x), ring_end = ring + STAGES * per_stage;
     const auto fetch = [&](uint32_t to) {
         if (mine && ahead < p.T) {
             const uint16_t *src = BACK ? p.grad[part] + ahead * part_pitch + in_part : p.qkv + ahead * p.pitch + in_row;
@@ -247,14 +281,8 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
                 pos = (unsigned)t % (unsigned)p.n_pos;         // both are below 2^31
             }
         }
-        float c[8], sn[8];
-        if (turns && part < 2) {
-            const float *pc = p.cos_t + pos * (p.rot / 2), *ps = p.sin_t + pos * (p.rot / 2);
-            const float4 c0 = __ldg(reinterpret_cast<const float4 *>(pc + i0)), c1 = __ldg(reinterpret_cast<const float4 *>(pc + i1));
-            const float4 s0 = __ldg(reinterpret_cast<const float4 *>(ps + i0)), s1 = __ldg(reinterpret_cast<const float4 *>(ps + i1));
-            c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
-            sn[0] = s0.x; sn[1] = s0.y; sn[2] = s0.z; sn[3] = s0.w; sn[4] = s1.x; sn[5] = s1.y; sn[6] = s1.z; sn[7] = s1.w;
-        }
+        Angles<PAIRS> angles;
+        if (turns && part < 2) angles.load(p.cos_t + pos * (p.rot / 2), p.sin_t + pos * (p.rot / 2), i0, i1, BACK);
         cp_async_wait<STAGES - 2>();
         fetch(fill);                                           // the stage of the token before this one
         fill = now;
@@ -263,20 +291,16 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
 #pragma unroll
         for (int hh = 0; hh < ROPE_HEADS; ++hh, o += d, o8 += d) {
             if (hh > 0 && __all_sync(0xffffffffu, hh >= here)) break;
-            float a[8], b[8], x[8], y[8];
-            unpack8(ring_get(now + (2 * hh) * per_slot), a);
-            unpack8(ring_get(now + (2 * hh + 1) * per_slot), b);
+            uint64_t a[4], b[4], x[4], y[4];
+            unpack4x2(ring_get(now + (2 * hh) * per_slot), a);
+            unpack4x2(ring_get(now + (2 * hh + 1) * per_slot), b);
             if (SAVED && part < 2) {
-                unpack8(ring_get(now + (2 * ROPE_HEADS + 2 * hh) * per_slot), x);
-                unpack8(ring_get(now + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot), y);
+                unpack4x2(ring_get(now + (2 * ROPE_HEADS + 2 * hh) * per_slot), x);
+                unpack4x2(ring_get(now + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot), y);
             }
             float r = 1.0f;
             if (MODE == FP8_QK_RMS) {
-                float ss = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss = BACK ? fmaf(x[e], x[e], fmaf(y[e], y[e], ss)) : fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
-                if (!mine) ss = 0.0f;
-                for (int off = lanes >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                const float ss = row_sum<false, 4>(!mine ? 0.0f : BACK ? dot16(x, y, x, y) : dot16(a, b, a, b), p.lanes_log2, nullptr);
                 r = rsqrtf(fmaf(ss, p.inv_d, p.eps));
             }
             if (!BACK && part < 2) {
@@ -284,39 +308,44 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
                     scale8(a, r);
                     scale8(b, r);
                 } else if (MODE == FP8_QK_TANH) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { a[e] = tanhf(p.alpha * a[e]); b[e] = tanhf(p.alpha * b[e]); }
+                    each8(a, [&](float v) { return tanhf(p.alpha * v); });
+                    each8(b, [&](float v) { return tanhf(p.alpha * v); });
                 }
             }
-            if (turns && part < 2) rotate<PAIRS, BACK>(a, b, c, sn);
+            if (turns && part < 2) angles.turn(a, b);
             if (BACK && MODE == FP8_QK_RMS) {
-                float s = 0.0f;
                 scale8(x, r);
                 scale8(y, r);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s = fmaf(a[e], x[e], fmaf(b[e], y[e], s));
-                if (!mine) s = 0.0f;
-                for (int off = lanes >> 1; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                const float s = row_sum<false, 4>(!mine ? 0.0f : dot16(a, b, x, y), p.lanes_log2, nullptr) * -p.inv_d;
                 if (part < 2) {
-                    s *= -p.inv_d;
+                    const uint64_t s2 = both(s);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { a[e] = fmaf(s, x[e], a[e]); b[e] = fmaf(s, y[e], b[e]); }
+                    for (int e = 0; e < 4; ++e) {
+                        a[e] = fma_f32x2(s2, x[e], a[e]);
+                        b[e] = fma_f32x2(s2, y[e], b[e]);
+                    }
                     scale8(a, r);
                     scale8(b, r);
                 }
             }
             if (BACK && MODE == FP8_QK_TANH && part < 2) {
+                each8(x, [&](float v) { return p.alpha * sech2(p.alpha * v); });
+                each8(y, [&](float v) { return p.alpha * sech2(p.alpha * v); });
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { a[e] *= p.alpha * sech2(p.alpha * x[e]); b[e] *= p.alpha * sech2(p.alpha * y[e]); }
+                for (int e = 0; e < 4; ++e) {
+                    a[e] = mul_f32x2(a[e], x[e]);
+                    b[e] = mul_f32x2(b[e], y[e]);
+                }
             }
             if (!live || hh >= here) continue;
             if (!known) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.0f;
+                for (int e = 0; e < 4; ++e) a[e] = b[e] = 0ull;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = absmax3(m, a[e], b[e]);
-            const uint4 oa = pack8(a), ob = pack8(b);
+            for (int e = 0; e < 4; ++e) m = absmax3(absmax3(m, a[e]), b[e]);
+            const uint4 oa = make_uint4(round2(a[0]), round2(a[1]), round2(a[2]), round2(a[3]));
+            const uint4 ob = make_uint4(round2(b[0]), round2(b[1]), round2(b[2]), round2(b[3]));
             if (out) {
                 *reinterpret_cast<uint4 *>(o) = oa;
                 *reinterpret_cast<uint4 *>(o + other) = ob;
@@ -346,7 +375,7 @@ static int rope_run(const RopeArgs &p, int slots, unsigned grid, unsigned thread
         const int rc = allow_shared<Kernel>((int)(256 * per_thread));
         if (rc != FP8_OK) return rc;
     }
-    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, threads * per_thread, st, p, slots, p.words);
+    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, 256 * per_thread, st, p, slots, p.words);
 }
 
 template <bool BACK>

@@ -221,7 +221,9 @@ def test_rope_forward_agrees_with_qk_norm_rope(d, mode):
         x = c.qkv.view(99, -1, d)[:, first:first + got.shape[1]].contiguous()
         out = torch.empty_like(x)
         fp8.fp8_qk_norm_rope(x, mode, c.alpha, c.eps, c.cos, c.sin, c.N, out)
-        assert torch.equal(out, got)
+        # both are within 64 u of the same values in front of their rounding, which then moves them by 2 h at most
+        assert ((out.to(F64) - got.to(F64)).abs() <= 2 * HALF[BF16] * out.to(F64).abs() + 128 * U * 8).all()
+        assert (out != got).to(F64).mean() < 1e-2
 
 
 def test_rope_leaves_out_what_is_not_asked_for():
