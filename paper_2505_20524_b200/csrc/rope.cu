@@ -208,65 +208,165 @@ __device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int
 // A group of lanes takes up to ROPE_HEADS heads of one tensor of one token with the token's angles in registers.  Persistent: a
 // group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
 // bind: every element is read once and written once.
+//
+// Instructions are the next bound, so the usual case, all lanes of a warp with whole pieces of Q and K or of V, runs through four
+// heads without a branch; V's pieces lie behind Q's and K's of all tokens of the CTA for that.  What is left takes the other path.
+// KIND: what is written, BF16 alone, codes alone in the direction's usual type (E4M3, E5M2 backward), or anything.
+enum RopeKind { ROPE_BF16, ROPE_CODES, ROPE_ANY };
 template <int MODE, bool BACK>
 __host__ __device__ constexpr int rope_slots() { return ROPE_HEADS * (BACK && MODE != FP8_QK_NONE ? 4 : 2); }
-template <int MODE, bool PAIRS, bool BACK, int STAGES>
-__global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs p, int slots)
+
+// Sum over a head's lanes.
+__device__ __forceinline__ float head_sum(float v, int lanes)
+{
+#pragma unroll
+    for (int off = 8; off > 0; off >>= 1) {
+        const float u = __shfl_xor_sync(0xffffffffu, v, off);
+        if (off < lanes) v += u;
+    }
+    return v;
+}
+
+template <int MODE, bool PAIRS, bool BACK, RopeKind KIND, int STAGES>
+__global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs p, int)
 {
     extern __shared__ __align__(16) uint4 ring_mem[];
     constexpr bool SAVED = BACK && MODE != FP8_QK_NONE;
     constexpr int N = BACK ? 1 : 3;
     const bool alone = amax_begin(p.amax_bits, N);
     const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log2;
-    const int turned = p.rot / 16, per_token = p.chunks[0] + p.chunks[1] + p.chunks[2];
+    const int turned = p.rot / 16, n_qk = p.chunks[0] + p.chunks[1], per_token = n_qk + p.chunks[2];
     const unsigned share = blockIdx.x % p.blocks, first = blockIdx.x / p.blocks, ctas = gridDim.x / p.blocks;
-    const int local = group / p.per_cta;
-    int piece = share * p.per_cta + group - local * p.per_cta;
+    int local, piece;
+    if (p.blocks > 1) {
+        local = 0;
+        piece = group < p.per_cta ? share * p.per_cta + group : per_token;
+    } else if (group < p.tokens * n_qk) {
+        local = group / n_qk;
+        piece = group - local * n_qk;
+    } else {
+        const int g = group - p.tokens * n_qk;
+        local = p.chunks[2] ? g / p.chunks[2] : p.tokens;
+        piece = n_qk + g - local * p.chunks[2];
+    }
     const bool mine = j < p.d / 16 && local < p.tokens && piece < per_token, turns = j < turned;
     piece = min(piece, per_token - 1);
-    const int part = piece < p.chunks[0] ? 0 : piece < p.chunks[0] + p.chunks[1] ? 1 : 2;
+    const int part = piece < p.chunks[0] ? 0 : piece < n_qk ? 1 : 2;
     if (part > 0) piece -= p.chunks[0];
     if (part > 1) piece -= p.chunks[1];
-    const int h0 = piece * ROPE_HEADS, n_heads = p.heads[part], here = min(ROPE_HEADS, n_heads - h0);
+    const int h0 = piece * ROPE_HEADS, n_heads = p.heads[part], here = min(ROPE_HEADS, n_heads - h0), d = p.d;
     const int before = (part > 0 ? p.heads[0] : 0) + (part > 1 ? p.heads[1] : 0) + h0;       // heads of the row in front
-    const int lo = turns ? 8 * j : p.rot + 16 * (j - turned), hi = turns ? p.rot / 2 + 8 * j : lo + 8, d = p.d;
+    const int lo = turns ? 8 * j : p.rot + 16 * (j - turned), hi = turns ? p.rot / 2 + 8 * j : lo + 8, other = hi - lo;
     const size_t in_row = (size_t)before * d + lo, in_part = (size_t)h0 * d + lo;
-    const int other = hi - lo;
     const size_t step = (size_t)ctas * p.tokens;
     const size_t part_pitch = (size_t)n_heads * d, row_pitch = (size_t)(p.heads[0] + p.heads[1] + p.heads[2]) * d;
     size_t t = (size_t)first * p.tokens + local, ahead = t;
     // places in shared memory: [stage][slot][thread]; slots 2 hh, 2 hh + 1 are a head's groups, behind them those of what is saved
-    constexpr uint32_t per_slot = 256u * 16u, per_stage = per_slot * rope_slots<MODE, BACK>();
+    const uint32_t per_slot = blockDim.x * 16u, per_stage = per_slot * rope_slots<MODE, BACK>();
     const uint32_t ring = smem_u32(ring_mem + threadIdx.x), ring_end = ring + STAGES * per_stage;
+    const uint16_t *next = (BACK ? p.grad[part] + in_part : p.qkv + in_row) + ahead * (BACK ? part_pitch : p.pitch);
+    const uint16_t *next_saved = SAVED ? p.qkv + in_row + ahead * p.pitch : nullptr;
+    const size_t next_step = step * (BACK ? part_pitch : p.pitch), saved_step = step * p.pitch;
     const auto fetch = [&](uint32_t to) {
         if (mine && ahead < p.T) {
-            const uint16_t *src = BACK ? p.grad[part] + ahead * part_pitch + in_part : p.qkv + ahead * p.pitch + in_row;
-            const uint16_t *saved = p.qkv + ahead * p.pitch + in_row;
 #pragma unroll
             for (int hh = 0; hh < ROPE_HEADS; ++hh) {
                 if (hh < here) {
-                    cp_async16(to + (2 * hh) * per_slot, src + hh * d);
-                    cp_async16(to + (2 * hh + 1) * per_slot, src + hh * d + other);
+                    cp_async16(to + (2 * hh) * per_slot, next + hh * d);
+                    cp_async16(to + (2 * hh + 1) * per_slot, next + hh * d + other);
                     if (SAVED && part < 2) {
-                        cp_async16(to + (2 * ROPE_HEADS + 2 * hh) * per_slot, saved + hh * d);
-                        cp_async16(to + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot, saved + hh * d + other);
+                        cp_async16(to + (2 * ROPE_HEADS + 2 * hh) * per_slot, next_saved + hh * d);
+                        cp_async16(to + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot, next_saved + hh * d + other);
                     }
                 }
             }
         }
         cp_async_commit();
         ahead += step;
+        next += next_step;
+        if (SAVED) next_saved += saved_step;
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) fetch(ring + s * per_stage);
-    const float qs = p.scales ? __ldg(p.scales + (BACK ? 0 : part)) : 1.0f;
-    const uint64_t qs2 = both(qs);
+    const uint64_t qs2 = both(p.scales ? __ldg(p.scales + (BACK ? 0 : part)) : 1.0f);
+    const size_t out_pitch = BACK ? p.out_pitch : part_pitch, out8_pitch = BACK ? row_pitch : part_pitch, out_at = BACK ? in_row : in_part;
     uint16_t *const out = BACK ? p.out[0] : p.out[part];
     uint8_t *const out8 = BACK ? p.out8[0] : p.out8[part];
-    const size_t out_pitch = BACK ? p.out_pitch : part_pitch, out8_pitch = BACK ? row_pitch : part_pitch, out_at = BACK ? in_row : in_part;
     const int i0 = PAIRS ? 4 * j : 8 * j, i1 = PAIRS ? p.rot / 4 + 4 * j : 8 * j + 4;
     float m = 0.0f;
     uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage;
+
+    // A lane's part of a head: what is read, regularised and rotated (or back), with `qk` false as it is.
+    const auto work = [&](int hh, bool qk, bool every_lane_turns, const Angles<PAIRS> &angles, uint64_t (&a)[4], uint64_t (&b)[4]) {
+        uint64_t x[4], y[4];
+        unpack4x2(ring_get(now + (2 * hh) * per_slot), a);
+        unpack4x2(ring_get(now + (2 * hh + 1) * per_slot), b);
+        if (!qk) return;
+        if (SAVED) {
+            unpack4x2(ring_get(now + (2 * ROPE_HEADS + 2 * hh) * per_slot), x);
+            unpack4x2(ring_get(now + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot), y);
+        }
+        float r = 1.0f;
+        if (MODE == FP8_QK_RMS) r = rsqrtf(fmaf(head_sum(mine ? (BACK ? dot16(x, y, x, y) : dot16(a, b, a, b)) : 0.0f, lanes), p.inv_d, p.eps));
+        if (!BACK) {
+            if (MODE == FP8_QK_RMS) {
+                scale8(a, r);
+                scale8(b, r);
+            } else if (MODE == FP8_QK_TANH) {
+                each8(a, [&](float v) { return tanhf(p.alpha * v); });
+                each8(b, [&](float v) { return tanhf(p.alpha * v); });
+            }
+        }
+        if (every_lane_turns) {
+            angles.turn(a, b);
+        } else if (p.rot) {
+            uint64_t u[4] = {a[0], a[1], a[2], a[3]}, w[4] = {b[0], b[1], b[2], b[3]};
+            angles.turn(u, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = turns ? u[e] : a[e];
+                b[e] = turns ? w[e] : b[e];
+            }
+        }
+        if (BACK && MODE == FP8_QK_RMS) {
+            scale8(x, r);
+            scale8(y, r);
+            const uint64_t s2 = both(head_sum(mine ? dot16(a, b, x, y) : 0.0f, lanes) * -p.inv_d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = fma_f32x2(s2, x[e], a[e]);
+                b[e] = fma_f32x2(s2, y[e], b[e]);
+            }
+            scale8(a, r);
+            scale8(b, r);
+        }
+        if (BACK && MODE == FP8_QK_TANH) {
+            each8(x, [&](float v) { return p.alpha * sech2(p.alpha * v); });
+            each8(y, [&](float v) { return p.alpha * sech2(p.alpha * v); });
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = mul_f32x2(a[e], x[e]);
+                b[e] = mul_f32x2(b[e], y[e]);
+            }
+        }
+    };
+    const auto store = [&](int hh, const uint64_t (&a)[4], const uint64_t (&b)[4], uint16_t *o, uint8_t *o8) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = absmax3(absmax3(m, a[e]), b[e]);
+        const uint4 oa = make_uint4(round2(a[0]), round2(a[1]), round2(a[2]), round2(a[3]));
+        const uint4 ob = make_uint4(round2(b[0]), round2(b[1]), round2(b[2]), round2(b[3]));
+        if (KIND == ROPE_BF16 || (KIND == ROPE_ANY && out)) {
+            *reinterpret_cast<uint4 *>(o + hh * d) = oa;
+            *reinterpret_cast<uint4 *>(o + hh * d + other) = ob;
+        }
+        if (KIND == ROPE_CODES || (KIND == ROPE_ANY && out8)) {
+            const int fmt = KIND == ROPE_CODES ? BACK : p.fmt;
+            *reinterpret_cast<uint2 *>(o8 + hh * d) = codes8(oa, qs2, fmt);
+            *reinterpret_cast<uint2 *>(o8 + hh * d + other) = codes8(ob, qs2, fmt);
+        }
+    };
+    const bool plain_lane = mine && here == ROPE_HEADS, whole_head = p.rot == d;
+    const bool plain_qk = __all_sync(0xffffffffu, plain_lane && part < 2), plain_v = __all_sync(0xffffffffu, plain_lane && part == 2);
     for (size_t base = (size_t)first * p.tokens; base < p.T; base += step, t += step) {
         size_t pos = 0;
         bool known = true;
@@ -286,73 +386,35 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
         cp_async_wait<STAGES - 2>();
         fetch(fill);                                           // the stage of the token before this one
         fill = now;
-        uint16_t *o = out + t * out_pitch + out_at;
-        uint8_t *o8 = out8 + t * out8_pitch + out_at;
+        uint16_t *const o = out + t * out_pitch + out_at;
+        uint8_t *const o8 = out8 + t * out8_pitch + out_at;
+        const bool plain = __all_sync(0xffffffffu, live && known);
+        if (plain && plain_qk) {
 #pragma unroll
-        for (int hh = 0; hh < ROPE_HEADS; ++hh, o += d, o8 += d) {
-            if (hh > 0 && __all_sync(0xffffffffu, hh >= here)) break;
-            uint64_t a[4], b[4], x[4], y[4];
-            unpack4x2(ring_get(now + (2 * hh) * per_slot), a);
-            unpack4x2(ring_get(now + (2 * hh + 1) * per_slot), b);
-            if (SAVED && part < 2) {
-                unpack4x2(ring_get(now + (2 * ROPE_HEADS + 2 * hh) * per_slot), x);
-                unpack4x2(ring_get(now + (2 * ROPE_HEADS + 2 * hh + 1) * per_slot), y);
+            for (int hh = 0; hh < ROPE_HEADS; ++hh) {
+                uint64_t a[4], b[4];
+                work(hh, true, whole_head, angles, a, b);
+                store(hh, a, b, o, o8);
             }
-            float r = 1.0f;
-            if (MODE == FP8_QK_RMS) {
-                const float ss = row_sum<false, 4>(!mine ? 0.0f : BACK ? dot16(x, y, x, y) : dot16(a, b, a, b), p.lanes_log2, nullptr);
-                r = rsqrtf(fmaf(ss, p.inv_d, p.eps));
-            }
-            if (!BACK && part < 2) {
-                if (MODE == FP8_QK_RMS) {
-                    scale8(a, r);
-                    scale8(b, r);
-                } else if (MODE == FP8_QK_TANH) {
-                    each8(a, [&](float v) { return tanhf(p.alpha * v); });
-                    each8(b, [&](float v) { return tanhf(p.alpha * v); });
-                }
-            }
-            if (turns && part < 2) angles.turn(a, b);
-            if (BACK && MODE == FP8_QK_RMS) {
-                scale8(x, r);
-                scale8(y, r);
-                const float s = row_sum<false, 4>(!mine ? 0.0f : dot16(a, b, x, y), p.lanes_log2, nullptr) * -p.inv_d;
-                if (part < 2) {
-                    const uint64_t s2 = both(s);
+        } else if (plain && plain_v) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        a[e] = fma_f32x2(s2, x[e], a[e]);
-                        b[e] = fma_f32x2(s2, y[e], b[e]);
-                    }
-                    scale8(a, r);
-                    scale8(b, r);
-                }
+            for (int hh = 0; hh < ROPE_HEADS; ++hh) {
+                uint64_t a[4], b[4];
+                work(hh, false, false, angles, a, b);
+                store(hh, a, b, o, o8);
             }
-            if (BACK && MODE == FP8_QK_TANH && part < 2) {
-                each8(x, [&](float v) { return p.alpha * sech2(p.alpha * v); });
-                each8(y, [&](float v) { return p.alpha * sech2(p.alpha * v); });
+        } else {
+#pragma unroll 1
+            for (int hh = 0; hh < ROPE_HEADS; ++hh) {
+                uint64_t a[4], b[4], u[4], w[4];
+                work(hh, true, false, angles, a, b);           // all lanes: it has sums over lanes
+                work(hh, false, false, angles, u, w);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    a[e] = mul_f32x2(a[e], x[e]);
-                    b[e] = mul_f32x2(b[e], y[e]);
+                    a[e] = !known ? 0ull : part < 2 ? a[e] : u[e];
+                    b[e] = !known ? 0ull : part < 2 ? b[e] : w[e];
                 }
-            }
-            if (!live || hh >= here) continue;
-            if (!known) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) a[e] = b[e] = 0ull;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m = absmax3(absmax3(m, a[e]), b[e]);
-            const uint4 oa = make_uint4(round2(a[0]), round2(a[1]), round2(a[2]), round2(a[3]));
-            const uint4 ob = make_uint4(round2(b[0]), round2(b[1]), round2(b[2]), round2(b[3]));
-            if (out) {
-                *reinterpret_cast<uint4 *>(o) = oa;
-                *reinterpret_cast<uint4 *>(o + other) = ob;
-            }
-            if (out8) {
-                *reinterpret_cast<uint2 *>(o8) = codes8(oa, qs2, p.fmt);
-                *reinterpret_cast<uint2 *>(o8 + other) = codes8(ob, qs2, p.fmt);
+                if (live && hh < here) store(hh, a, b, o, o8);
             }
         }
         now += per_stage;
@@ -369,13 +431,13 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
 }
 
 template <auto Kernel>
-static int rope_run(const RopeArgs &p, int slots, unsigned grid, unsigned threads, size_t per_thread, size_t elements, cudaStream_t st)
+static int rope_run(const RopeArgs &p, unsigned grid, unsigned threads, size_t per_thread, size_t elements, cudaStream_t st)
 {
     if (256 * per_thread > 40 * 1024) {
         const int rc = allow_shared<Kernel>((int)(256 * per_thread));
         if (rc != FP8_OK) return rc;
     }
-    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, 256 * per_thread, st, p, slots, p.words);
+    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, threads * per_thread, st, p, 0, p.words);
 }
 
 template <bool BACK>
@@ -404,17 +466,32 @@ static int rope_launch(RopeArgs &p, int mode, bool pairs, cudaStream_t st)
     if (ctas == 0) ctas = 1;
     const unsigned grid = (unsigned)(ctas * p.blocks);
     const size_t elements = p.T * (size_t)(p.heads[0] + p.heads[1] + p.heads[2]) * p.d;
+    bool bf16 = true, codes = true;
+    for (int i = 0; i < (BACK ? 1 : 3); ++i) {
+        if (!BACK && !p.chunks[i]) continue;
+        bf16 &= p.out[i] && !p.out8[i];
+        codes &= !p.out[i] && p.out8[i] && p.fmt == (BACK ? FP8_E5M2 : FP8_E4M3);
+    }
+    constexpr int STAGES = 2;
+#define FP8DPA_ROPE_RUN(MODE, PAIRS, KIND) \
+    return rope_run<rope_kernel<MODE, PAIRS, BACK, KIND, STAGES>>(p, grid, threads, (size_t)STAGES * rope_slots<MODE, BACK>() * 16, elements, st)
+#define FP8DPA_ROPE_PAIRS(MODE, PAIRS) \
+    do { \
+        if (bf16) FP8DPA_ROPE_RUN(MODE, PAIRS, ROPE_BF16); \
+        if (codes) FP8DPA_ROPE_RUN(MODE, PAIRS, ROPE_CODES); \
+        FP8DPA_ROPE_RUN(MODE, PAIRS, ROPE_ANY); \
+    } while (0)
 #define FP8DPA_LAUNCH_ROPE(MODE) \
     do { \
-        constexpr int STAGES = 2, SLOTS = rope_slots<MODE, BACK>(); \
-        constexpr size_t per_thread = (size_t)STAGES * SLOTS * 16; \
-        if (pairs) return rope_run<rope_kernel<MODE, true, BACK, STAGES>>(p, SLOTS, grid, threads, per_thread, elements, st); \
-        return rope_run<rope_kernel<MODE, false, BACK, STAGES>>(p, SLOTS, grid, threads, per_thread, elements, st); \
+        if (pairs) FP8DPA_ROPE_PAIRS(MODE, true); \
+        else FP8DPA_ROPE_PAIRS(MODE, false); \
     } while (0)
     if (mode == FP8_QK_RMS) FP8DPA_LAUNCH_ROPE(FP8_QK_RMS);
     else if (mode == FP8_QK_TANH) FP8DPA_LAUNCH_ROPE(FP8_QK_TANH);
     else FP8DPA_LAUNCH_ROPE(FP8_QK_NONE);
 #undef FP8DPA_LAUNCH_ROPE
+#undef FP8DPA_ROPE_PAIRS
+#undef FP8DPA_ROPE_RUN
 }
 
 // What both directions check of an fp8_rope; 0 or a status.
