@@ -310,7 +310,7 @@ def _here(stream):
 
 
 _BF16, _F32, _U8, _I32 = torch.bfloat16, torch.float32, torch.uint8, torch.int32
-_FLOATS, _INTS, _ONE = (torch.bfloat16, torch.float32), (torch.int32, torch.int64), (1,)
+_FLOATS, _INTS, _ONE, _THREE = (torch.bfloat16, torch.float32), (torch.int32, torch.int64), (1,), (3,)
 
 
 def _matrix(name, t):
@@ -516,94 +516,98 @@ def fp8_rope_table(cos, sin, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, origi
 def _rope(mode, alpha, eps, cos, sin, positions, interleaved, T, dev):
     if cos is None:
         return Rope(mode, alpha, eps, None, None, 0, 0, bool(interleaved), None, 0)
-    N, half = _matrix("cos", cos)
-    return Rope(mode, alpha, eps, _addr("cos", cos, _F32, cos.shape, dev), _addr("sin", sin, _F32, cos.shape, dev), N, 2 * half,
-                bool(interleaved), _opt("positions", positions, _INTS, (T,), dev),
-                positions is not None and positions.dtype is torch.int64)
+    N, half = shape = cos.shape if cos.dim() == 2 else _matrix("cos", cos)
+    c, s = _addr("cos", cos, _F32, shape, dev), _addr("sin", sin, _F32, shape, dev)
+    if positions is None:
+        return Rope(mode, alpha, eps, c, s, N, 2 * half, interleaved, None, 0)
+    return Rope(mode, alpha, eps, c, s, N, 2 * half, interleaved, _addr("positions", positions, _INTS, (T,), dev),
+                positions.dtype is torch.int64)
 
 
 def _pitched(name, t, T, W, dev):
     """(address, elements from row to row) of a BF16 matrix whose rows are contiguous."""
-    if t.dtype is _BF16 and t.shape == (T, W) and (W < 2 or t.stride(1) == 1) and (T < 2 or t.stride(0) >= W) and t.get_device() == dev:
-        return t.data_ptr(), t.stride(0) if T > 1 else W
+    if t.dtype is _BF16 and t.shape == (T, W) and t.get_device() == dev:
+        row, col = t.stride()
+        if (col == 1 or W < 2) and (row >= W or T < 2):
+            return t.data_ptr(), row if T > 1 else W
     raise ValueError(f"{name}: expects a bfloat16 matrix of shape {(T, W)} with contiguous rows on the current device, cuda:{dev}; got "
                      f"{t.dtype} of shape {tuple(t.shape)} and strides {t.stride()} on {t.device}")
 
 
 def _heads(qkv, Hq, Hkv):
     T, W = _matrix("qkv", qkv)
-    if Hq <= 0 or Hkv < 0 or W == 0 or W % (Hq + 2 * Hkv):
+    H = Hq + 2 * Hkv
+    if Hq <= 0 or Hkv < 0 or W == 0 or W % H:
         raise ValueError(f"qkv: rows of {W} values are not {Hq} + 2 * {Hkv} heads")
-    return T, W, W // (Hq + 2 * Hkv)
-
-
-def _rope_fwd_args(qkv, Hq, Hkv, rope, q, k, v, q8, k8, v8, stream):
-    (T, W, d), (dev, st) = _heads(qkv, Hq, Hkv), _here(stream)
-    heads = ((T, Hq, d), (T, Hkv, d), (T, Hkv, d))
-    return (dev, st, (*_pitched("qkv", qkv, T, W, dev), T, Hq, Hkv, d, C.byref(_rope(*rope, T, dev))),
-            [_opt(n, t, _BF16, s, dev) for n, t, s in zip("qkv", (q, k, v), heads)],
-            [_opt(n + "8", t, _U8, s, dev) for n, t, s in zip("qkv", (q8, k8, v8), heads)])
+    return T, W, W // H
 
 
 def fp8_rope_qkv_fwd(qkv, Hq, Hkv, mode, alpha, eps, cos, sin, positions, interleaved, q, k, v, amax_out=None, stream=None):
     """Rows of the QKV projection [T, (Hq + 2 Hkv) d] BF16 (rows may be strided) -> q [T, Hq, d], k, v [T, Hkv, d] BF16 (each may be
     None): regulariser `mode` (QK_*) and rotation of Q and K by the tables cos, sin [n_pos, rot / 2] (None: no rotation) at positions
     [T] int32 / int64 (None: t mod n_pos; outside the table: a token of zeros); amax_out [3] FP32: amax of q, k, v."""
-    dev, st, ins, outs, _ = _rope_fwd_args(qkv, Hq, Hkv, (mode, alpha, eps, cos, sin, positions, interleaved), q, k, v, None, None, None,
-                                           stream)
-    _check(load().fp8_rope_qkv_fwd(*ins, *outs, _opt("amax_out", amax_out, _F32, (3,), dev), st))
+    T, W, d = _heads(qkv, Hq, Hkv)
+    dev, st = _here(stream)
+    at, pitch = _pitched("qkv", qkv, T, W, dev)
+    kv = (T, Hkv, d)
+    _check(load().fp8_rope_qkv_fwd(at, pitch, T, Hq, Hkv, d, C.byref(_rope(mode, alpha, eps, cos, sin, positions, interleaved, T, dev)),
+                                   _opt("q", q, _BF16, (T, Hq, d), dev), _opt("k", k, _BF16, kv, dev), _opt("v", v, _BF16, kv, dev),
+                                   _opt("amax_out", amax_out, _F32, _THREE, dev), st))
 
 
 def fp8_rope_qkv_fwd_q(qkv, Hq, Hkv, mode, alpha, eps, cos, sin, positions, interleaved, scales, fmt, q8, k8, v8, q=None, k=None,
                        v=None, amax_out=None, stream=None):
     """fp8_rope_qkv_fwd that also writes the FP8 codes q8, k8, v8 (each may be None) of its (BF16-rounded) results under the delayed
     scales [3] FP32."""
-    dev, st, ins, outs, codes = _rope_fwd_args(qkv, Hq, Hkv, (mode, alpha, eps, cos, sin, positions, interleaved), q, k, v, q8, k8, v8,
-                                               stream)
-    _check(load().fp8_rope_qkv_fwd_q(*ins, _addr("scales", scales, _F32, (3,), dev), fmt, *outs, *codes,
-                                     _opt("amax_out", amax_out, _F32, (3,), dev), st))
+    T, W, d = _heads(qkv, Hq, Hkv)
+    dev, st = _here(stream)
+    at, pitch = _pitched("qkv", qkv, T, W, dev)
+    qs, kv = (T, Hq, d), (T, Hkv, d)
+    _check(load().fp8_rope_qkv_fwd_q(at, pitch, T, Hq, Hkv, d, C.byref(_rope(mode, alpha, eps, cos, sin, positions, interleaved, T, dev)),
+                                     _addr("scales", scales, _F32, _THREE, dev), fmt,
+                                     None if q is None else _addr("q", q, _BF16, qs, dev), None if k is None else _addr("k", k, _BF16, kv, dev),
+                                     None if v is None else _addr("v", v, _BF16, kv, dev), _opt("q8", q8, _U8, qs, dev),
+                                     _opt("k8", k8, _U8, kv, dev), _opt("v8", v8, _U8, kv, dev),
+                                     _opt("amax_out", amax_out, _F32, _THREE, dev), st))
 
 
-def _rope_bwd_args(dq, dk, dv, qkv, rope, stream):
+def _rope_grads(dq, dk, dv, qkv, dev):
+    """What both forms of the gradient take first: addresses of the gradients and of what is saved, and the sizes."""
     if dq.dim() != 3:
         raise ValueError(f"dq: expects [T, Hq, d], got shape {tuple(dq.shape)}")
-    (T, Hq, d), Hkv = dq.shape, 0 if dk is None else dk.shape[1]
-    dev, st = _here(stream)
-    W = (Hq + 2 * Hkv) * d
-    kv = (T, Hkv, d)
+    T, Hq, d = dq.shape
+    Hkv = 0 if dk is None else dk.shape[1]
     if (dk is None) != (dv is None):
         raise ValueError("dk and dv come together")
-    saved = (None, 0) if qkv is None else _pitched("qkv", qkv, T, W, dev)
-    return dev, st, T, W, (_addr("dq", dq, _BF16, dq.shape, dev), _opt("dk", dk, _BF16, kv, dev), _opt("dv", dv, _BF16, kv, dev), *saved,
-                           T, Hq, Hkv, d, C.byref(_rope(*rope, T, dev)))
+    W, kv = (Hq + 2 * Hkv) * d, (T, Hkv, d)
+    at, pitch = (None, 0) if qkv is None else _pitched("qkv", qkv, T, W, dev)
+    return T, W, (_addr("dq", dq, _BF16, dq.shape, dev), _opt("dk", dk, _BF16, kv, dev), _opt("dv", dv, _BF16, kv, dev), at, pitch,
+                  T, Hq, Hkv, d)
 
 
 def fp8_rope_qkv_bwd(dq, dk, dv, qkv, mode, alpha, eps, cos, sin, positions, interleaved, dqkv, amax_out=None, stream=None):
     """Gradient of fp8_rope_qkv_fwd: dq [T, Hq, d], dk, dv [T, Hkv, d] BF16 (None without K and V) and the forward's qkv (None with
     QK_NONE) -> dqkv [T, (Hq + 2 Hkv) d] BF16 (rows may be strided); amax of dqkv optional."""
-    dev, st, T, W, ins = _rope_bwd_args(dq, dk, dv, qkv, (mode, alpha, eps, cos, sin, positions, interleaved), stream)
-    _check(load().fp8_rope_qkv_bwd(*ins, *_pitched("dqkv", dqkv, T, W, dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+    dev, st = _here(stream)
+    T, W, ins = _rope_grads(dq, dk, dv, qkv, dev)
+    _check(load().fp8_rope_qkv_bwd(*ins, C.byref(_rope(mode, alpha, eps, cos, sin, positions, interleaved, T, dev)),
+                                   *_pitched("dqkv", dqkv, T, W, dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
 
 
 def fp8_rope_qkv_bwd_q(dq, dk, dv, qkv, mode, alpha, eps, cos, sin, positions, interleaved, scale, fmt, dqkv8, dqkv=None, amax_out=None,
                        stream=None):
     """fp8_rope_qkv_bwd that writes the FP8 codes dqkv8 [T, (Hq + 2 Hkv) d] of its (BF16-rounded) result under the delayed `scale`
     (and the result itself where dqkv is given)."""
-    dev, st, T, W, ins = _rope_bwd_args(dq, dk, dv, qkv, (mode, alpha, eps, cos, sin, positions, interleaved), stream)
-    out = (None, 0) if dqkv is None else _pitched("dqkv", dqkv, T, W, dev)
-    _check(load().fp8_rope_qkv_bwd_q(*ins, _addr("scale", scale, _F32, _ONE, dev), fmt, *out, _addr("dqkv8", dqkv8, _U8, (T, W), dev),
+    dev, st = _here(stream)
+    T, W, ins = _rope_grads(dq, dk, dv, qkv, dev)
+    out, pitch = (None, 0) if dqkv is None else _pitched("dqkv", dqkv, T, W, dev)
+    _check(load().fp8_rope_qkv_bwd_q(*ins, C.byref(_rope(mode, alpha, eps, cos, sin, positions, interleaved, T, dev)),
+                                     _addr("scale", scale, _F32, _ONE, dev), fmt, out, pitch, _addr("dqkv8", dqkv8, _U8, (T, W), dev),
                                      _opt("amax_out", amax_out, _F32, _ONE, dev), st))
 
 
 class BlockNorm(C.Structure):
     _fields_ = [("post", C.c_int), ("gate", C.c_int), ("x_scale", C.c_float), ("y_scale", C.c_float), ("eps", C.c_float)]
-
-
-def _block_norm_ins(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, dev):
-    T, D = _matrix("x", x)
-    return (_addr("x", x, _BF16, x.shape, dev), _opt("y", y, _BF16, x.shape, dev), _opt("gate", gate, _BF16, x.shape, dev),
-            _opt("gamma_post", gamma_post, _F32, (D,), dev), _opt("gamma_pre", gamma_pre, _F32, (D,), dev), T, D,
-            C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, eps)))
 
 
 def fp8_block_norm_fwd(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, h, out, r_post=None, r_pre=None,
@@ -612,34 +616,54 @@ def fp8_block_norm_fwd(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_sca
     gate (GATE_LINEAR) or its sigmoid (GATE_SIGMOID); out = gamma_pre h / rms(h).  All [T, D] BF16 with gammas [D] FP32; y, gate, gamma_pre
     (then out) may be None; r_post, r_pre [T] FP32 for the backward pass; amax of out (of h without gamma_pre) optional."""
     dev, st = _here(stream)
-    s, T = x.shape, (x.shape[0],)
-    _check(load().fp8_block_norm_fwd(*_block_norm_ins(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, dev),
-                                     _opt("h", h, _BF16, s, dev), _opt("out", out, _BF16, s, dev), _opt("r_post", r_post, _F32, T, dev),
-                                     _opt("r_pre", r_pre, _F32, T, dev), _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+    T, D = s = _matrix("x", x)
+    cols, rows = (D,), (T,)
+    _check(load().fp8_block_norm_fwd(_addr("x", x, _BF16, s, dev),
+                                     None if y is None else _addr("y", y, _BF16, s, dev),
+                                     None if gate is None else _addr("gate", gate, _BF16, s, dev),
+                                     None if gamma_post is None else _addr("gamma_post", gamma_post, _F32, cols, dev),
+                                     None if gamma_pre is None else _addr("gamma_pre", gamma_pre, _F32, cols, dev), T, D,
+                                     C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, eps)),
+                                     None if h is None else _addr("h", h, _BF16, s, dev),
+                                     None if out is None else _addr("out", out, _BF16, s, dev),
+                                     None if r_post is None else _addr("r_post", r_post, _F32, rows, dev),
+                                     None if r_pre is None else _addr("r_pre", r_pre, _F32, rows, dev),
+                                     None if amax_out is None else _addr("amax_out", amax_out, _F32, _ONE, dev), st))
 
 
 def fp8_block_norm_fwd_q(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, scale, fmt, h, out, out8,
                          r_post=None, r_pre=None, amax_out=None, stream=None):
     """fp8_block_norm_fwd that also writes the FP8 codes out8 of its (BF16-rounded) result under the delayed `scale` (out may be None)."""
     dev, st = _here(stream)
-    s, T = x.shape, (x.shape[0],)
-    _check(load().fp8_block_norm_fwd_q(*_block_norm_ins(x, y, gate, gamma_post, gamma_pre, post, gate_mode, x_scale, y_scale, eps, dev),
-                                       _addr("scale", scale, _F32, _ONE, dev), fmt, _opt("h", h, _BF16, s, dev),
-                                       _opt("out", out, _BF16, s, dev), _addr("out8", out8, _U8, s, dev),
-                                       _opt("r_post", r_post, _F32, T, dev), _opt("r_pre", r_pre, _F32, T, dev),
-                                       _opt("amax_out", amax_out, _F32, _ONE, dev), st))
+    T, D = s = _matrix("x", x)
+    cols, rows = (D,), (T,)
+    _check(load().fp8_block_norm_fwd_q(_addr("x", x, _BF16, s, dev),
+                                       None if y is None else _addr("y", y, _BF16, s, dev),
+                                       None if gate is None else _addr("gate", gate, _BF16, s, dev),
+                                       None if gamma_post is None else _addr("gamma_post", gamma_post, _F32, cols, dev),
+                                       None if gamma_pre is None else _addr("gamma_pre", gamma_pre, _F32, cols, dev), T, D,
+                                       C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, eps)),
+                                       _addr("scale", scale, _F32, _ONE, dev), fmt,
+                                       None if h is None else _addr("h", h, _BF16, s, dev),
+                                       None if out is None else _addr("out", out, _BF16, s, dev), _addr("out8", out8, _U8, s, dev),
+                                       None if r_post is None else _addr("r_post", r_post, _F32, rows, dev),
+                                       None if r_pre is None else _addr("r_pre", r_pre, _F32, rows, dev),
+                                       None if amax_out is None else _addr("amax_out", amax_out, _F32, _ONE, dev), st))
 
 
 def fp8_block_norm_bwd_workspace_bytes(T, D) -> int:
     return load().fp8_block_norm_bwd_workspace_bytes(T, D)
 
 
-def _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dev):
-    s = T, D = _matrix("dx", dx)
-    return s, (_opt("dout", dout, _BF16, s, dev), _opt("dh", dh, _BF16, s, dev), _opt("h", h, _BF16, s, dev), _opt("y", y, _BF16, s, dev),
-               _opt("gate", gate, _BF16, s, dev), _opt("gamma_post", gamma_post, _F32, (D,), dev),
-               _opt("gamma_pre", gamma_pre, _F32, (D,), dev), _opt("r_post", r_post, _F32, (T,), dev),
-               _opt("r_pre", r_pre, _F32, (T,), dev), T, D, C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, 0.0)))
+def _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, T, D, s, dev):
+    cols, rows = (D,), (T,)
+    return (None if dout is None else _addr("dout", dout, _BF16, s, dev), None if dh is None else _addr("dh", dh, _BF16, s, dev),
+            None if h is None else _addr("h", h, _BF16, s, dev), None if y is None else _addr("y", y, _BF16, s, dev),
+            None if gate is None else _addr("gate", gate, _BF16, s, dev),
+            None if gamma_post is None else _addr("gamma_post", gamma_post, _F32, cols, dev),
+            None if gamma_pre is None else _addr("gamma_pre", gamma_pre, _F32, cols, dev),
+            None if r_post is None else _addr("r_post", r_post, _F32, rows, dev),
+            None if r_pre is None else _addr("r_pre", r_pre, _F32, rows, dev), T, D)
 
 
 def fp8_block_norm_bwd(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dy, dgate,
@@ -649,25 +673,31 @@ def fp8_block_norm_bwd(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pr
     with `accumulate`); None where there is nothing; amax of dy optional; ws: a uint8 CUDA tensor of
     fp8_block_norm_bwd_workspace_bytes(T, D)."""
     dev, st = _here(stream)
-    s, ins = _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dev)
+    T, D = s = _matrix("dx", dx)
     w, nw = _scratch(ws, dev)
-    _check(load().fp8_block_norm_bwd(*ins, _addr("dx", dx, _BF16, s, dev), _opt("dy", dy, _BF16, s, dev),
-                                     _opt("dgate", dgate, _BF16, s, dev), _opt("dgamma_post", dgamma_post, _F32, (s[1],), dev),
-                                     _opt("dgamma_pre", dgamma_pre, _F32, (s[1],), dev), bool(accumulate),
-                                     _opt("amax_out", amax_out, _F32, _ONE, dev), w, nw, st))
+    _check(load().fp8_block_norm_bwd(*_block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, T, D, s, dev),
+                                     C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, 0.0)), _addr("dx", dx, _BF16, s, dev),
+                                     None if dy is None else _addr("dy", dy, _BF16, s, dev),
+                                     None if dgate is None else _addr("dgate", dgate, _BF16, s, dev),
+                                     None if dgamma_post is None else _addr("dgamma_post", dgamma_post, _F32, (D,), dev),
+                                     None if dgamma_pre is None else _addr("dgamma_pre", dgamma_pre, _F32, (D,), dev), bool(accumulate),
+                                     None if amax_out is None else _addr("amax_out", amax_out, _F32, _ONE, dev), w, nw, st))
 
 
 def fp8_block_norm_bwd_q(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, scale, fmt, dx,
                          dy, dy8, dgate, dgamma_post, dgamma_pre, ws, accumulate=False, amax_out=None, stream=None):
     """fp8_block_norm_bwd that also writes the FP8 codes dy8 of the (BF16-rounded) dy under the delayed `scale` (dy may be None)."""
     dev, st = _here(stream)
-    s, ins = _block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, post, gate_mode, x_scale, y_scale, dx, dev)
+    T, D = s = _matrix("dx", dx)
     w, nw = _scratch(ws, dev)
-    _check(load().fp8_block_norm_bwd_q(*ins, _addr("scale", scale, _F32, _ONE, dev), fmt, _addr("dx", dx, _BF16, s, dev),
-                                       _opt("dy", dy, _BF16, s, dev), _addr("dy8", dy8, _U8, s, dev),
-                                       _opt("dgate", dgate, _BF16, s, dev), _opt("dgamma_post", dgamma_post, _F32, (s[1],), dev),
-                                       _opt("dgamma_pre", dgamma_pre, _F32, (s[1],), dev), bool(accumulate),
-                                       _opt("amax_out", amax_out, _F32, _ONE, dev), w, nw, st))
+    _check(load().fp8_block_norm_bwd_q(*_block_norm_grads(dout, dh, h, y, gate, gamma_post, gamma_pre, r_post, r_pre, T, D, s, dev),
+                                       C.byref(BlockNorm(post, gate_mode, x_scale, y_scale, 0.0)),
+                                       _addr("scale", scale, _F32, _ONE, dev), fmt, _addr("dx", dx, _BF16, s, dev),
+                                       None if dy is None else _addr("dy", dy, _BF16, s, dev), _addr("dy8", dy8, _U8, s, dev),
+                                       None if dgate is None else _addr("dgate", dgate, _BF16, s, dev),
+                                       None if dgamma_post is None else _addr("dgamma_post", dgamma_post, _F32, (D,), dev),
+                                       None if dgamma_pre is None else _addr("dgamma_pre", dgamma_pre, _F32, (D,), dev), bool(accumulate),
+                                       None if amax_out is None else _addr("amax_out", amax_out, _F32, _ONE, dev), w, nw, st))
 
 
 class AdamWItem(C.Structure):

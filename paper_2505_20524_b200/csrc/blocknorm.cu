@@ -210,6 +210,7 @@ struct BnBwd {
 // threads, the second from what the first gives.  Every tensor is read once and written once.
 // STAGES = 1: the ring holds one row, and a thread asks for the next row's piece as soon as it has read its own.
 __host__ __device__ constexpr int bn_bwd_tensors(bool pre, bool gate) { return 2 + 2 * pre + gate; }
+__host__ __device__ constexpr bool bn_bwd_gammas_near(int kg) { return kg <= 2; }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd p, int lanes_log2)
 {
@@ -247,6 +248,30 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
             for (int i = 0; i < NT; ++i)
                 if (!in[k] || (i == DH && !p.dh) || (i == Y && !p.need_y)) ring_put_zero(at + i * per_tensor + k * per_k);
     }
+    // the gammas lie behind the ring, [which][k][half][thread], where there is room, 1 for a missing one
+    constexpr bool NEAR = bn_bwd_gammas_near(KG);
+    if (NEAR) {
+#pragma unroll
+        for (int i = 0; i < (PRE ? 2 : 1); ++i)
+#pragma unroll
+            for (int k = 0; k < KG; ++k) {
+                uint64_t g[4] = {TWO_ONES, TWO_ONES, TWO_ONES, TWO_ONES};
+                const float *from = i ? p.gamma_pre : p.gamma_post;
+                if (in[k] && from) load4x2(from + 8 * (k * span + lane), g);
+                ring_put(ring_end + ((i * KG + k) * 2) * per_k, g[0], g[1]);
+                ring_put(ring_end + ((i * KG + k) * 2 + 1) * per_k, g[2], g[3]);
+            }
+    }
+    const auto gamma = [&](int i, int k, uint64_t (&g)[4]) {
+        if (NEAR) {
+            ring_get(ring_end + ((i * KG + k) * 2) * per_k, g[0], g[1]);
+            ring_get(ring_end + ((i * KG + k) * 2 + 1) * per_k, g[2], g[3]);
+        } else if (i || p.gamma_post) {
+            load4x2((i ? p.gamma_pre : p.gamma_post) + 8 * (k * span + lane), g);
+        } else {
+            g[0] = g[1] = g[2] = g[3] = TWO_ONES;
+        }
+    };
     const size_t pitch = (size_t)at_once * p.n8;
     size_t ahead = rows.begin + sub, at = ahead * p.n8 + lane, at_ahead = at;
     const auto ask = [&](uint32_t to, int i, const uint16_t *src) {
@@ -281,7 +306,7 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
     float m = 0.0f;
     uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage;
     int flip = 0;
-    const uint64_t a2 = both(p.a), b2 = both(p.b);
+    const uint64_t a2 = both(p.a);
     float rp32 = 1.0f, rq32 = 1.0f, rp_ahead = 1.0f, rq_ahead = 1.0f;      // lane l: the statistics of row l of a batch of 32
     if (rows.begin + (threadIdx.x & 31) < rows.end) {
         if (PRE) rp_ahead = __ldg(p.r_pre + rows.begin + (threadIdx.x & 31));
@@ -308,91 +333,86 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
             }
         }
         const float rp = __shfl_sync(0xffffffffu, rp32, in_batch + sub), rq = __shfl_sync(0xffffffffu, rq32, in_batch + sub);
-        float s1 = 0.0f;
-        if (PRE) {
+        uint64_t f[KG][4];
+        float c1 = 0.0f;
+        {
             uint64_t acc = 0ull;
 #pragma unroll
             for (int k = 0; k < KG; ++k) {
-                if (!live || !in[k]) continue;
-                uint64_t d[4], hh[4], g[4];
+                unpack4x2(ring_get(now + DH * per_tensor + k * per_k), f[k]);
+                if (!PRE || !live || !in[k]) continue;
+                uint64_t d[4], h[4], g[4];
                 unpack4x2(ring_get(now + DOUT * per_tensor + k * per_k), d);
-                unpack4x2(ring_get(now + H * per_tensor + k * per_k), hh);
-                load4x2(p.gamma_pre + 8 * (k * span + lane), g);
+                unpack4x2(ring_get(now + H * per_tensor + k * per_k), h);
+                gamma(1, k, g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    hh[e] = mul_f32x2(hh[e], both(rp));
-                    dgp[k][e] = fma_f32x2(d[e], hh[e], dgp[k][e]);
-                    acc = fma_f32x2(mul_f32x2(d[e], g[e]), hh[e], acc);
+                for (int e = 0; e < 4; ++e) {                 // e r_pre and sums of dout hh, e hh
+                    d[e] = mul_f32x2(d[e], both(rp));
+                    dgp[k][e] = fma_f32x2(d[e], h[e], dgp[k][e]);
+                    d[e] = mul_f32x2(d[e], g[e]);
+                    acc = fma_f32x2(d[e], h[e], acc);
+                    f[k][e] = add_f32x2(f[k][e], d[e]);
                 }
             }
-            s1 = row_sum<CTA, MAXT / 32>(add_halves(acc), lanes_log2, red[flip][0]) * inv_d;
+            if (PRE) c1 = row_sum<CTA, MAXT / 32>(add_halves(acc), lanes_log2, red[flip][0]) * -inv_d * rp * rp;
         }
         if (STAGES == 1) cp_async_wait<0>();
-        uint64_t f[KG][4], acc = 0ull;
+        uint64_t acc = 0ull;
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[k][e] = 0ull;
             if (!live || !in[k]) continue;
-            uint64_t D[4], y[4], gq[4];
-            unpack4x2(ring_get(now + DH * per_tensor + k * per_k), D);
+            uint64_t y[4], gq[4];
             if (PRE) {
-                uint64_t d[4], hh[4], g[4];
-                unpack4x2(ring_get(now + DOUT * per_tensor + k * per_k), d);
-                unpack4x2(ring_get(now + H * per_tensor + k * per_k), hh);
-                load4x2(p.gamma_pre + 8 * (k * span + lane), g);
+                uint64_t h[4];
+                unpack4x2(ring_get(now + H * per_tensor + k * per_k), h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    D[e] = fma_f32x2(both(rp), fma_f32x2(mul_f32x2(hh[e], both(rp)), both(-s1), mul_f32x2(d[e], g[e])), D[e]);
+                for (int e = 0; e < 4; ++e) f[k][e] = fma_f32x2(h[e], both(c1), f[k][e]);
             }
-            reinterpret_cast<uint4 *>(p.dx)[at + k * span] =
-                make_uint4(round2(mul_f32x2(a2, D[0])), round2(mul_f32x2(a2, D[1])), round2(mul_f32x2(a2, D[2])), round2(mul_f32x2(a2, D[3])));
+            reinterpret_cast<uint4 *>(p.dx)[at + k * span] = make_uint4(round2(mul_f32x2(a2, f[k][0])), round2(mul_f32x2(a2, f[k][1])),
+                                                                       round2(mul_f32x2(a2, f[k][2])), round2(mul_f32x2(a2, f[k][3])));
             unpack4x2(ring_get(now + Y * per_tensor + k * per_k), y);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                D[e] = mul_f32x2(b2, D[e]);
-                y[e] = mul_f32x2(y[e], both(rq));
-                gq[e] = TWO_ONES;
-            }
-            if (p.gamma_post) load4x2(p.gamma_post + 8 * (k * span + lane), gq);
+            gamma(0, k, gq);
             if (GATE) {
                 uint64_t g[4];
                 uint32_t o[4];
                 unpack4x2(ring_get(now + G * per_tensor + k * per_k), g);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    uint64_t slope = mul_f32x2(D[e], mul_f32x2(y[e], gq[e]));
+                    f[k][e] = mul_f32x2(f[k][e], both(p.b * rq));
+                    uint64_t slope = mul_f32x2(f[k][e], mul_f32x2(y[e], gq[e]));
                     if (p.sigmoid) {
                         uint64_t rest;
                         g[e] = sigmoid2(g[e], rest);
                         slope = mul_f32x2(slope, mul_f32x2(g[e], rest));
                     }
                     o[e] = round2(slope);
-                    D[e] = mul_f32x2(D[e], g[e]);
+                    f[k][e] = mul_f32x2(f[k][e], g[e]);
                 }
                 reinterpret_cast<uint4 *>(p.dgate)[at + k * span] = make_uint4(o[0], o[1], o[2], o[3]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[k][e] = mul_f32x2(f[k][e], both(p.b * rq));
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                dgq[k][e] = fma_f32x2(D[e], y[e], dgq[k][e]);
-                f[k][e] = mul_f32x2(D[e], gq[e]);
+            for (int e = 0; e < 4; ++e) {                     // dz r_post, f r_post and sums of dz yh, f yh
+                dgq[k][e] = fma_f32x2(f[k][e], y[e], dgq[k][e]);
+                f[k][e] = mul_f32x2(f[k][e], gq[e]);
                 acc = fma_f32x2(f[k][e], y[e], acc);
             }
         }
         if (STAGES == 1) fetch_first(ring);
-        float s2 = 0.0f;
-        if (p.rms) s2 = row_sum<CTA, MAXT / 32>(add_halves(acc), lanes_log2, red[flip][1]) * inv_d;
+        float c2 = 0.0f;
+        if (p.rms) c2 = row_sum<CTA, MAXT / 32>(add_halves(acc), lanes_log2, red[flip][1]) * -inv_d * rq * rq;
 #pragma unroll
         for (int k = 0; k < KG; ++k) {
             if (!live || !in[k]) continue;
-            uint32_t o[4];
             if (p.rms) {
                 uint64_t y[4];
                 unpack4x2(ring_get(now + Y * per_tensor + k * per_k), y);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    f[k][e] = mul_f32x2(both(rq), fma_f32x2(mul_f32x2(y[e], both(rq)), both(-s2), f[k][e]));
+                for (int e = 0; e < 4; ++e) f[k][e] = fma_f32x2(y[e], both(c2), f[k][e]);
             }
+            uint32_t o[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 o[e] = round2(f[k][e]);
@@ -476,8 +496,10 @@ static BnShape bn_fwd_shape(size_t T, size_t D)
     s.lanes_log2 = s.cta ? 0 : D > 256 ? 5 : log2_at_least(lanes);
     s.threads = s.cta ? (lanes + 31) & ~31u : 256;
     const size_t at_once = s.cta ? 1 : s.threads >> s.lanes_log2, want = (T + at_once - 1) / at_once;
-    const size_t most = 148 * (size_t)((kg == 2 ? 512 : D <= 8192 ? 256 : 512) / s.threads);
+    const size_t most = 148 * (size_t)((kg == 2 ? 768 : D <= 8192 ? 256 : 512) / s.threads);
     s.grid = (unsigned)(want < most ? want : most);
+    // up to 16 CTAs are one cluster, which sets the amax to zero itself; a second row per unit is less than a launch for that
+    if (s.grid > 16 && s.grid <= 32) s.grid = 16;
     return s;
 }
 // Backward: lanes of a warp with one group of columns each up to 128 columns, a warp with one up to 256 and two up to 512, then
@@ -519,16 +541,16 @@ template <int NT, bool PRE>
 static int bn_fwd_run(const BnFwd &p, size_t D, cudaStream_t st)
 {
     const BnShape s = bn_fwd_shape(p.T, D);
-    if (D <= 256) return bn_fwd_launch<2, ROW_LANES, NT, PRE, 256, 2>(p, s, st);
-    if (D <= 512) return bn_fwd_launch<2, ROW_WARP, NT, PRE, 256, 2>(p, s, st);
-    if (D <= 4096) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 256, 2>(p, s, st);
+    if (D <= 256) return bn_fwd_launch<2, ROW_LANES, NT, PRE, 256, 3>(p, s, st);
+    if (D <= 512) return bn_fwd_launch<2, ROW_WARP, NT, PRE, 256, 3>(p, s, st);
+    if (D <= 4096) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 256, 3>(p, s, st);
     if (D <= 8192) return bn_fwd_launch<4, ROW_CTA, NT, PRE, 256, 1>(p, s, st);
     return bn_fwd_launch<4, ROW_CTA, NT, PRE, 512, 1>(p, s, st);
 }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
 static int bn_bwd_launch(const BnBwd &p, const BnShape &s, cudaStream_t st)
 {
-    constexpr size_t per_thread = STAGES * bn_bwd_tensors(PRE, GATE) * KG * 16;
+    constexpr size_t per_thread = (STAGES * bn_bwd_tensors(PRE, GATE) + (bn_bwd_gammas_near(KG) ? PRE ? 4 : 2 : 0)) * KG * 16;
     return bn_launch<block_norm_bwd_kernel<KG, UNIT, PRE, GATE, STAGES, MAXT, MINB>>(p, s, per_thread * s.threads, per_thread * MAXT, st);
 }
 template <bool PRE, bool GATE>

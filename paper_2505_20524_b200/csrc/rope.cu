@@ -204,7 +204,7 @@ __device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int
 }
 
 // A head is on 2^lanes_log2 neighbouring lanes, 16 elements each: below `rot` lane j holds elements [8 j, 8 j + 8) and the same
-// of the rotated part's second half, so that both kinds of partners are in one lane; behind it 16 in a row, which pass through.
+// of the rotated part's second half, so that both kinds of partners are in one lane; behind it likewise, which passes through.
 // A group of lanes takes up to ROPE_HEADS heads of one tensor of one token with the token's angles in registers.  Persistent: a
 // group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
 // bind: every element is read once and written once.
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
     if (part > 1) piece -= p.chunks[1];
     const int h0 = piece * ROPE_HEADS, n_heads = p.heads[part], here = min(ROPE_HEADS, n_heads - h0), d = p.d;
     const int before = (part > 0 ? p.heads[0] : 0) + (part > 1 ? p.heads[1] : 0) + h0;       // heads of the row in front
-    const int lo = turns ? 8 * j : p.rot + 16 * (j - turned), hi = turns ? p.rot / 2 + 8 * j : lo + 8, other = hi - lo;
+    const int lo = turns ? 8 * j : p.rot + 8 * (j - turned), other = (turns ? p.rot : d - p.rot) / 2;
     const size_t in_row = (size_t)before * d + lo, in_part = (size_t)h0 * d + lo;
     const size_t step = (size_t)ctas * p.tokens;
     const size_t part_pitch = (size_t)n_heads * d, row_pitch = (size_t)(p.heads[0] + p.heads[1] + p.heads[2]) * d;
