@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -706,6 +707,9 @@ class AdamWItem(C.Structure):
                 ("n", C.c_size_t), ("weight_decay", C.c_float), ("g_is_fp32", C.c_int), ("state_bits", C.c_int), ("fmt", C.c_int)]
 
 
+_FLOAT_BITS = struct.Struct("<f").pack
+
+
 class AdamWItems:
     """The tensors of a model as fp8_adamw takes them: built once, used every step (it keeps the tensors alive; they have to stay
     where they are)."""
@@ -720,31 +724,41 @@ class AdamWItems:
             raise ValueError("expects CUDA tensors")
         if params8 is not None and q_scales is None:
             raise ValueError("FP8 copies need their scales")
-        self.tensors = [None if x is None else list(x) for x in lists] + [q_scales, amaxes]
+        none = [None] * n
+        p_, g_, m_, v_, decays, me_, ve_, p16_, p8_ = self.tensors = [none if x is None else list(x) for x in lists]
+        self.others = (q_scales, amaxes)
         scales, maxima = _opt("q_scales", q_scales, _F32, (n,), dev), _opt("amaxes", amaxes, _F32, (n,), dev)
-        self.array = (AdamWItem * n)()
-        for i in range(n):
-            p, g, m, v = params[i], grads[i], ms[i], vs[i]
-            shape, numel, eight = p.shape, p.numel(), m.dtype is _U8
-            blocks, state = (-(-numel // 128),), _U8 if eight else _F32
-            if eight and (m_exps is None or v_exps is None):
-                raise ValueError(f"ms[{i}]: moments in 8 bits need their exponents")
-            at = lambda name, t, dt, sh: _addr(f"{name}[{i}]", t, dt, sh, dev)  # noqa: E731
-            it = self.array[i]
-            it.p, it.g = at("params", p, _F32, shape), at("grads", g, _FLOATS, shape)
-            it.m, it.v = at("ms", m, state, shape), at("vs", v, state, shape)
+        words, written = [], []
+        for i, (p, g, m, v, me, ve, p16, p8) in enumerate(zip(p_, g_, m_, v_, me_, ve_, p16_, p8_)):
+            shape, numel, gt = p.shape, p.numel(), g.dtype
+            eight = m.dtype is _U8
+            state = _U8 if eight else _F32
+            if not (p.dtype is _F32 and (gt is _BF16 or gt is _F32) and m.dtype is state and v.dtype is state and g.shape == shape
+                    and m.shape == shape and v.shape == shape and p.is_contiguous() and g.is_contiguous() and m.is_contiguous()
+                    and v.is_contiguous() and p.get_device() == dev and g.get_device() == dev and m.get_device() == dev
+                    and v.get_device() == dev):              # _addr's checks written out: a list of hundreds is made at once
+                _addr(f"params[{i}]", p, _F32, shape, dev)
+                _addr(f"grads[{i}]", g, _FLOATS, shape, dev)
+                _addr(f"ms[{i}]", m, state, shape, dev)
+                _addr(f"vs[{i}]", v, state, shape, dev)
+            out = [p.data_ptr(), m.data_ptr(), v.data_ptr(), 0, 0, 0, 0]
             if eight:
-                it.m_exp, it.v_exp = at("m_exps", m_exps[i], _U8, blocks), at("v_exps", v_exps[i], _U8, blocks)
-            if params16 is not None and params16[i] is not None:
-                it.p_bf16 = at("params16", params16[i], _BF16, shape)
-            if params8 is not None and params8[i] is not None:
-                it.p8, it.q_scale = at("params8", params8[i], _U8, shape), scales + 4 * i
-            if maxima is not None:
-                it.amax = maxima + 4 * i
-            it.n, it.weight_decay, it.g_is_fp32, it.state_bits, it.fmt = numel, decays[i], g.dtype is _F32, 8 if eight else 32, fmt
-        written = [a for it in self.array if it.n for a in (it.p, it.m, it.v, it.m_exp, it.v_exp, it.p_bf16, it.p8) if a]
+                if me is None or ve is None:
+                    raise ValueError(f"ms[{i}]: moments in 8 bits need their exponents")
+                blocks = (-(-numel // 128),)
+                out[3], out[4] = _addr(f"m_exps[{i}]", me, _U8, blocks, dev), _addr(f"v_exps[{i}]", ve, _U8, blocks, dev)
+            if p16 is not None:
+                out[5] = _addr(f"params16[{i}]", p16, _BF16, shape, dev)
+            if p8 is not None:
+                out[6] = _addr(f"params8[{i}]", p8, _U8, shape, dev)
+            if numel:
+                written += out
+            words += (out[0], g.data_ptr(), *out[1:], 0 if p8 is None else scales + 4 * i, 0 if maxima is None else maxima + 4 * i, numel,
+                      int.from_bytes(_FLOAT_BITS(decays[i]), "little") | (gt is _F32) << 32, (8 if eight else 32) | fmt << 32)
+        written = [a for a in written if a]
         if len(set(written)) < len(written):
             raise ValueError("a tensor that is written stands in the lists twice")     # tied weights would take two steps at once
+        self.array = (AdamWItem * n).from_buffer(array.array("Q", words))
 
     def __len__(self):
         return len(self.array)

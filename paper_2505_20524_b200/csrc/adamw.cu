@@ -11,8 +11,9 @@ namespace fp8dpa {
 constexpr int AW_THREADS = 256;
 constexpr int AW_PER_THREAD = 16;
 constexpr int AW_CHUNK = AW_THREADS * AW_PER_THREAD;
-constexpr int AW_ITEMS = 256;                             // tensors per launch (27 KB of kernel parameters)
-constexpr int AW_BUCKETS = 1024;
+constexpr int AW_ITEMS = 304;                             // tensors per launch (31 KB of kernel parameters)
+constexpr int AW_BUCKETS = 512;
+constexpr int AW_MAXIMA = 512;                            // amaxes that one launch sets to zero
 constexpr int AW_BLOCK = 128;                             // values that share a scale in the 8-bit moments
 
 struct AdamTable {
@@ -24,7 +25,7 @@ struct AdamTable {
     uint8_t *p8[AW_ITEMS];
     const float *q_scale[AW_ITEMS];
     unsigned int *amax[AW_ITEMS];
-    unsigned long long n[AW_ITEMS], done[AW_ITEMS];       // elements here, and of the tensor in front of them
+    unsigned long long n[AW_ITEMS];
     unsigned first[AW_ITEMS + 1];                         // the tensor's first chunk
     float decay[AW_ITEMS];
     unsigned short start[AW_BUCKETS];                     // the tensor that holds chunk j << bucket_log2
@@ -49,15 +50,19 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)
     return x ^ (x >> 16);
 }
 
-__global__ void __launch_bounds__(AW_ITEMS) adamw_begin_kernel(const __grid_constant__ AdamTable t, AdamStep *out, const float *lr,
-                                                              int *step, double log_beta1, double log_beta2, const float *norm,
-                                                              float max_norm, uint32_t seed_lo, uint32_t seed_hi, int first_launch)
+struct AdamMaxima {
+    unsigned int *amax[AW_MAXIMA];
+    int n;
+};
+__global__ void __launch_bounds__(AW_MAXIMA) adamw_begin_kernel(const __grid_constant__ AdamMaxima maxima, AdamStep *out, const float *lr,
+                                                                int *step, double log_beta1, double log_beta2, const float *norm,
+                                                                float max_norm, uint32_t seed_lo, uint32_t seed_hi)
 {
     cudaTriggerProgrammaticLaunchCompletion();
     const float n = norm ? *norm : 0.0f;
     const bool skip = !(n - n == 0.0f);                   // infinite or NaN
-    if (!skip && threadIdx.x < t.items && t.done[threadIdx.x] == 0 && t.amax[threadIdx.x]) *t.amax[threadIdx.x] = 0u;
-    if (threadIdx.x == 0 && first_launch) {
+    if (!skip && threadIdx.x < maxima.n) *maxima.amax[threadIdx.x] = 0u;
+    if (threadIdx.x == 0 && out) {
         AdamStep s;
         const int now = *step + 1;
         s.skip = skip;
@@ -334,8 +339,7 @@ __device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned 
         }
         store8(t.p[k] + i, some, x.w);
         if constexpr (EIGHT) {
-            const unsigned long long at = t.done[k] + i;
-            const uint32_t key = mix32(mix32(s.key + (uint32_t)(t.number + k)) + (uint32_t)(at >> 32)) + (uint32_t)at;
+            const uint32_t key = mix32(mix32(s.key + (uint32_t)(t.number + k)) + (uint32_t)(i >> 32)) + (uint32_t)i;
             float top_m = 0.0f, top_r = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -427,43 +431,32 @@ static int adamw_check_items(const fp8_adamw_item *items, int n_items)
     return FP8_OK;
 }
 
-// The next launch's table from item *item on; chunk numbers stay below 2^30, one tensor may be cut for that.
-static void adamw_fill(AdamTable &t, const fp8_adamw_item *items, int n_items, int &item, size_t &done)
+// The next launch's table from `item` on, up to 2^30 chunks (a tensor has 2^28 at most).
+static void adamw_fill(AdamTable &t, const fp8_adamw_item *items, int n_items, int &item)
 {
-    const size_t most = (size_t)1 << 30;
     t.items = 0;
     t.chunks = 0;
     t.number = item;
-    while (item < n_items && t.items < AW_ITEMS && t.chunks < most) {
+    for (; item < n_items && t.items < AW_ITEMS; ++item) {
         const fp8_adamw_item &it = items[item];
+        const size_t chunks = (it.n + AW_CHUNK - 1) / AW_CHUNK;
+        if (t.chunks + chunks > (size_t)1 << 30) break;
         const int k = t.items++;                              // empty ones too: the number in the list is part of the key
-        size_t n = it.n - done, chunks = (n + AW_CHUNK - 1) / AW_CHUNK;
-        if (chunks > most - t.chunks) {
-            chunks = most - t.chunks;
-            n = chunks * AW_CHUNK;
-        }
-        const bool eight = it.state_bits == 8;
-        t.p[k] = it.p + done;
-        t.g[k] = static_cast<const char *>(it.g) + done * (it.g_is_fp32 ? 4 : 2);
-        t.m[k] = static_cast<char *>(it.m) + done * (eight ? 1 : 4);
-        t.v[k] = static_cast<char *>(it.v) + done * (eight ? 1 : 4);
-        t.m_exp[k] = it.m_exp + (eight ? done / AW_BLOCK : 0);
-        t.v_exp[k] = it.v_exp + (eight ? done / AW_BLOCK : 0);
-        t.p16[k] = it.p_bf16 ? static_cast<uint16_t *>(it.p_bf16) + done : nullptr;
-        t.p8[k] = it.p8 ? it.p8 + done : nullptr;
+        t.p[k] = it.p;
+        t.g[k] = it.g;
+        t.m[k] = it.m;
+        t.v[k] = it.v;
+        t.m_exp[k] = it.m_exp;
+        t.v_exp[k] = it.v_exp;
+        t.p16[k] = static_cast<uint16_t *>(it.p_bf16);
+        t.p8[k] = it.p8;
         t.q_scale[k] = it.q_scale;
         t.amax[k] = reinterpret_cast<unsigned int *>(it.amax);
-        t.n[k] = n;
-        t.done[k] = done;
+        t.n[k] = it.n;
         t.first[k] = t.chunks;
         t.decay[k] = it.weight_decay;
-        t.types[k] = (it.g_is_fp32 ? 1 : 0) | (eight ? 2 : 0) | (it.fmt == FP8_E5M2 ? 4 : 0);
+        t.types[k] = (it.g_is_fp32 ? 1 : 0) | (it.state_bits == 8 ? 2 : 0) | (it.fmt == FP8_E5M2 ? 4 : 0);
         t.chunks += (unsigned)chunks;
-        done += n;
-        if (done == it.n) {
-            ++item;
-            done = 0;
-        }
     }
     t.first[t.items] = t.chunks;
     t.bucket_log2 = 0;
@@ -516,15 +509,20 @@ extern "C" int fp8_adamw(const fp8_adamw_item *items, int n_items, const float *
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     AdamStep *s = static_cast<AdamStep *>(ws);
     const AdamRates a = {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps};
-    AdamTable t;
-    int item = 0, first = 1;
-    size_t done = 0;
-    while (item < n_items) {
-        adamw_fill(t, items, n_items, item, done);
-        adamw_begin_kernel<<<1, AW_ITEMS, 0, st>>>(t, s, lr, step, log(beta1), log(beta2), norm, max_norm, (uint32_t)seed,
-                                                   (uint32_t)(seed >> 32), first);
+    AdamMaxima maxima;
+    int at = 0;
+    do {                                                      // the step's numbers, and zeros where maxima will be
+        const bool first = at == 0;
+        maxima.n = 0;
+        for (; at < n_items && maxima.n < AW_MAXIMA; ++at)
+            if (items[at].amax) maxima.amax[maxima.n++] = reinterpret_cast<unsigned int *>(items[at].amax);
+        adamw_begin_kernel<<<1, AW_MAXIMA, 0, st>>>(maxima, first ? s : nullptr, lr, step, log(beta1), log(beta2), norm, max_norm,
+                                                    (uint32_t)seed, (uint32_t)(seed >> 32));
         FP8_CUDA_CHECK(cudaGetLastError());
-        first = 0;
+    } while (at < n_items);
+    AdamTable t;
+    for (int item = 0; item < n_items;) {
+        adamw_fill(t, items, n_items, item);
         if (t.chunks == 0) continue;
         rc = launch_early(adamw_kernel, t.chunks, AW_THREADS, 0, st, t, static_cast<const AdamStep *>(s), a);
         if (rc != FP8_OK) return rc;

@@ -490,13 +490,13 @@ struct BnShape {
 // four above.
 static BnShape bn_fwd_shape(size_t T, size_t D)
 {
-    const unsigned kg = D <= 4096 ? 2 : 4, lanes = ((unsigned)(D / 8) + kg - 1) / kg;
+    const unsigned kg = D <= 8192 ? 2 : 4, lanes = ((unsigned)(D / 8) + kg - 1) / kg;
     BnShape s;
     s.cta = D > 512;
     s.lanes_log2 = s.cta ? 0 : D > 256 ? 5 : log2_at_least(lanes);
     s.threads = s.cta ? (lanes + 31) & ~31u : 256;
     const size_t at_once = s.cta ? 1 : s.threads >> s.lanes_log2, want = (T + at_once - 1) / at_once;
-    const size_t most = 148 * (size_t)((kg == 2 ? 768 : D <= 8192 ? 256 : 512) / s.threads);
+    const size_t most = 148 * (size_t)((D <= 4096 ? 768 : 512) / s.threads);
     s.grid = (unsigned)(want < most ? want : most);
     // up to 16 CTAs are one cluster, which sets the amax to zero itself; a second row per unit is less than a launch for that
     if (s.grid > 16 && s.grid <= 32) s.grid = 16;
@@ -511,10 +511,10 @@ static BnShape bn_bwd_shape(size_t T, size_t D)
     BnShape s;
     s.cta = D > 512;
     s.lanes_log2 = s.cta || D > 128 ? 5 : log2_at_least(n8);
-    const unsigned kg = D <= 8192 ? 2 : 4;
+    const unsigned kg = D <= 2048 ? 1 : D <= 8192 ? 2 : 4;
     s.threads = s.cta ? ((n8 + kg - 1) / kg + 31) & ~31u : 256;
     const size_t at_once = s.cta ? 8 : (size_t)8 << (5 - s.lanes_log2);
-    const size_t most = 148 * (size_t)(s.cta ? 512 / s.threads : 2);
+    const size_t most = 148 * (size_t)(s.cta ? (kg == 1 ? 768 : 512) / s.threads : 2);
     size_t want = (T + at_once - 1) / at_once;
     if (s.cta && want < 148) want = T < 148 ? T : 148;
     s.grid = (unsigned)(want < most ? want : most);
@@ -544,7 +544,7 @@ static int bn_fwd_run(const BnFwd &p, size_t D, cudaStream_t st)
     if (D <= 256) return bn_fwd_launch<2, ROW_LANES, NT, PRE, 256, 3>(p, s, st);
     if (D <= 512) return bn_fwd_launch<2, ROW_WARP, NT, PRE, 256, 3>(p, s, st);
     if (D <= 4096) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 256, 3>(p, s, st);
-    if (D <= 8192) return bn_fwd_launch<4, ROW_CTA, NT, PRE, 256, 1>(p, s, st);
+    if (D <= 8192) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 512, 1>(p, s, st);
     return bn_fwd_launch<4, ROW_CTA, NT, PRE, 512, 1>(p, s, st);
 }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
@@ -559,6 +559,7 @@ static int bn_bwd_run(const BnBwd &p, const BnShape &s, size_t D, cudaStream_t s
     if (D <= 128) return bn_bwd_launch<1, ROW_LANES, PRE, GATE, 2, 256, 2>(p, s, st);
     if (D <= 256) return bn_bwd_launch<1, ROW_WARP, PRE, GATE, 2, 256, 2>(p, s, st);
     if (D <= 512) return bn_bwd_launch<2, ROW_WARP, PRE, GATE, 2, 256, 2>(p, s, st);
+    if (D <= 2048) return bn_bwd_launch<1, ROW_CTA, PRE, GATE, 2, 256, 3>(p, s, st);
     if (D <= 4096) return bn_bwd_launch<2, ROW_CTA, PRE, GATE, 2, 256, 2>(p, s, st);
     if (D <= 8192) return bn_bwd_launch<2, ROW_CTA, PRE, GATE, 2, 512, 1>(p, s, st);
     return bn_bwd_launch<4, ROW_CTA, PRE, GATE, 1, 512, 1>(p, s, st);
