@@ -44,10 +44,14 @@ struct AdamStep {
 
 // 32-bit integers to 32-bit integers that look random: xor-shifts and products with odd numbers (2^32 times the fractions of the
 // golden ratio and of the square root of 2).  Every output bit changes with a probability within 0.011 of 1/2 with each input bit.
-__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)
+__device__ __forceinline__ uint32_t mix32_products(uint32_t x)
 {
     x = (x ^ (x >> 16)) * 0x9E3779B9u;
-    x = (x ^ (x >> 15)) * 0x6A09E667u;
+    return (x ^ (x >> 15)) * 0x6A09E667u;
+}
+__device__ __forceinline__ uint32_t mix32(uint32_t x)
+{
+    x = mix32_products(x);
     return x ^ (x >> 16);
 }
 
@@ -206,15 +210,18 @@ __device__ __forceinline__ uint32_t exponent_of(float most) { return (__float_as
 // an addition below bit 20: away from zero with the probability of the part that is cut off (16 bits of it), so that a change far
 // below a step is not lost over many steps but comes through on average.  ROOT: not negative, and values above zero get the
 // smallest code at least (a root of zero in the update's denominator would let it through unchecked).
-template <bool ROOT>
+// FAR: blocks whose power of two and 2^-120 do not fit into one factor.
+constexpr uint32_t AW_FAR = 134;
+template <bool ROOT, bool FAR>
 __device__ __forceinline__ uint2 encode8(const uint64_t (&f)[4], const uint32_t (&bits)[8], uint32_t exponent)
 {
-    const uint64_t inv = both(__uint_as_float((254u - exponent) << 23)), down = both(7.5231638e-37f);       // 2^-120
+    const uint64_t inv = both(__uint_as_float((FAR ? 254u - exponent : 134u - exponent) << 23)), down = both(7.5231638e-37f);   // 2^-120
     uint32_t z[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const uint64_t y = mul_f32x2(mul_f32x2(f[e >> 1], inv), down);
-        const uint32_t cut = ROOT ? bits[e] >> 16 : bits[e] & 0xFFFFu;
+        uint64_t y = mul_f32x2(f[e >> 1], inv);
+        if (FAR) y = mul_f32x2(y, down);
+        const uint32_t cut = ROOT ? bits[e] >> 16 : (bits[e] ^ bits[e] >> 16) & 0xFFFFu;       // the halves of mix32's result
         z[e] = half_bits(y, e & 1) + (cut << 4);
         if (ROOT) z[e] = max(z[e], min(half_bits(f[e >> 1], e & 1), 0x100000u)) << 4;
         else z[e] = ((z[e] << 4) & 0x7FFFFFFFu) | (z[e] & 0x80000000u);
@@ -225,17 +232,17 @@ __device__ __forceinline__ uint2 encode8(const uint64_t (&f)[4], const uint32_t 
         w[i] = __byte_perm(__byte_perm(z[4 * i], z[4 * i + 1], 0x0073), __byte_perm(z[4 * i + 2], z[4 * i + 3], 0x0073), 0x5410);
     return make_uint2(w[0], w[1]);
 }
-// The same for a block with values that are not finite: they get the code of NaN, the others are scaled by the largest of theirs.
+// The same for any block.  Values that are not finite get the code of NaN, the others are scaled by the largest of theirs.
 // By all lanes of a warp together.
 template <bool ROOT>
-__device__ __noinline__ uint2 encode8_broken(uint64_t f0, uint64_t f1, uint64_t f2, uint64_t f3, uint32_t key, uint32_t &exponent)
+__device__ __noinline__ uint2 encode8_any(uint64_t f0, uint64_t f1, uint64_t f2, uint64_t f3, uint32_t key, uint32_t &exponent)
 {
     uint64_t f[4] = {f0, f1, f2, f3};
     uint32_t bits[8], broken = 0u;
     float most = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        bits[e] = mix32(key + e);
+        bits[e] = mix32_products(key + e);
         const float v = fabsf(__uint_as_float(half_bits(f[e >> 1], e & 1)));
         if (v < INFINITY) most = fmaxf(most, v);
         else broken |= 1u << e;
@@ -249,7 +256,7 @@ __device__ __noinline__ uint2 encode8_broken(uint64_t f0, uint64_t f1, uint64_t 
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
     exponent = (uint32_t)max((int)exponent_of(most) - 8, 1);
-    uint2 c = encode8<ROOT>(f, bits, exponent);
+    uint2 c = encode8<ROOT, true>(f, bits, exponent);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         if (broken >> e & 1u) (e < 4 ? c.x : c.y) |= 0x7Fu << (8 * (e & 3));
@@ -308,7 +315,7 @@ __device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned 
         if (!EIGHT && u > 0) x.load(t, k, i, some);
         uint64_t m[4], v[4], r[4], w[4];
         if constexpr (EIGHT) {
-            decode8(x.mc, __uint_as_float(x.me << 23), m);
+            decode8(x.mc, __fmul_rn(a.beta1, __uint_as_float(x.me << 23)), m);       // beta1 m: a power of two moves no rounding
             decode8(x.vc, __uint_as_float(x.ve << 23), v);
         }
 #pragma unroll
@@ -320,7 +327,7 @@ __device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned 
                 v[e] = pack_f32x2(x.v[2 * e], x.v[2 * e + 1]);
             }
             const uint64_t g = mul_f32x2(pack_f32x2(x.g[2 * e], x.g[2 * e + 1]), both(s.factor));
-            const uint64_t rest = mul_f32x2(both(a.beta1), m[e]), new_m = mul_f32x2(both(a.rest1), g);
+            const uint64_t rest = EIGHT ? m[e] : mul_f32x2(both(a.beta1), m[e]), new_m = mul_f32x2(both(a.rest1), g);
             const uint64_t old = mul_f32x2(both(a.beta2), v[e]), more = mul_f32x2(mul_f32x2(both(a.rest2), g), g);
             if constexpr (EIGHT) {
                 m[e] = add_ftz2(rest, new_m);                // below the normal numbers: 0
@@ -356,15 +363,15 @@ __device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned 
             for (int off = 8; off > 0; off >>= 1) up = __vmaxu2(up, __shfl_xor_sync(0xffffffffu, up, off));   // the block's 16 lanes
             uint32_t me = (uint32_t)max((int)(up >> 16) - 8, 1), ve = (uint32_t)max((int)(up & 0xFFFFu) - 8, 1);
             uint2 mc, vc;
-            if (__any_sync(0xffffffffu, max(up >> 16, up & 0xFFFFu) >= 255u)) {
-                mc = encode8_broken<false>(m[0], m[1], m[2], m[3], key, me);
-                vc = encode8_broken<true>(r[0], r[1], r[2], r[3], key, ve);
+            if (__any_sync(0xffffffffu, max(me, ve) >= AW_FAR)) {
+                mc = encode8_any<false>(m[0], m[1], m[2], m[3], key, me);
+                vc = encode8_any<true>(r[0], r[1], r[2], r[3], key, ve);
             } else {
                 uint32_t bits[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) bits[e] = mix32(key + e);
-                mc = encode8<false>(m, bits, me);
-                vc = encode8<true>(r, bits, ve);
+                for (int e = 0; e < 8; ++e) bits[e] = mix32_products(key + e);
+                mc = encode8<false, false>(m, bits, me);
+                vc = encode8<true, false>(r, bits, ve);
             }
             store8(static_cast<uint8_t *>(t.m[k]) + i, some, mc);
             store8(static_cast<uint8_t *>(t.v[k]) + i, some, vc);
