@@ -210,7 +210,7 @@ struct BnBwd {
 // threads, the second from what the first gives.  Every tensor is read once and written once.
 // STAGES = 1: the ring holds one row, and a thread asks for the next row's piece as soon as it has read its own.
 __host__ __device__ constexpr int bn_bwd_tensors(bool pre, bool gate) { return 2 + 2 * pre + gate; }
-__host__ __device__ constexpr bool bn_bwd_gammas_near(int kg) { return kg <= 2; }
+__host__ __device__ constexpr int bn_bwd_near(int kg, bool pre) { return kg <= 3 && pre ? 2 : 1; }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd p, int lanes_log2)
 {
@@ -248,24 +248,22 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
             for (int i = 0; i < NT; ++i)
                 if (!in[k] || (i == DH && !p.dh) || (i == Y && !p.need_y)) ring_put_zero(at + i * per_tensor + k * per_k);
     }
-    // the gammas lie behind the ring, [which][k][half][thread], where there is room, 1 for a missing one
-    constexpr bool NEAR = bn_bwd_gammas_near(KG);
-    if (NEAR) {
+    // gammas behind the ring, [which][k][half][thread], as many as there is room for; 1 for a missing one
+    constexpr int NEAR = bn_bwd_near(KG, PRE), FIRST = KG > 3 && PRE ? 1 : 0;
 #pragma unroll
-        for (int i = 0; i < (PRE ? 2 : 1); ++i)
+    for (int i = FIRST; i < FIRST + NEAR; ++i)
 #pragma unroll
-            for (int k = 0; k < KG; ++k) {
-                uint64_t g[4] = {TWO_ONES, TWO_ONES, TWO_ONES, TWO_ONES};
-                const float *from = i ? p.gamma_pre : p.gamma_post;
-                if (in[k] && from) load4x2(from + 8 * (k * span + lane), g);
-                ring_put(ring_end + ((i * KG + k) * 2) * per_k, g[0], g[1]);
-                ring_put(ring_end + ((i * KG + k) * 2 + 1) * per_k, g[2], g[3]);
-            }
-    }
+        for (int k = 0; k < KG; ++k) {
+            uint64_t g[4] = {TWO_ONES, TWO_ONES, TWO_ONES, TWO_ONES};
+            const float *from = i ? p.gamma_pre : p.gamma_post;
+            if (in[k] && from) load4x2(from + 8 * (k * span + lane), g);
+            ring_put(ring_end + (((i - FIRST) * KG + k) * 2) * per_k, g[0], g[1]);
+            ring_put(ring_end + (((i - FIRST) * KG + k) * 2 + 1) * per_k, g[2], g[3]);
+        }
     const auto gamma = [&](int i, int k, uint64_t (&g)[4]) {
-        if (NEAR) {
-            ring_get(ring_end + ((i * KG + k) * 2) * per_k, g[0], g[1]);
-            ring_get(ring_end + ((i * KG + k) * 2 + 1) * per_k, g[2], g[3]);
+        if (i >= FIRST && i < FIRST + NEAR) {
+            ring_get(ring_end + (((i - FIRST) * KG + k) * 2) * per_k, g[0], g[1]);
+            ring_get(ring_end + (((i - FIRST) * KG + k) * 2 + 1) * per_k, g[2], g[3]);
         } else if (i || p.gamma_post) {
             load4x2((i ? p.gamma_pre : p.gamma_post) + 8 * (k * span + lane), g);
         } else {
@@ -511,7 +509,7 @@ static BnShape bn_bwd_shape(size_t T, size_t D)
     BnShape s;
     s.cta = D > 512;
     s.lanes_log2 = s.cta || D > 128 ? 5 : log2_at_least(n8);
-    const unsigned kg = D <= 2048 ? 1 : D <= 8192 ? 2 : 4;
+    const unsigned kg = D <= 2048 ? 1 : D <= 8192 ? 2 : D <= 12288 ? 3 : 4;
     s.threads = s.cta ? ((n8 + kg - 1) / kg + 31) & ~31u : 256;
     const size_t at_once = s.cta ? 8 : (size_t)8 << (5 - s.lanes_log2);
     const size_t most = 148 * (size_t)(s.cta ? (kg == 1 ? 768 : 512) / s.threads : 2);
@@ -550,7 +548,7 @@ static int bn_fwd_run(const BnFwd &p, size_t D, cudaStream_t st)
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
 static int bn_bwd_launch(const BnBwd &p, const BnShape &s, cudaStream_t st)
 {
-    constexpr size_t per_thread = (STAGES * bn_bwd_tensors(PRE, GATE) + (bn_bwd_gammas_near(KG) ? PRE ? 4 : 2 : 0)) * KG * 16;
+    constexpr size_t per_thread = (STAGES * bn_bwd_tensors(PRE, GATE) + 2 * bn_bwd_near(KG, PRE)) * KG * 16;
     return bn_launch<block_norm_bwd_kernel<KG, UNIT, PRE, GATE, STAGES, MAXT, MINB>>(p, s, per_thread * s.threads, per_thread * MAXT, st);
 }
 template <bool PRE, bool GATE>
@@ -562,6 +560,7 @@ static int bn_bwd_run(const BnBwd &p, const BnShape &s, size_t D, cudaStream_t s
     if (D <= 2048) return bn_bwd_launch<1, ROW_CTA, PRE, GATE, 2, 256, 3>(p, s, st);
     if (D <= 4096) return bn_bwd_launch<2, ROW_CTA, PRE, GATE, 2, 256, 2>(p, s, st);
     if (D <= 8192) return bn_bwd_launch<2, ROW_CTA, PRE, GATE, 2, 512, 1>(p, s, st);
+    if (D <= 12288) return bn_bwd_launch<3, ROW_CTA, PRE, GATE, 1, 512, 1>(p, s, st);
     return bn_bwd_launch<4, ROW_CTA, PRE, GATE, 1, 512, 1>(p, s, st);
 }
 
