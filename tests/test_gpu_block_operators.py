@@ -343,7 +343,8 @@ class JointCase:
 
 
 JOINT = [(1, 8), (3, 16), (33, 72), (257, 256), (130, 264), (65, 520), (40, 1032), (300, 1600), (31, 4096), (20, 4104), (19, 8192),
-         (9, 8200), (12, 16384), (1000, 128)]
+         (9, 8200), (12, 16384), (1000, 128),
+         (2000, 520), (1800, 2056), (1500, 8200), (1300, 12296), (5000, 512), (9001, 64), (3001, 248)]       # many rows on a CTA
 
 
 @pytest.mark.parametrize("T,D", JOINT)
@@ -486,6 +487,39 @@ def test_joint_gradient_against_differences(post, gate):
             up[i], down[i] = at[i] + 1e-5 * way, at[i] - 1e-5 * way
             want = (loss(up) - loss(down)) / 2e-5
             assert abs((grad.to(F64) * way).sum().item() - want) <= 3 * HALF[BF16] * (grad.to(F64) * way).abs().sum().item()
+
+
+@pytest.mark.parametrize("T,D", [(5, 64), (300, 1600), (700, 4096), (300, 16384)])
+@pytest.mark.parametrize("place", ["x", "y"])
+def test_joint_sum_in_the_place_of_an_input(T, D, place):
+    c = JointCase(T, D, fp8.NORM_RMS, fp8.GATE_SIGMOID, True)
+    h, out, o2 = full((T, D)), full((T, D)), full((T, D))
+    fp8.fp8_block_norm_fwd(*c.ins(), c.eps, h, out)
+    x, y = c.x.clone(), c.y.clone()
+    at = x if place == "x" else y
+    fp8.fp8_block_norm_fwd(x, y, *c.ins()[2:], c.eps, at, o2)
+    assert torch.equal(at, h) and torch.equal(o2, out)
+
+
+@pytest.mark.parametrize("T,D", [(16, 4096), (20, 4096), (150, 1032), (33, 64), (257, 256), (529, 256), (8200, 2056)])
+def test_joint_amax_in_every_kind_of_grid(T, D):
+    """One CTA, one cluster, a memset in front, a kernel beside: NaN and stale values too."""
+    x = rnd(gen(T), T, D, dtype=BF16)
+    g = torch.ones(D, device="cuda")
+    for bad in (None, math.inf, NAN):
+        if bad is not None:
+            x[T // 2, D // 3] = bad
+        h, amax = full((T, D)), scalar(1e30)
+        fp8.fp8_block_norm_fwd(x, x, None, g, None, fp8.NORM_LAYERSCALE, 0, 1.0, 0.5, 0.0, h, None, amax_out=amax)
+        assert amax.item() == amax_of(h) if bad is None else math.isinf(amax.item()) if math.isinf(bad) else math.isnan(amax.item())
+    c = RopeCase(T, 4, 2, 64, 64, fp8.QK_NONE, False, None)
+    for bad in (None, NAN):
+        if bad is not None:
+            c.qkv[T // 2, 4 * 64] = bad
+        q, k, v, amax = full((T, 4, 64)), full((T, 2, 64)), full((T, 2, 64)), full((3,), 1e30, F32)
+        fp8.fp8_rope_qkv_fwd(c.qkv, 4, 2, *c.how, q, k, v, amax_out=amax)
+        assert amax[0].item() == amax_of(q) and amax[2].item() == amax_of(v)
+        assert math.isnan(amax[1].item()) if bad is not None else amax[1].item() == amax_of(k)
 
 
 def test_joint_rows_of_zeros():
@@ -692,6 +726,46 @@ def test_adamw_skips_a_step_whose_norm_is_not_finite(bad, bits):
     c.norm = scalar(0.1)                                           # below max_norm: not scaled
     c.call(items)
     assert c.step.item() == 5 and not torch.isnan(c.p[0]).any()
+
+
+@pytest.mark.parametrize("bad", [math.inf, NAN, 1e30])
+def test_adamw_of_gradients_that_are_not_finite_without_a_norm(bad):
+    """A value that is not finite spoils its own element, not the block's others; squares that overflow likewise."""
+    c, d = AdamCase([400], 8, F32), AdamCase([400], 8, F32)
+    for x in (c, d):
+        x.norm = None
+    c.g[0][200] = bad
+    d.g[0][200] = 0.0
+    c.call(c.items())
+    d.call(d.items())
+    other = torch.arange(400, device="cuda") != 200
+    assert torch.equal(c.p[0][other], d.p[0][other])
+    far = (torch.arange(400, device="cuda") // 128) != 1
+    assert torch.equal(c.m[0][far], d.m[0][far]) and torch.equal(c.v[0][far], d.v[0][far])
+    r = decode(c.v[0], c.ve[0], 400)
+    assert torch.isnan(r[200]) and not torch.isnan(r[other]).any()                  # 0.001 * 1e60 is over FP32's range
+    m = decode(c.m[0], c.me[0], 400)
+    assert not torch.isnan(m[other]).any() and (torch.isnan(m[200]) if bad != 1e30 else m[200] > 1e28)
+
+
+@pytest.mark.parametrize("scale", [1e-20, 1e-12, 1e3, 1e12])
+def test_adamw_8_bit_moments_over_the_range_of_scales(scale):
+    """Blocks far from the usual size: small ones down to where squares vanish (below FP32's normal numbers: 0), large ones up to
+    where they overflow."""
+    c = AdamCase([1000], 8, F32)
+    c.norm = None
+    c.m[0].zero_(), c.v[0].zero_(), c.me[0].zero_(), c.ve[0].zero_()
+    c.g[0].mul_(1e3 * scale)
+    g = c.g[0].to(F64)
+    c.call(c.items())
+    new_m = (1 - c.b1) * g
+    v = (1 - c.b2) * g * g
+    gone = v < 2.0 ** -125
+    check_codes(c.m[0], c.me[0], new_m, new_m.abs(), random_bits(c.seed, 5, 0, 1000) & 0xFFFF, False)
+    got = decode(c.v[0], c.ve[0], 1000)
+    assert (got[v < 2.0 ** -127] == 0).all()
+    if not gone.any() or scale > 1e-15:
+        check_codes(c.v[0], c.ve[0], v.sqrt(), v.sqrt(), random_bits(c.seed, 5, 0, 1000) >> 16, True)
 
 
 def test_adamw_random_rounding_is_unbiased_and_repeats():
