@@ -198,7 +198,8 @@ struct BnBwd {
     int rms, sigmoid, need_y;
     uint16_t *dx, *dy, *dgate;
     float *partial;
-    unsigned int *amax_bits;
+    unsigned int *maxima;                // behind them: the CTAs' largest dy, for the kernel that adds up the sums
+    unsigned int *amax_bits;             // or, without sums, where it goes
     const float *q_scale;
     uint8_t *dy8;
     int fmt;
@@ -424,6 +425,10 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_bwd_kernel(const BnBwd 
         if (now == ring_end) now = ring;
     }
     cp_async_wait<0>();
+    if (p.maxima) {
+        const uint32_t most = block_max_bf16(pack_bf16x2(m, 0.0f));
+        if (threadIdx.x == 0) p.maxima[blockIdx.x] = most;
+    }
     amax_end(pack_bf16x2(m, 0.0f), p.amax_bits, alone);
     if (!p.partial) return;
     const size_t D = (size_t)p.n8 * 8;
@@ -685,7 +690,9 @@ static int bn_bwd(const char *who, const void *dout, const void *dh, const void 
     p.dy = static_cast<uint16_t *>(dy);
     p.dgate = static_cast<uint16_t *>(dgate);
     p.partial = pre || scaled ? static_cast<float *>(ws) : nullptr;
-    p.amax_bits = reinterpret_cast<unsigned int *>(y ? amax_out : nullptr);
+    unsigned int *const amax = reinterpret_cast<unsigned int *>(y ? amax_out : nullptr);
+    p.maxima = p.partial && amax ? reinterpret_cast<unsigned int *>(p.partial + (size_t)s.grid * 2 * D) : nullptr;
+    p.amax_bits = p.maxima ? nullptr : amax;
     p.q_scale = q_scale;
     p.dy8 = dy8;
     p.fmt = fmt;
@@ -693,7 +700,8 @@ static int bn_bwd(const char *who, const void *dout, const void *dh, const void 
     else rc = gate ? bn_bwd_run<false, true>(p, s, D, st) : bn_bwd_run<false, false>(p, s, D, st);
     if (rc != FP8_OK || !p.partial) return rc;
     return launch_early(column_sums_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, p.partial, (int)s.grid, (unsigned)D,
-                        pre ? dgamma_pre : nullptr, scaled ? dgamma_post : nullptr, accumulate ? 1 : 0);
+                        pre ? dgamma_pre : nullptr, scaled ? dgamma_post : nullptr, accumulate ? 1 : 0,
+                        static_cast<const unsigned int *>(p.maxima), amax);
 }
 
 }  // namespace fp8dpa
@@ -735,7 +743,7 @@ extern "C" int fp8_block_norm_fwd_q(const void *x_bf16, const void *y_bf16, cons
 extern "C" size_t fp8_block_norm_bwd_workspace_bytes(size_t T, size_t D)
 {
     if (T == 0 || D == 0 || D % 8 || D > 16384 || T > 0x7FFFFFFFull) return 0;
-    return ((size_t)bn_bwd_shape(T, D).grid * 2 * D * sizeof(float) + 255) & ~(size_t)255;
+    return ((size_t)bn_bwd_shape(T, D).grid * (2 * D + 1) * sizeof(float) + 255) & ~(size_t)255;
 }
 
 extern "C" int fp8_block_norm_bwd(const void *dout_bf16, const void *dh_bf16, const void *h_bf16, const void *y_bf16,

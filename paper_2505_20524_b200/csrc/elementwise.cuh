@@ -25,6 +25,17 @@ __device__ __forceinline__ void block_max_bf16_to(uint32_t m2, unsigned int *ama
     }
 }
 
+// The block's maximum (of packed BF16 magnitudes) as FP32 bits, in the threads of warp 0.
+__device__ __forceinline__ uint32_t block_max_bf16(uint32_t m2)
+{
+    __shared__ uint32_t warp_max[32];
+    uint32_t m = __reduce_max_sync(0xffffffffu, max(m2 & 0xFFFFu, m2 >> 16));
+    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
+    __syncthreads();
+    m = (threadIdx.x & 31) < (blockDim.x + 31) >> 5 ? warp_max[threadIdx.x & 31] : 0u;
+    return __reduce_max_sync(0xffffffffu, m) << 16;
+}
+
 // Eight BF16 values (four packed words) -> eight FP8 codes under `scale`: the codes fp8_cast gives for the same
 // values (binary32 product, one rounding to FP8).  fmt: 0 = E4M3, 1 = E5M2.
 __device__ __forceinline__ uint2 bf16x8_to_fp8x8(const uint32_t (&w)[4], float scale, int fmt)
