@@ -67,9 +67,12 @@ __global__ void __launch_bounds__(AW_MAXIMA) adamw_begin_kernel(const __grid_con
     const float n = norm ? *norm : 0.0f;
     const bool skip = !(n - n == 0.0f);                   // infinite or NaN
     if (!skip && threadIdx.x < maxima.n) *maxima.amax[threadIdx.x] = 0u;
-    if (threadIdx.x == 0 && out) {
+    if (threadIdx.x < 32 && out) {                        // 1 - beta^t of both rates side by side, on two lanes
         AdamStep s;
         const int now = *step + 1;
+        const double gone = -expm1((double)now * (threadIdx.x & 1 ? log_beta2 : log_beta1));
+        const double gone2 = __shfl_sync(0xffffffffu, gone, 1);
+        if (threadIdx.x != 0) return;
         s.skip = skip;
         s.factor = 1.0f;
         if (norm) {
@@ -77,8 +80,8 @@ __global__ void __launch_bounds__(AW_MAXIMA) adamw_begin_kernel(const __grid_con
             if (f < 1.0f) s.factor = f;
         }
         s.lr = *lr;
-        s.rate = (float)((double)s.lr / -expm1((double)now * log_beta1));
-        s.inv_root = (float)(1.0 / sqrt(-expm1((double)now * log_beta2)));
+        s.rate = (float)((double)s.lr / gone);
+        s.inv_root = (float)(1.0 / sqrt(gone2));
         s.key = mix32(mix32(mix32(seed_lo) ^ seed_hi) ^ (uint32_t)now);
         *out = s;
         if (!skip) *step = now;
