@@ -493,13 +493,13 @@ struct BnShape {
 // four above.
 static BnShape bn_fwd_shape(size_t T, size_t D)
 {
-    const unsigned kg = D <= 8192 ? 2 : 4, lanes = ((unsigned)(D / 8) + kg - 1) / kg;
+    const unsigned kg = D <= 8192 ? 2 : D <= 12288 ? 3 : 4, lanes = ((unsigned)(D / 8) + kg - 1) / kg;
     BnShape s;
     s.cta = D > 512;
     s.lanes_log2 = s.cta ? 0 : D > 256 ? 5 : log2_at_least(lanes);
     s.threads = s.cta ? (lanes + 31) & ~31u : 256;
     const size_t at_once = s.cta ? 1 : s.threads >> s.lanes_log2, want = (T + at_once - 1) / at_once;
-    const size_t most = 148 * (size_t)((D <= 4096 ? 768 : 512) / s.threads);
+    const size_t most = 148 * (size_t)((D <= 4096 ? 768 : D <= 8192 ? 640 : 512) / s.threads);
     s.grid = (unsigned)(want < most ? want : most);
     // up to 16 CTAs are one cluster, which sets the amax to zero itself; a second row per unit is less than a launch for that
     if (s.grid > 16 && s.grid <= 32) s.grid = 16;
@@ -533,10 +533,9 @@ static int bn_launch(const P &p, const BnShape &s, size_t smem, size_t most, cud
     }
     return launch_behind_amax<Kernel>(p.T * p.n8 * 8, p.amax_bits, s.grid, s.threads, smem, st, p, s.lanes_log2);
 }
-template <int KG, RowUnit UNIT, int NT, bool PRE, int MAXT, int MINB>
+template <int KG, RowUnit UNIT, int NT, bool PRE, int STAGES, int MAXT, int MINB>
 static int bn_fwd_launch(const BnFwd &p, const BnShape &s, cudaStream_t st)
 {
-    constexpr int STAGES = 2;
     constexpr size_t per_thread = STAGES * NT * KG * 16;
     return bn_launch<block_norm_fwd_kernel<KG, UNIT, NT, PRE, STAGES, MAXT, MINB>>(p, s, per_thread * s.threads, per_thread * MAXT, st);
 }
@@ -544,11 +543,12 @@ template <int NT, bool PRE>
 static int bn_fwd_run(const BnFwd &p, size_t D, cudaStream_t st)
 {
     const BnShape s = bn_fwd_shape(p.T, D);
-    if (D <= 256) return bn_fwd_launch<2, ROW_LANES, NT, PRE, 256, 3>(p, s, st);
-    if (D <= 512) return bn_fwd_launch<2, ROW_WARP, NT, PRE, 256, 3>(p, s, st);
-    if (D <= 4096) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 256, 3>(p, s, st);
-    if (D <= 8192) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 512, 1>(p, s, st);
-    return bn_fwd_launch<4, ROW_CTA, NT, PRE, 512, 1>(p, s, st);
+    if (D <= 256) return bn_fwd_launch<2, ROW_LANES, NT, PRE, 2, 256, 3>(p, s, st);
+    if (D <= 512) return bn_fwd_launch<2, ROW_WARP, NT, PRE, 2, 256, 3>(p, s, st);
+    if (D <= 4096) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 2, 256, 3>(p, s, st);
+    if (D <= 8192) return bn_fwd_launch<2, ROW_CTA, NT, PRE, 3, 512, 1>(p, s, st);
+    if (D <= 12288) return bn_fwd_launch<3, ROW_CTA, NT, PRE, 3, 512, 1>(p, s, st);
+    return bn_fwd_launch<4, ROW_CTA, NT, PRE, 2, 512, 1>(p, s, st);
 }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
 static int bn_bwd_launch(const BnBwd &p, const BnShape &s, cudaStream_t st)
