@@ -631,6 +631,53 @@ def report_step_operators(fp8, T, H, add, timed, bf16, f32):
     add("fp8_grad_clip (BF16 to FP32)", f"{numel}", timed(lambda: fp8.fp8_grad_clip(items, a, 1.0)), nbytes=6 * numel)
 
 
+def report_block_operators(fp8, T, cfg, add, timed, bf16, f32):
+    """Rows of the operators between a block's products and of the optimizer: rotary positions, the joint of two blocks, AdamW."""
+    import torch
+
+    H, Hq, Hkv, d = cfg.hidden, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+    W = (Hq + 2 * Hkv) * d
+    empty = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device="cuda")
+    e8 = lambda *s: empty(*s, dt=torch.uint8)
+    vec = lambda n: 1 + 0.1 * torch.randn(n, device="cuda")
+    cos, sin = empty(131072, d // 2, dt=torch.float32), empty(131072, d // 2, dt=torch.float32)
+    add("fp8_rope_table", f"131072x{d // 2}", timed(lambda: fp8.fp8_rope_table(cos, sin, 500000.0, fp8.ROPE_BY_PARTS, 16.0, 8192.0)),
+        nbytes=8 * cos.numel())
+    qkv, sc, a, a3 = bf16(T, W), f32(2.0 ** 10), f32(), empty(3, dt=torch.float32)
+    how, scales = (fp8.QK_RMS, 0.0, 1e-6, cos, sin, None, False), torch.full((3,), 32.0, device="cuda")
+    q8, k8, v8, dqkv8 = e8(T, Hq, d), e8(T, Hkv, d), e8(T, Hkv, d), e8(T, W)
+    add("fp8_rope_qkv_fwd_q (RMS, FP8 codes + amax)", f"{T}x({Hq}+2x{Hkv})x{d}",
+        timed(lambda: fp8.fp8_rope_qkv_fwd_q(qkv, Hq, Hkv, *how, scales, 0, q8, k8, v8, amax_out=a3)), nbytes=3 * T * W)
+    dq, dk, dv = bf16(T, Hq, d), bf16(T, Hkv, d), bf16(T, Hkv, d)
+    add("fp8_rope_qkv_bwd_q (RMS, E5M2 codes + amax)", f"{T}x({Hq}+2x{Hkv})x{d}",
+        timed(lambda: fp8.fp8_rope_qkv_bwd_q(dq, dk, dv, qkv, *how, sc, 1, dqkv8, amax_out=a)), nbytes=3 * T * W + 2 * T * (Hq + Hkv) * d)
+    x, y, gate, h, o8, rq, rp = bf16(T, H), bf16(T, H), bf16(T, H), empty(T, H), e8(T, H), empty(T, dt=torch.float32), empty(T, dt=torch.float32)
+    gq, gp = vec(H), vec(H)
+    for name, g, n in (("", None, 7), (", gate", gate, 9)):
+        add(f"fp8_block_norm_fwd_q (norm behind and in front{name}, FP8 codes + amax)", f"{T}x{H}", timed(lambda: fp8.fp8_block_norm_fwd_q(
+            x, y, g, gq, gp, fp8.NORM_RMS, 1, 1.0, 1.0, 1e-5, sc, 0, h, None, o8, r_post=rq, r_pre=rp, amax_out=a)), nbytes=n * T * H)
+    dout, dh, dx, dg, dgq, dgp = bf16(T, H), bf16(T, H), empty(T, H), empty(T, H), vec(H), vec(H)
+    w = e8(fp8.fp8_block_norm_bwd_workspace_bytes(T, H))
+    for name, g, n in (("", None, 11), (", gate", gate, 15)):
+        add(f"fp8_block_norm_bwd_q (norm behind and in front{name}, E5M2 codes + amax)", f"{T}x{H}", timed(lambda: fp8.fp8_block_norm_bwd_q(
+            dout, dh, h, y, g, gq, gp, rq, rp, fp8.NORM_RMS, 1, 1.0, 1.0, sc, 1, dx, None, o8, None if g is None else dg, dgq, dgp, w,
+            amax_out=a)), nbytes=n * T * H)
+    del qkv, dq, dk, dv, x, y, gate, h, dout, dh, dx, dg
+    grads = [bf16(6144, H), bf16(H, H), bf16(28672, H), bf16(H, 14336)]
+    n = sum(g.numel() for g in grads)
+    params, p16, p8 = [g.float() for g in grads], [g.clone() for g in grads], [e8(*g.shape) for g in grads]
+    lr, step, norm, ones = f32(1e-4), torch.zeros(1, dtype=torch.int32, device="cuda"), f32(2.0), torch.ones(4, device="cuda")
+    for bits in (32, 8):
+        zeros = lambda g: torch.zeros_like(g, dtype=torch.float32 if bits == 32 else torch.uint8)
+        ms, vs = [zeros(g) for g in grads], [zeros(g) for g in grads]
+        exps = [[torch.zeros(-(-g.numel() // 128), dtype=torch.uint8, device="cuda") for g in grads] for _ in range(2)]
+        items = fp8.fp8_adamw_items(params, grads, ms, vs, [0.1] * 4, m_exps=exps[0], v_exps=exps[1], params16=p16, params8=p8,
+                                    q_scales=ones, amaxes=empty(4, dt=torch.float32))
+        w = e8(fp8.fp8_adamw_workspace_bytes(items))
+        add(f"fp8_adamw ({bits}-bit moments, BF16 gradients, BF16 + FP8 copies + amax)", f"{n}",
+            timed(lambda: fp8.fp8_adamw(items, lr, step, 0.9, 0.95, 1e-8, w, norm=norm)), nbytes=n * (29 if bits == 32 else 17))
+
+
 def run_report(args):
     """`--report`: every kernel of the library timed alone (CUDA events on the launching stream, 3 warm-ups, median of
     `--steps` launches).  Between launches a 256 MB buffer is written (nothing of the previous launch stays in L2) and
@@ -764,6 +811,7 @@ def run_report(args):
         nbytes=3 * qk.numel())
     del r, y, o_, qk, qo, q8_
     report_step_operators(fp8, T, H, add, timed, bf16, f32)
+    report_block_operators(fp8, T, c4, add, timed, bf16, f32)
 
     # ---- GEMMs of c3 and c4: forward / dgrad / wgrad, the producer form and the blockwise recipe
     for cname in ("c3", "c4"):

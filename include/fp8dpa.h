@@ -432,7 +432,8 @@ FP8_API int fp8_rope_qkv_bwd_q(const void *dq_bf16, const void *dk_bf16, const v
  *          y                      FP8_NORM_NONE (gamma_post is not read)
  *   h    = x_scale x + y_scale s z, rounded to BF16;  s = gate (FP8_GATE_LINEAR), sigmoid(gate) (FP8_GATE_SIGMOID), 1 without one
  *   out  = gamma_pre h r_pre, r_pre = 1 / sqrt(mean(h^2) + eps) of the rounded h, rounded to BF16
- * The reciprocal roots come from the hardware's, off by 2 ulp at most; a row of zeros without eps gives NaN. */
+ * The reciprocal roots come from the hardware's, off by 2 ulp at most; a row of zeros without eps gives NaN, and one whose mean
+ * square and eps lie below FP32's normal numbers (2^-126) has no gradient (its reciprocal root's square overflows). */
 enum { FP8_NORM_NONE = 2 };                             /* beside FP8_NORM_RMS and FP8_NORM_LAYERSCALE */
 enum { FP8_GATE_LINEAR = 0, FP8_GATE_SIGMOID = 1 };
 typedef struct {
@@ -532,13 +533,15 @@ FP8_API int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *
  *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *   p = p (1 - *lr weight_decay) - *lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
  * and *step = t.  A norm that is NaN or infinite skips the step: nothing is changed, *step and the outputs neither.  (Without norm
- * a gradient that is not finite makes its element, and with moments in 8 bits its block of 128, worthless.)
+ * a gradient that is not finite makes its element NaN, that one alone.)
  * Outputs (nullable): p_bf16 the rounded weights, p8 = FP8cast(*q_scale * p_bf16) in `fmt` (bit-identical to fp8_cast of p_bf16),
  * *amax = amax(p_bf16): what fp8_quantize_delayed_multi would take another pass for.
  *
  * state_bits = 32: m, v: n binary32.  state_bits = 8: m: n E4M3 codes, v: n E4M3 codes of sqrt(v), in blocks of 128 consecutive
  * elements with a scale 2^(m_exp[i / 128] - 127), 2^(v_exp[i / 128] - 127): the smallest power of two (2^-126 at least) that leaves no
- * value above 448.  The update uses the values before they are stored.  A stored value is rounded towards zero or away from it
+ * value above 448.  m, v and the root of v take one rounding per operation in the order written above (a sum below FP32's normal
+ * numbers is 0), so that codes are the same wherever they are worked out.  The update uses the values before they are stored.  A
+ * stored value is rounded towards zero or away from it
  * with the probability of the part cut off, from 16 random bits each: the lower (m) and upper (v) half of
  * mix(mix(mix(K + item) + (i >> 32)) + i) modulo 2^32, K = mix(mix(mix(seed) ^ (seed >> 32)) ^ t), with mix(x): x = (x ^ x >> 16) *
  * 0x9E3779B9; x = (x ^ x >> 15) * 0x6A09E667; x ^ x >> 16, item the number in the list; the same seed and step give the same

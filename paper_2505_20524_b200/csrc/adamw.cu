@@ -1,5 +1,10 @@
 // AdamW over many tensors: clip, moments, decayed weights, their BF16 copy, FP8 codes and amax for the next step's products, with
 // moments in FP32 or in 8 bits.
+//
+// The tensors are cut into chunks, numbered through all of them, and a short CTA takes one, found through a table that travels with
+// the launch.  With FP32 moments bytes bind (218 M weights, BF16 gradients and both copies: 924 us, 6.3 GB at 6.8 TB/s).  With 8
+// bits 17 bytes are left per weight and the arithmetic comes up to them: 102 instructions per weight took 916 us, 59 take 565 to
+// 610 (3.7 GB at 6.1 to 6.6 TB/s; the longer it runs the lower the clocks that power allows).
 #include <math.h>
 
 #include "common.cuh"

@@ -50,7 +50,8 @@ struct BnFwd {
 // Rows and columns on threads as in the layer norm: a thread holds KG groups of eight columns of its unit's rows, both gammas of
 // them in registers, and the next rows travel through its private ring.  NT tensors are read (x; y; gate); the sum of squares of
 // y, the joint, its rounding to BF16, the sum of squares of that and the result follow in one pass: every tensor is read once and
-// written once.  The reciprocal roots by rsqrtf, off by 2 ulp of FP32 at most.
+// written once (8192 x 4096 with both norms and codes: 39.5 us in a graph, 235 MB at 5.9 TB/s; 43 with two CTAs per SM for three;
+// with a gate 49.5 us, 6.1 TB/s).  The reciprocal roots by rsqrtf, off by 2 ulp of FP32 at most.
 template <int KG, RowUnit UNIT, int NT, bool PRE, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd p, int lanes_log2)
 {
@@ -208,8 +209,14 @@ struct BnBwd {
 // With hh = h r_pre, e = gamma_pre dout:  D = dh + r_pre (e - hh mean(e hh)), dx = a D;  yh = y r_post, z = gamma_post yh,
 // dgate = b D z s', dz = b D s, f = gamma_post dz:  dy = r_post (f - yh mean(f yh));  over rows dgamma_pre = sum dout hh and
 // dgamma_post = sum dz yh, which a thread keeps in registers for its columns.  The two means are two sums over the row's
-// threads, the second from what the first gives.  Every tensor is read once and written once.
-// STAGES = 1: the ring holds one row, and a thread asks for the next row's piece as soon as it has read its own.
+// threads, the second from what the first gives.  Every tensor is read once and written once.  The reciprocal roots go into
+// scalars of the row: the loop forms e r_pre, dz r_post and f r_post and adds multiples of h and y to them, and the gammas lie in
+// shared memory (8192 x 4096 with gate and codes: 106 -> 88 us in a graph, 503 MB at 5.7 TB/s; without a gate 70 us for 369 MB).
+// Two barriers per row on 16 warps leave 0.55 instructions per cycle and scheduler; 512 threads with one group each, two CTAs
+// per SM, have to do with 64 registers and spill (120 us).
+// STAGES = 1: the ring holds one row, and a thread asks for the next row's piece as soon as it has read its own: above 8192
+// columns, where two rows find no room (3000 x 10000: 84 us without a gate, memory's 55; 2048 x 16384 102, memory's 62: 64 of 128
+// registers are the gammas' sums there, and one CTA fills an SM).
 __host__ __device__ constexpr int bn_bwd_tensors(bool pre, bool gate) { return 2 + 2 * pre + gate; }
 __host__ __device__ constexpr int bn_bwd_near(int kg, bool pre) { return kg <= 3 && pre ? 2 : 1; }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
@@ -489,8 +496,10 @@ struct BnShape {
     int lanes_log2;
     unsigned threads, grid;
 };
-// Forward: two groups of columns per thread on lanes of a warp up to 256 columns, on a warp up to 512, on the CTA up to 4096;
-// four above.
+// Forward: two groups of columns per thread on lanes of a warp up to 256 columns, on a warp up to 512, on the CTA up to 8192 (one
+// group up to 2048 was 3 us slower at 16384 x 1024, four above 4096 1 to 3 us at 4096 x 8192), three up to 12288, then four.  As
+// many CTAs per SM as 768 threads make, 640 above 4096 columns (6000 x 5120: 49 -> 38 us), one above 8192.  Above 4096 columns
+// three rows travel instead of two, where they find room (4096 x 8192 without a norm in front 43 -> 40 us).
 static BnShape bn_fwd_shape(size_t T, size_t D)
 {
     const unsigned kg = D <= 8192 ? 2 : D <= 12288 ? 3 : 4, lanes = ((unsigned)(D / 8) + kg - 1) / kg;
@@ -506,8 +515,9 @@ static BnShape bn_fwd_shape(size_t T, size_t D)
     return s;
 }
 // Backward: lanes of a warp with one group of columns each up to 128 columns, a warp with one up to 256 and two up to 512, then
-// the CTA with two, above 8192 with four.  A CTA has eight rows at least where there are more than 148 of them (fewer sums to
-// add up behind the pass).
+// the CTA with one up to 2048 (8192 x 2048 with a gate: 63 us with two, 52 with one), two up to 8192, three up to 12288 (3000 x
+// 10000 with a gate: 154 us with four, 104 with three), four above.  A CTA has eight rows at least where there are more than 148 of
+// them (fewer sums to add up behind the pass).
 static BnShape bn_bwd_shape(size_t T, size_t D)
 {
     const unsigned n8 = (unsigned)(D / 8);

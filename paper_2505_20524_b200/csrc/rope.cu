@@ -38,7 +38,8 @@ __device__ __forceinline__ void sincos2(uint64_t x, uint64_t &sn, uint64_t &cs)
 // The angle in turns is a product in 64 bits, good to 2^-52 of itself; what is left of it next to the nearest quarter turn is
 // rounded to FP32, so that cos and sin are good to 2 ulp wherever the position lies, next to their zeros too.  Adding 1.5 * 2^52
 // leaves the nearest whole number of quarters in the low bits (2^31 turns at most).
-// A thread keeps four frequencies and walks over the positions.
+// A thread keeps four frequencies and walks over the positions (131072 x 64: 12.0 us in a graph, 67 MB at 5.6 TB/s; 34 us with the
+// frequencies read from the launch's parameters at every place, where lanes ask for different ones).
 __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__ RopeTable t)
 {
     const unsigned quads = t.pairs / 4, wide = 256 / quads, q = threadIdx.x % quads;
@@ -207,10 +208,13 @@ __device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int
 // of the rotated part's second half, so that both kinds of partners are in one lane; behind it likewise, which passes through.
 // A group of lanes takes up to ROPE_HEADS heads of one tensor of one token with the token's angles in registers.  Persistent: a
 // group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
-// bind: every element is read once and written once.
+// bind: every element is read once and written once (8192 tokens of 32 + 2 x 8 heads of 128 with codes: 29.1 us in a graph, 153 MB
+// at 5.3 TB/s; gradient 42.4 us, 237 MB at 5.6 TB/s; with a launch per call and whole-token CTAs that do not stay 47 and 72 us).
 //
-// Instructions are the next bound, so the usual case, all lanes of a warp with whole pieces of Q and K or of V, runs through four
-// heads without a branch; V's pieces lie behind Q's and K's of all tokens of the CTA for that.  What is left takes the other path.
+// Instructions are the next bound (23.7 M of a warp at first, 15.6 M now), so the usual case, all lanes of a warp with whole pieces
+// of Q and K or of V, runs through four heads without a branch (33 -> 29.6 us, gradient 59 -> 43); V's pieces lie behind Q's and K's
+// of all tokens of the CTA for that.  What is left takes the other path.  A second set of registers for the next token's angles or
+// a branch around the rotation spills and costs 4 to 17 us.
 // KIND: what is written, BF16 alone, codes alone in the direction's usual type (E4M3, E5M2 backward), or anything.
 enum RopeKind { ROPE_BF16, ROPE_CODES, ROPE_ANY };
 template <int MODE, bool BACK>
@@ -228,10 +232,10 @@ __device__ __forceinline__ float head_sum(float v, int lanes)
     return v;
 }
 
-// D: the head's size where it is one of the attention's and all of it is rotated (places are then known to the compiler; 8192
-// tokens with codes: 29.6 us without), else 0.
+// D: the head's size where it is one of the attention's and all of it is rotated (places are then known to the compiler: 18.7 -> 15.6 M
+// instructions), else 0.
 template <int D, int MODE, bool PAIRS, bool BACK, RopeKind KIND, int STAGES>
-__global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs p, int)
+__global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs p, int /* of no use here */)
 {
     extern __shared__ __align__(16) uint4 ring_mem[];
     constexpr bool SAVED = BACK && MODE != FP8_QK_NONE;
