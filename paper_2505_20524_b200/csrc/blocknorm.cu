@@ -709,7 +709,7 @@ static int bn_bwd(const char *who, const void *dout, const void *dh, const void 
     if (pre) rc = gate ? bn_bwd_run<true, true>(p, s, D, st) : bn_bwd_run<true, false>(p, s, D, st);
     else rc = gate ? bn_bwd_run<false, true>(p, s, D, st) : bn_bwd_run<false, false>(p, s, D, st);
     if (rc != FP8_OK || !p.partial) return rc;
-    return launch_early(column_sums_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, p.partial, (int)s.grid, (unsigned)D,
+    return launch_early(p.maxima ? column_sums_kernel<true> : column_sums_kernel<false>, (unsigned)((2 * D + 31) / 32), 1024, 0, st, p.partial, (int)s.grid, (unsigned)D,
                         pre ? dgamma_pre : nullptr, scaled ? dgamma_post : nullptr, accumulate ? 1 : 0,
                         static_cast<const unsigned int *>(p.maxima), amax);
 }

@@ -530,7 +530,7 @@ extern "C" int fp8_layernorm_bwd(const void *dout_bf16, const void *x_bf16, cons
     else if (D <= 8192) rc = ln_bwd_launch<2, ROW_CTA, 512, 1>(p, s, st);
     else rc = ln_bwd_launch<4, ROW_CTA, 512, 1>(p, s, st);
     if (rc != FP8_OK) return rc;
-    return launch_early(column_sums_kernel, (unsigned)((2 * D + 31) / 32), 1024, 0, st, partial, (int)s.grid,
+    return launch_early(column_sums_kernel<false>, (unsigned)((2 * D + 31) / 32), 1024, 0, st, partial, (int)s.grid,
                         (unsigned)D, dgamma, dbeta, accumulate ? 1 : 0, static_cast<const unsigned int *>(nullptr),
                         static_cast<unsigned int *>(nullptr));
 }

@@ -110,12 +110,13 @@ constexpr int ROPE_HEADS = 4;
 template <bool PAIRS>
 struct Angles {
     uint64_t c[PAIRS ? 8 : 4], up[PAIRS ? 1 : 4], down[PAIRS ? 8 : 4];
-    __device__ __forceinline__ void load(const float *pc, const float *ps, int i0, int i1, bool back)
+    // from eight cos and eight sin, places 0 to 3 and 4 to 7 of the lane
+    __device__ __forceinline__ void set(const uint4 c0, const uint4 c1, const uint4 s0, const uint4 s1, bool back)
     {
-        const float4 c0 = __ldg(reinterpret_cast<const float4 *>(pc + i0)), c1 = __ldg(reinterpret_cast<const float4 *>(pc + i1));
-        const float4 s0 = __ldg(reinterpret_cast<const float4 *>(ps + i0)), s1 = __ldg(reinterpret_cast<const float4 *>(ps + i1));
-        const float cs[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-        float sn[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+        const float cs[8] = {__uint_as_float(c0.x), __uint_as_float(c0.y), __uint_as_float(c0.z), __uint_as_float(c0.w),
+                             __uint_as_float(c1.x), __uint_as_float(c1.y), __uint_as_float(c1.z), __uint_as_float(c1.w)};
+        float sn[8] = {__uint_as_float(s0.x), __uint_as_float(s0.y), __uint_as_float(s0.z), __uint_as_float(s0.w),
+                       __uint_as_float(s1.x), __uint_as_float(s1.y), __uint_as_float(s1.z), __uint_as_float(s1.w)};
 #pragma unroll
         for (int e = 0; e < 8; ++e) sn[e] = back ? -sn[e] : sn[e];
 #pragma unroll
@@ -208,8 +209,8 @@ __device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int
 // of the rotated part's second half, so that both kinds of partners are in one lane; behind it likewise, which passes through.
 // A group of lanes takes up to ROPE_HEADS heads of one tensor of one token with the token's angles in registers.  Persistent: a
 // group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
-// bind: every element is read once and written once (8192 tokens of 32 + 2 x 8 heads of 128 with codes: 29.1 us in a graph, 153 MB
-// at 5.3 TB/s; gradient 42.4 us, 237 MB at 5.6 TB/s; with a launch per call and whole-token CTAs that do not stay 47 and 72 us).
+// bind: every element is read once and written once (8192 tokens of 32 + 2 x 8 heads of 128 with codes: 27.5 us in a graph, 153 MB
+// at 5.6 TB/s; gradient 42.4 us, 237 MB at 5.6 TB/s; with a launch per call and whole-token CTAs that do not stay 47 and 72 us).
 //
 // Instructions are the next bound (23.7 M of a warp at first, 15.6 M now), so the usual case, all lanes of a warp with whole pieces
 // of Q and K or of V, runs through four heads without a branch (33 -> 29.6 us, gradient 59 -> 43); V's pieces lie behind Q's and K's
@@ -272,9 +273,33 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
     // places in shared memory: [stage][slot][thread]; slots 2 hh, 2 hh + 1 are a head's groups, behind them those of what is saved
     const uint32_t per_slot = blockDim.x * 16u, per_stage = per_slot * rope_slots<MODE, BACK>();
     const uint32_t ring = smem_u32(ring_mem + threadIdx.x), ring_end = ring + STAGES * per_stage;
+    // Forward: the angles lie behind them, [stage][token][cos, sin][rot / 2], copied by the first group of a token's for all (29.1
+    // -> 27.5 us).  Backward has half the warps, whom the barrier for that costs more than the loads (42.4 us, 46.6 with it).
+    constexpr bool SHARED = !BACK;
+    const uint32_t tables = smem_u32(ring_mem) + STAGES * per_stage, per_table = p.tokens * rot * 4u;
+    const bool copies = SHARED && mine && turns && part < 2 && (p.blocks > 1 ? group == 0 : group == local * n_qk);
+    const uint32_t at0 = (PAIRS ? 4 * j : 8 * j) * 4u, at1 = (PAIRS ? rot / 4 + 4 * j : 8 * j + 4) * 4u, apart = rot * 2u;
+    // A token's row of the tables, or -1 outside of them.
+    const auto row_of = [&](unsigned t) -> int {
+        if (!rot || !mine || t >= T) return 0;
+        if (!p.positions) return (int)(t % (unsigned)p.n_pos);
+        const long long at = p.wide_positions ? __ldg(static_cast<const long long *>(p.positions) + t)
+                                              : (long long)__ldg(static_cast<const int *>(p.positions) + t);
+        return at >= 0 && (unsigned long long)at < p.n_pos ? (int)at : -1;
+    };
+    int row_now = SHARED ? row_of(t) : 0, row_ahead = row_now;
     const uint16_t *next = (BACK ? p.grad[part] + in_part : p.qkv + in_row) + (size_t)ahead * (BACK ? part_pitch : p.pitch);
     const uint16_t *next_saved = SAVED ? p.qkv + in_row + (size_t)ahead * p.pitch : nullptr;
-    const auto fetch = [&](uint32_t to) {
+    const auto fetch = [&](uint32_t to, uint32_t table) {
+        if (copies && ahead < T) {
+            const size_t from = (size_t)max(row_ahead, 0) * (rot / 2);
+            const uint32_t into = table + local * rot * 4u;
+            const float *c = p.cos_t + from, *s = p.sin_t + from;
+            cp_async16(into + at0, reinterpret_cast<const char *>(c) + at0);
+            cp_async16(into + at1, reinterpret_cast<const char *>(c) + at1);
+            cp_async16(into + apart + at0, reinterpret_cast<const char *>(s) + at0);
+            cp_async16(into + apart + at1, reinterpret_cast<const char *>(s) + at1);
+        }
         if (mine && ahead < T) {
 #pragma unroll
             for (int hh = 0; hh < ROPE_HEADS; ++hh) {
@@ -290,18 +315,18 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
         }
         cp_async_commit();
         ahead += step;
+        if (SHARED) row_ahead = row_of(ahead);
         next += step * (BACK ? part_pitch : p.pitch);
         if (SAVED) next_saved += step * p.pitch;
     };
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) fetch(ring + s * per_stage);
+    static_assert(STAGES == 2, "row_ahead is one token ahead");
+    fetch(ring, tables);
     const uint64_t qs2 = both(p.scales ? __ldg(p.scales + (BACK ? 0 : part)) : 1.0f);
     const size_t out_pitch = BACK ? p.out_pitch : part_pitch, out8_pitch = BACK ? row_pitch : part_pitch, out_at = BACK ? in_row : in_part;
     uint16_t *const out = BACK ? p.out[0] : p.out[part];
     uint8_t *const out8 = BACK ? p.out8[0] : p.out8[part];
-    const int i0 = PAIRS ? 4 * j : 8 * j, i1 = PAIRS ? rot / 4 + 4 * j : 8 * j + 4;
     float m = 0.0f;
-    uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage;
+    uint32_t now = ring, fill = ring + (STAGES - 1) * per_stage, table = tables;
 
     // A lane's part of a head: what is read, regularised and rotated (or back), with `qk` false as it is.
     const auto work = [&](int hh, bool qk, bool every_lane_turns, const Angles<PAIRS> &angles, uint64_t (&a)[4], uint64_t (&b)[4]) {
@@ -375,24 +400,25 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
     const bool plain_lane = mine && here == ROPE_HEADS, whole_head = rot == d;
     const bool plain_qk = __all_sync(0xffffffffu, plain_lane && part < 2), plain_v = __all_sync(0xffffffffu, plain_lane && part == 2);
     for (unsigned base = first * p.tokens; base < T; base += step, t += step) {
-        unsigned pos = 0;
-        bool known = true;
-        const bool live = mine && t < T;
-        if (live) {
-            if (p.positions) {
-                const long long at = p.wide_positions ? __ldg(static_cast<const long long *>(p.positions) + t)
-                                                      : (long long)__ldg(static_cast<const int *>(p.positions) + t);
-                known = at >= 0 && (unsigned long long)at < p.n_pos;
-                pos = known ? (unsigned)at : 0u;                  // row 0 for a token outside the table
-            } else if (rot) {
-                pos = t % (unsigned)p.n_pos;
-            }
-        }
+        const int here_row = SHARED ? row_now : row_of(t);
+        const bool live = mine && t < T, known = here_row >= 0;
+        row_now = row_ahead;
         Angles<PAIRS> angles;
-        if (turns && part < 2) angles.load(p.cos_t + (size_t)pos * (rot / 2), p.sin_t + (size_t)pos * (rot / 2), i0, i1, BACK);
+        if (!SHARED && turns && part < 2) {
+            const size_t from = (size_t)max(here_row, 0) * (rot / 2);                  // row 0 for a token outside the table
+            const char *c = reinterpret_cast<const char *>(p.cos_t + from), *s = reinterpret_cast<const char *>(p.sin_t + from);
+            const auto get = [](const char *q) { return __ldg(reinterpret_cast<const uint4 *>(q)); };
+            angles.set(get(c + at0), get(c + at1), get(s + at0), get(s + at1), BACK);
+        }
         cp_async_wait<STAGES - 2>();
-        fetch(fill);                                           // the stage of the token before this one
+        if (SHARED) __syncthreads();                           // the token's angles are there, and the stage in front is read
+        fetch(fill, table == tables ? tables + per_table : tables);
         fill = now;
+        if (SHARED && turns && part < 2) {
+            const uint32_t c = table + local * rot * 4u, s = c + apart;
+            angles.set(ring_get(c + at0), ring_get(c + at1), ring_get(s + at0), ring_get(s + at1), BACK);
+        }
+        table = table == tables ? tables + per_table : tables;
         uint16_t *const o = out + (size_t)t * out_pitch + out_at;
         uint8_t *const o8 = out8 + (size_t)t * out8_pitch + out_at;
         const bool plain = __all_sync(0xffffffffu, live && known);
@@ -437,14 +463,13 @@ __global__ void __launch_bounds__(256, BACK ? 2 : 3) rope_kernel(const __grid_co
     }
 }
 
-template <auto Kernel>
+template <auto Kernel, bool SHARED>
 static int rope_run(const RopeArgs &p, unsigned grid, unsigned threads, size_t per_thread, size_t elements, cudaStream_t st)
 {
-    if (256 * per_thread > 40 * 1024) {
-        const int rc = allow_shared<Kernel>((int)(256 * per_thread));
-        if (rc != FP8_OK) return rc;
-    }
-    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, threads * per_thread, st, p, 0, p.words);
+    const int rc = allow_shared<Kernel>((int)(256 * per_thread + (SHARED ? 2 * 16384 : 0)));      // of angles 16 KB at most a stage
+    if (rc != FP8_OK) return rc;
+    return launch_behind_amax<Kernel>(elements, p.amax_bits, grid, threads, threads * per_thread + (SHARED ? 8 * (size_t)p.tokens * p.rot : 0),
+                                      st, p, 0, p.words);
 }
 
 template <bool BACK>
@@ -482,7 +507,7 @@ static int rope_launch(RopeArgs &p, int mode, bool pairs, cudaStream_t st)
     constexpr int STAGES = 2;
     const int whole = p.rot == p.d ? p.d : 0;
 #define FP8DPA_ROPE_RUN(D, MODE, PAIRS, KIND) \
-    return rope_run<rope_kernel<D, MODE, PAIRS, BACK, KIND, STAGES>>(p, grid, threads, (size_t)STAGES * rope_slots<MODE, BACK>() * 16, elements, st)
+    return rope_run<rope_kernel<D, MODE, PAIRS, BACK, KIND, STAGES>, !BACK>(p, grid, threads, (size_t)STAGES * rope_slots<MODE, BACK>() * 16, elements, st)
 #define FP8DPA_ROPE_SIZE(MODE, PAIRS, KIND) \
     do { \
         if (whole == 128) FP8DPA_ROPE_RUN(128, MODE, PAIRS, KIND); \

@@ -133,8 +133,9 @@ struct Rows {
 __device__ __forceinline__ Rows rows_of(size_t u, size_t n, size_t T) { return {T * u / n, T * (u + 1) / n}; }
 
 // Two vectors of D columns (each may be missing) from the CTAs' sums in `partial` [CTA][2][D]: 32 columns per CTA, a warp takes
-// every 32nd of the sums, then the warps in order.  With `maxima` [CTA] (bits of values that are not negative) the first CTA also
-// leaves the largest in *amax.
+// every 32nd of the sums, then the warps in order.  MAXIMA: the first CTA also leaves the largest of `maxima` [CTA] (bits of values
+// that are not negative) in *amax.
+template <bool MAXIMA>
 static __global__ void __launch_bounds__(1024) column_sums_kernel(const float *__restrict__ partial, int parts, unsigned D,
                                                                   float *__restrict__ first, float *__restrict__ second,
                                                                   int accumulate, const unsigned int *__restrict__ maxima,
@@ -143,7 +144,7 @@ static __global__ void __launch_bounds__(1024) column_sums_kernel(const float *_
     cudaGridDependencySynchronize();
     __shared__ float red[32][33];
     __shared__ unsigned int most;
-    if (maxima && blockIdx.x == 0) {
+    if (MAXIMA && blockIdx.x == 0) {
         if (threadIdx.x == 0) most = 0u;
         __syncthreads();
         unsigned int m = 0u;
