@@ -31,6 +31,16 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t v)
     return sigmoid2(v, unused);
 }
 
+// A sum of products, each with its own rounding as written (the compiler joins packed sums with their products): without a norm
+// or a sigmoid the joint is then what elementary operations give, bit for bit.
+__device__ __forceinline__ uint64_t add_apart(uint64_t a, uint64_t b)
+{
+    float a0, a1, b0, b1;
+    unpack_f32x2(a, a0, a1);
+    unpack_f32x2(b, b0, b1);
+    return pack_f32x2(__fadd_rn(a0, b0), __fadd_rn(a1, b1));
+}
+
 // ---------------------------------------------------------------- forward
 struct BnFwd {
     const uint16_t *in[3];               // x, y, gate
@@ -151,7 +161,7 @@ __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd 
                     for (int e = 0; e < 4; ++e) y[e] = mul_f32x2(y[e], p.sigmoid ? sigmoid2(g[e]) : g[e]);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = fma_f32x2(b2, y[e], f[e]);
+                for (int e = 0; e < 4; ++e) f[e] = add_apart(f[e], mul_f32x2(b2, y[e]));
             }
             hw[k] = make_uint4(round2(f[0]), round2(f[1]), round2(f[2]), round2(f[3]));
             if (!in[k]) hw[k] = make_uint4(0u, 0u, 0u, 0u);   // 0 * inf where a row of zeros has no eps
