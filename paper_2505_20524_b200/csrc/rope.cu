@@ -702,17 +702,20 @@ extern "C" int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, d
     int rc = check_arch();
     if (rc != FP8_OK) return rc;
     RopeTable t = {};
-    const double full_turn = 6.283185307179586477;
-    if (scaling == FP8_ROPE_NTK) base *= pow(factor, rot / (rot - 2.0));
-    for (int i = 0; i < rot / 2; ++i) {
-        double f = pow(base, -2.0 * i / rot);
+    // powers of one ratio in 80 bits: 127 products in a row leave less than 2^-56 of error, in the time of two calls of pow
+    const long double full_turn = 6.28318530717958647692529L;
+    long double power_of = base, f_i = 1.0L;
+    if (scaling == FP8_ROPE_NTK) power_of *= powl(factor, rot / (rot - 2.0L));
+    const long double ratio = powl(power_of, -2.0L / rot);
+    for (int i = 0; i < rot / 2; ++i, f_i *= ratio) {
+        long double f = f_i;
         if (scaling == FP8_ROPE_LINEAR) f /= factor;
         if (parts) {
-            double w = (original_len * f / full_turn - turns_low) / (turns_high - turns_low);
-            w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
-            f = (1.0 - w) * f / factor + w * f;
+            long double w = (original_len * f / full_turn - turns_low) / (turns_high - turns_low);
+            w = w < 0.0L ? 0.0L : w > 1.0L ? 1.0L : w;
+            f = (1.0L - w) * f / factor + w * f;
         }
-        t.turns[i] = f / full_turn;
+        t.turns[i] = (double)(f / full_turn);
     }
     t.cos_t = cos_table;
     t.sin_t = sin_table;

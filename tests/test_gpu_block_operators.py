@@ -176,6 +176,8 @@ ROPE_CASES = [  # T, Hq, Hkv, d, rot, positions, strided
     (77, 6, 2, 96, 48, torch.int32, False), (50, 7, 1, 192, 64, None, True), (40, 8, 2, 256, 256, torch.int64, False),
     (65, 2, 2, 32, 16, None, False), (31, 9, 0, 128, 64, torch.int32, True), (20, 5, 5, 112, 0, None, False),
     (9, 130, 33, 256, 32, None, False),
+    (11, 130, 33, 256, 256, torch.int64, True), (700, 70, 10, 128, 128, torch.int32, False), (3000, 1, 1, 16, 16, torch.int64, False),
+    (6000, 2, 1, 64, 64, torch.int32, True),
 ]
 
 
@@ -520,6 +522,61 @@ def test_joint_amax_in_every_kind_of_grid(T, D):
         fp8.fp8_rope_qkv_fwd(c.qkv, 4, 2, *c.how, q, k, v, amax_out=amax)
         assert amax[0].item() == amax_of(q) and amax[2].item() == amax_of(v)
         assert math.isnan(amax[1].item()) if bad is not None else amax[1].item() == amax_of(k)
+
+
+@pytest.mark.parametrize("T,D", [(1, 16384), (3, 12296), (8, 8200), (5, 4096), (16, 8), (2, 1032)])
+def test_joint_gradient_of_few_rows_without_sums(T, D):
+    """No gammas: the amax takes the other way, a cluster of a few large CTAs among them."""
+    c = JointCase(T, D, fp8.NORM_NONE, fp8.GATE_LINEAR, False)
+    dx, dy, dg, amax = full((T, D)), full((T, D)), full((T, D)), scalar(9e9)
+    ws = ws_of(fp8.fp8_block_norm_bwd_workspace_bytes(T, D))
+    fp8.fp8_block_norm_bwd(None, c.dh, None, c.y, c.gate, None, None, None, None, *c.how, dx, dy, dg, None, None, ws, amax_out=amax)
+    G = c.dh.to(F64)
+    within(dy, c.b * G * c.gate.to(F64), (HALF[BF16] + 8 * U) * (c.b * G * c.gate.to(F64)).abs() + 2.0 ** -126)
+    within(dg, c.b * G * c.y.to(F64), (HALF[BF16] + 8 * U) * (c.b * G * c.y.to(F64)).abs() + 2.0 ** -126)
+    assert amax.item() == amax_of(dy)
+
+
+def test_two_streams_at_once():
+    """Calls side by side, each with its own outputs, workspace and step."""
+    g1, g2 = torch.cuda.Stream(), torch.cuda.Stream()
+    cases = [(RopeCase(3000, 8, 2, 128, 128, fp8.QK_RMS, False, None), JointCase(2000, 2048, fp8.NORM_RMS, None, True),
+              AdamCase([300001, 77, 4096], 8, BF16, seed=s)) for s in (1, 2)]
+    outs = []
+    for (c, j, a), stream in zip(cases, (g1, g2)):
+        q, k, v, dqkv = full((3000, 8, 128)), full((3000, 2, 128)), full((3000, 2, 128)), full((3000, c.W))
+        h, out, dx, dy = (full((2000, 2048)) for _ in range(4))
+        rq, rp, dgq, dgp, am = full((2000,), 0, F32), full((2000,), 0, F32), full((2048,), 0, F32), full((2048,), 0, F32), scalar(0)
+        ws, aws, items = ws_of(fp8.fp8_block_norm_bwd_workspace_bytes(2000, 2048)), ws_of(256), a.items()
+        start = [t.clone() for t in a.tensors()]
+
+        def run(stream, c=c, j=j, a=a, q=q, k=k, v=v, dqkv=dqkv, h=h, out=out, dx=dx, dy=dy, rq=rq, rp=rp, dgq=dgq, dgp=dgp, am=am, ws=ws,
+                aws=aws, items=items):
+            for _ in range(4):
+                fp8.fp8_rope_qkv_fwd(c.qkv, 8, 2, *c.how, q, k, v, stream=stream)
+                fp8.fp8_rope_qkv_bwd(c.dq, c.dk, c.dv, c.qkv, *c.how, dqkv, stream=stream)
+                fp8.fp8_block_norm_fwd(*j.ins(), j.eps, h, out, r_post=rq, r_pre=rp, stream=stream)
+                fp8.fp8_block_norm_bwd(j.dout, j.dh, h, j.y, None, j.gq, j.gp, rq, rp, *j.how, dx, dy, None, dgq, dgp, ws, amax_out=am,
+                                       stream=stream)
+                fp8.fp8_adamw(items, a.lr, a.step, a.b1, a.b2, a.eps, aws, norm=a.norm, max_norm=0.5, seed=7, stream=stream)
+
+        outs.append((run, [q, k, v, dqkv, h, out, dx, dy, dgq, dgp, am], a, start))
+    torch.cuda.synchronize()
+    want = []
+    for run, made, a, start in outs:                               # one after the other
+        run(None)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in made + a.tensors()])
+        for t, s in zip(a.tensors(), start):
+            t.copy_(s)
+        for t in made:
+            t.fill_(2)
+    torch.cuda.synchronize()
+    for (run, *_), stream in zip(outs, (g1, g2)):
+        run(stream)
+    torch.cuda.synchronize()
+    for (_, made, a, _), w in zip(outs, want):
+        assert all(torch.equal(t, x) for t, x in zip(made + a.tensors(), w))
 
 
 def test_joint_rows_of_zeros():
