@@ -60,7 +60,7 @@ struct BnFwd {
 // Rows and columns on threads as in the layer norm: a thread holds KG groups of eight columns of its unit's rows, both gammas of
 // them in registers, and the next rows travel through its private ring.  NT tensors are read (x; y; gate); the sum of squares of
 // y, the joint, its rounding to BF16, the sum of squares of that and the result follow in one pass: every tensor is read once and
-// written once (8192 x 4096 with both norms and codes: 39.5 us in a graph, 235 MB at 5.9 TB/s; 43 with two CTAs per SM for three;
+// written once (8192 x 4096 with both norms and codes: 39.8 us in a graph, 235 MB at 5.9 TB/s; 43 with two CTAs per SM for three;
 // with a gate 49.5 us, 6.1 TB/s).  The reciprocal roots by rsqrtf, off by 2 ulp of FP32 at most.
 template <int KG, RowUnit UNIT, int NT, bool PRE, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd p, int lanes_log2)
@@ -221,7 +221,7 @@ struct BnBwd {
 // dgamma_post = sum dz yh, which a thread keeps in registers for its columns.  The two means are two sums over the row's
 // threads, the second from what the first gives.  Every tensor is read once and written once.  The reciprocal roots go into
 // scalars of the row: the loop forms e r_pre, dz r_post and f r_post and adds multiples of h and y to them, and the gammas lie in
-// shared memory (8192 x 4096 with gate and codes: 106 -> 88 us in a graph, 503 MB at 5.7 TB/s; without a gate 70 us for 369 MB).
+// shared memory (8192 x 4096 with gate and codes: 106 -> 87 us in a graph, 503 MB at 5.8 TB/s; without a gate 70 us for 369 MB).
 // Two barriers per row on 16 warps leave 0.55 instructions per cycle and scheduler; 512 threads with one group each, two CTAs
 // per SM, have to do with 64 registers and spill (120 us).
 // STAGES = 1: the ring holds one row, and a thread asks for the next row's piece as soon as it has read its own: above 8192

@@ -210,7 +210,7 @@ __device__ __forceinline__ void block_max_each(const float (&m)[N], unsigned int
 // A group of lanes takes up to ROPE_HEADS heads of one tensor of one token with the token's angles in registers.  Persistent: a
 // group keeps its heads and walks over the tokens, and what it reads next travels through the threads' private ring.  Bytes
 // bind: every element is read once and written once (8192 tokens of 32 + 2 x 8 heads of 128 with codes: 27.5 us in a graph, 153 MB
-// at 5.6 TB/s; gradient 42.4 us, 237 MB at 5.6 TB/s; with a launch per call and whole-token CTAs that do not stay 47 and 72 us).
+// at 5.6 TB/s; gradient 40.7 us, 237 MB at 5.8 TB/s; with a launch per call and whole-token CTAs that do not stay 47 and 72 us).
 //
 // Instructions are the next bound (23.7 M of a warp at first, 15.6 M now), so the usual case, all lanes of a warp with whole pieces
 // of Q and K or of V, runs through four heads without a branch (33 -> 29.6 us, gradient 59 -> 43); V's pieces lie behind Q's and K's
