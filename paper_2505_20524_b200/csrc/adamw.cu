@@ -442,8 +442,9 @@ static int adamw_check_items(const fp8_adamw_item *items, int n_items)
             set_error("fp8_adamw: item %d: NULL pointer", i);
             return FP8_ERR_NULL;
         }
-        if (!aligned16(it.p) || !aligned16(it.g) || !aligned16(it.m) || !aligned16(it.v) || !aligned16(it.p_bf16) || !aligned16(it.p8)) {
-            set_error("fp8_adamw: item %d: pointers must be 16-byte aligned", i);
+        if (!aligned16(it.p) || !aligned16(it.g) || !aligned16(it.m) || !aligned16(it.v) || !aligned16(it.p_bf16) || !aligned16(it.p8) ||
+            !aligned_to(it.q_scale, 4) || !aligned_to(it.amax, 4)) {
+            set_error("fp8_adamw: item %d: tensors must be 16-byte aligned, q_scale and amax to their type", i);
             return FP8_ERR_ALIGN;
         }
         if (it.n > ((size_t)1 << 40) || !(it.weight_decay >= 0.0f) || isinf(it.weight_decay)) {
@@ -538,7 +539,7 @@ extern "C" int fp8_adamw(const fp8_adamw_item *items, int n_items, const float *
         const bool first = at == 0;
         maxima.n = 0;
         for (; at < n_items && maxima.n < AW_MAXIMA; ++at)
-            if (items[at].amax) maxima.amax[maxima.n++] = reinterpret_cast<unsigned int *>(items[at].amax);
+            if (items[at].n && items[at].amax) maxima.amax[maxima.n++] = reinterpret_cast<unsigned int *>(items[at].amax);
         adamw_begin_kernel<<<1, AW_MAXIMA, 0, st>>>(maxima, first ? s : nullptr, lr, step, log(beta1), log(beta2), norm, max_norm,
                                                     (uint32_t)seed, (uint32_t)(seed >> 32));
         FP8_CUDA_CHECK(cudaGetLastError());

@@ -193,6 +193,7 @@ ADAMW_CASES = [
     (dict(me=None), {}, NULL), (dict(ve=None), {}, NULL), (dict(me=None, ve=None, bits=32), {}, None), (dict(q=None), {}, NULL),
     (dict(q=None, p8=None, p16=None, amax=None), {}, None), (dict(bits=16), {}, ENUM), (dict(fmt=2), {}, ENUM),
     (dict(p=A + 4), {}, ALIGN), (dict(g=A + 2), {}, ALIGN), (dict(m=A + 8), {}, ALIGN), (dict(p16=A + 2), {}, ALIGN), (dict(p8=A + 8), {}, ALIGN),
+    (dict(q=A + 2), {}, ALIGN), (dict(amax=A + 1), {}, ALIGN),
     (dict(me=A + 1, ve=A + 3), {}, None), (dict(wd=-0.1), {}, SHAPE), (dict(wd=NAN), {}, SHAPE), (dict(n=(1 << 40) + 1), {}, SHAPE),
     (dict(n=0, p=None, g=None, bits=5), {}, None),
     ({}, dict(lr=None), NULL), ({}, dict(step=None), NULL), ({}, dict(lr=A + 2), ALIGN), ({}, dict(norm=None, max_norm=NAN), None),

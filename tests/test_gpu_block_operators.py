@@ -753,6 +753,24 @@ def test_adamw(sizes, bits, gdt):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_passes_over_empty_tensors(bits):
+    """Their place in the list still counts: it is part of the random bits' key."""
+    c, d = AdamCase([300, 0, 5000, 0], bits, F32, seed=3), AdamCase([300, 0, 5000, 0], bits, F32, seed=3)
+    c.amax.fill_(5.0)
+    c.call(c.items())
+    d.call(d.items())
+    assert c.step.item() == 5 and c.amax[1].item() == 5.0 and c.amax[3].item() == 5.0
+    assert all(torch.equal(x, y) for x, y in zip(c.p + c.m + c.v, d.p + d.m + d.v))
+    if bits == 8:
+        e = AdamCase([300, 0, 5000, 0], bits, F32, seed=3)
+        m, v = e.moments(2)
+        e.call(e.items())
+        g = e.g[2].to(F64) * (0.5 / (2.0 + 1e-6))
+        new, size = e.b1 * m + (1 - e.b1) * g, e.b1 * m.abs() + (1 - e.b1) * g.abs()
+        check_codes(e.m[2], e.me[2], new, size, random_bits(e.seed, 5, 2, 5000) & 0xFFFF, False)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_from_zero_states_and_without_extras(bits):
     c = AdamCase([1000, 130], bits, F32, p16=False, p8=False, zero=True)
     c.norm = None
