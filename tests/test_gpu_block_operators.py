@@ -503,7 +503,7 @@ def test_joint_sum_in_the_place_of_an_input(T, D, place):
     assert torch.equal(at, h) and torch.equal(o2, out)
 
 
-@pytest.mark.parametrize("T,D", [(16, 4096), (20, 4096), (150, 1032), (33, 64), (257, 256), (529, 256), (8200, 2056)])
+@pytest.mark.parametrize("T,D", [(7, 16384), (8, 12288), (9, 8192), (16, 4096), (20, 4096), (150, 1032), (33, 64), (257, 256), (529, 256), (8200, 2056)])
 def test_joint_amax_in_every_kind_of_grid(T, D):
     """One CTA, one cluster, a memset in front, a kernel beside: NaN and stale values too."""
     x = rnd(gen(T), T, D, dtype=BF16)
