@@ -432,6 +432,7 @@ FP8_API int fp8_rope_qkv_bwd_q(const void *dq_bf16, const void *dk_bf16, const v
  *          y                      FP8_NORM_NONE (gamma_post is not read)
  *   h    = x_scale x + y_scale s z, rounded to BF16;  s = gate (FP8_GATE_LINEAR), sigmoid(gate) (FP8_GATE_SIGMOID), 1 without one
  *   out  = gamma_pre h r_pre, r_pre = 1 / sqrt(mean(h^2) + eps) of the rounded h, rounded to BF16
+ * A gate that is NaN or infinite counts as what the formula makes of it; a sigmoid below 2^-126 is 0.
  * The reciprocal roots come from the hardware's, off by 2 ulp at most; a row of zeros without eps gives NaN, and one whose mean
  * square and eps lie below FP32's normal numbers (2^-126) has no gradient (its reciprocal root's square overflows). */
 enum { FP8_NORM_NONE = 2 };                             /* beside FP8_NORM_RMS and FP8_NORM_LAYERSCALE */

@@ -10,14 +10,16 @@ namespace fp8dpa {
 
 constexpr uint64_t TWO_ONES = 0x3F8000003F800000ull;
 
-// sigmoid(v) of two values, s = 1 / (1 + e) with e = exp(-v), and 1 - s = e s (no cancellation where s is near 1); e stops at
-// 2^126, where the sigmoid is 2^-126.
+// sigmoid(v) of two values, s = 1 / (1 + e) with e = exp(-v), and 1 - s = e s (no cancellation where s is near 1).  A sigmoid below
+// 2^-126 is 0, and the infinity that e may be there is kept out of e s; NaN stays NaN in both.
 __device__ __forceinline__ uint64_t sigmoid2(uint64_t v, uint64_t &rest)
 {
     float a, b;
     unpack_f32x2(mul_f32x2(v, both(-1.4426950408889634f)), a, b);
-    const uint64_t e = pack_f32x2(ex2_approx(fminf(a, 126.0f)), ex2_approx(fminf(b, 126.0f)));
-    unpack_f32x2(add_f32x2(e, both(1.0f)), a, b);
+    a = ex2_approx(a);
+    b = ex2_approx(b);
+    const uint64_t e = pack_f32x2(fminf(a, 8.507059e37f), fminf(b, 8.507059e37f));      // 2^126
+    unpack_f32x2(add_f32x2(pack_f32x2(a, b), both(1.0f)), a, b);
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
     const uint64_t s = pack_f32x2(a, b);

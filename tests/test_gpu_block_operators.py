@@ -614,6 +614,69 @@ def test_joint_beyond_32_bit_offsets():
     assert torch.equal(dx[-40:], dx2)
 
 
+@pytest.mark.parametrize("T,D", [(2, 64), (4, 520), (300, 1600), (20, 4096), (9, 8200), (5, 16384)])
+@pytest.mark.parametrize("mode", [fp8.GATE_LINEAR, fp8.GATE_SIGMOID])
+@pytest.mark.parametrize("post", [fp8.NORM_LAYERSCALE, fp8.NORM_NONE])
+def test_joint_of_gates_that_are_not_finite(T, D, mode, post):
+    """NaN and the two infinities in a gate, element by element: what the formula gives, both ways and in the amax; a closed sigmoid
+    leaves the residual stream and gradients of exactly 0."""
+    c = JointCase(T, D, post, mode, False)
+    c.gate.clamp_(-60, 60)
+    bad = torch.tensor([NAN, math.inf, -math.inf, -200.0], dtype=BF16)
+    places = [(1, 0), (T - 1, D - 4)]
+    for t, j in places:
+        c.gate[t, j:j + 4] = bad
+    s, slope, extra = c.weight()
+    _, z = c.z()
+    h, amax = full((T, D)), scalar(-1)
+    fp8.fp8_block_norm_fwd(*c.ins(), c.eps, h, None, amax_out=amax)
+    G = c.dh.to(F64)
+    dx, dy, dg, dgq, a2 = full((T, D)), full((T, D)), full((T, D)), full((D,), 0, F32) if c.gq is not None else None, scalar(-1)
+    ws = ws_of(fp8.fp8_block_norm_bwd_workspace_bytes(T, D))
+    fp8.fp8_block_norm_bwd(None, c.dh, None, c.y, c.gate, c.gq, None, None, None, *c.how, dx, dy, dg, dgq, None, ws, amax_out=a2)
+    ref = c.a * c.x.to(F64) + c.b * s * z
+    dgate, grad = c.b * G * z * slope, c.b * G * s * (c.gq.to(F64) if c.gq is not None else 1.0)
+    sizes = (ref.abs() + 2 * (c.a * c.x.to(F64)).abs(), dgate.abs(), grad.abs())
+    for got, want, size in zip((h, dg, dy), (ref, dgate, grad), sizes):
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        far = torch.isinf(want)
+        assert torch.equal(got[far].to(F64), want[far])
+        there = torch.isfinite(want)
+        more = extra if isinstance(extra, float) else extra.nan_to_num(0.0, 0.0, 0.0)[there].clamp(max=200.0)
+        within(got[there], want[there], (HALF[BF16] + (64 + 2 * more) * U) * size[there] + 2.0 ** -126)
+    assert math.isnan(amax.item()) and math.isnan(a2.item())
+    if mode == fp8.GATE_SIGMOID:
+        for t, j in places:
+            assert torch.isnan(dg[t, j]) and (dg[t, j + 1:j + 4] == 0).all() and (dy[t, j + 2:j + 4] == 0).all()
+            assert torch.equal(h[t, j + 2:j + 4], (c.a * c.x[t, j + 2:j + 4].float()).to(BF16))
+    scale, h8, h2, d8 = scalar(37.0), full((T, D), 0xEE, U8), full((T, D)), full((T, D), 0xEE, U8)
+    fp8.fp8_block_norm_fwd_q(*c.ins(), c.eps, scale, fp8.E4M3, h2, None, h8)
+    fp8.fp8_block_norm_bwd_q(None, c.dh, None, c.y, c.gate, c.gq, None, None, None, *c.how, scale, fp8.E5M2, dx, None, d8, dg, dgq, None, ws)
+    assert torch.equal(h8, codes_of(h, scale, fp8.E4M3)) and torch.equal(d8, codes_of(dy, scale, fp8.E5M2))
+
+
+@pytest.mark.parametrize("mode", [fp8.GATE_LINEAR, fp8.GATE_SIGMOID])
+def test_joint_row_of_a_broken_gate(mode):
+    """Behind both norms a NaN in a gate is its whole row's, and no other's."""
+    T, D = 40, 1032
+    c, d = (JointCase(T, D, fp8.NORM_RMS, mode, True) for _ in range(2))
+    c.gate[7, 500] = NAN
+    rows = torch.arange(T, device="cuda") != 7
+    made = []
+    for x in (c, d):
+        h, out, rq, rp, amax = full((T, D)), full((T, D)), full((T,), 0, F32), full((T,), 0, F32), scalar(-1)
+        fp8.fp8_block_norm_fwd(*x.ins(), x.eps, h, out, r_post=rq, r_pre=rp, amax_out=amax)
+        dx, dy, dg, dgq, dgp, a2 = full((T, D)), full((T, D)), full((T, D)), full((D,), 0, F32), full((D,), 0, F32), scalar(-1)
+        fp8.fp8_block_norm_bwd(x.dout, x.dh, h, x.y, x.gate, x.gq, x.gp, rq, rp, *x.how, dx, dy, dg, dgq, dgp,
+                               ws_of(fp8.fp8_block_norm_bwd_workspace_bytes(T, D)), amax_out=a2)
+        made.append((h, out, rp, dx, dy, dg, amax, a2, dgq, dgp))
+    for got, want in zip(made[0][:6], made[1][:6]):
+        assert torch.equal(got[rows], want[rows])
+    h, out, rp, dx, dy, dg, amax, a2, dgq, dgp = made[0]
+    assert torch.isnan(h[7]).sum() == 1 and torch.isnan(rp[7]) and all(torch.isnan(x[7]).all() for x in (out, dx, dy, dg))
+    assert math.isnan(amax.item()) and math.isnan(a2.item()) and torch.isnan(dgq).all() and torch.isnan(dgp).all()
+
+
 # ------------------------------------------------------------------------------------------------ AdamW
 def mix(x):
     x = ((x ^ (x >> 16)) * 0x9E3779B9) & 0xFFFFFFFF
