@@ -534,7 +534,8 @@ FP8_API int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *
  *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
  *   p = p (1 - *lr weight_decay) - *lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
  * and *step = t.  A norm that is NaN or infinite skips the step: nothing is changed, *step and the outputs neither.  (Without norm
- * a gradient that is not finite makes its element NaN, that one alone.)
+ * a gradient that is not finite makes its element NaN, that one alone.  A finite one whose square is over FP32's range leaves an
+ * infinite v, under which p only decays, from then on; in 8 bits it is stored as NaN, which counts as infinite there.)
  * Outputs (nullable): p_bf16 the rounded weights, p8 = FP8cast(*q_scale * p_bf16) in `fmt` (bit-identical to fp8_cast of p_bf16),
  * *amax = amax(p_bf16): what fp8_quantize_delayed_multi would take another pass for.
  *

@@ -202,6 +202,13 @@ __device__ __forceinline__ float reciprocal(float v)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+// The same, and 0 of NaN: root2 makes NaN of an infinite second moment, and 8 bits store one as NaN, but an infinite root moves
+// nothing.  (A gradient that is NaN or infinite has made the first moment so, too: the element is NaN all the same.)
+__device__ __forceinline__ float reciprocal_or_zero(float v)
+{
+    asm("min.f32 %0, %0, %1;" : "+f"(v) : "f"(INFINITY));
+    return reciprocal(v);
+}
 __device__ __forceinline__ uint32_t half_bits(uint64_t v, int i)
 {
     float lo, hi;
@@ -352,7 +359,9 @@ __device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned 
             }
             float lo, hi;
             unpack_f32x2(fma_f32x2(r[e], both(s.inv_root), both(a.eps)), lo, hi);
-            w[e] = fma_f32x2(mul_f32x2(m[e], pack_f32x2(reciprocal(lo), reciprocal(hi))), both(-s.rate),
+            lo = EIGHT ? reciprocal_or_zero(lo) : reciprocal(lo);
+            hi = EIGHT ? reciprocal_or_zero(hi) : reciprocal(hi);
+            w[e] = fma_f32x2(mul_f32x2(m[e], pack_f32x2(lo, hi)), both(-s.rate),
                              mul_f32x2(pack_f32x2(x.w[2 * e], x.w[2 * e + 1]), keep));
             most = absmax3(most, w[e]);
             unpack_f32x2(w[e], x.w[2 * e], x.w[2 * e + 1]);

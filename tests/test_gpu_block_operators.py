@@ -906,6 +906,28 @@ def test_adamw_8_bit_moments_over_the_range_of_scales(scale):
         check_codes(c.v[0], c.ve[0], v.sqrt(), v.sqrt(), random_bits(c.seed, 5, 0, 1000) >> 16, True)
 
 
+@pytest.mark.parametrize("bad", [1e30, -3e38])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_of_squares_that_overflow(bad, bits):
+    """A finite gradient whose square is over FP32's range: an infinite second moment moves nothing, in this step and in the next
+    ones, whatever the moments' width; the weight only decays."""
+    c = AdamCase([8, 700], bits, F32)
+    c.norm = None
+    c.g[1][200] = bad
+    p0 = c.p[1].to(F64)
+    items = c.items()
+    decay = 1.0 - float(np.float32(3e-4)) * float(np.float32(c.decay[1]))
+    for step in range(1, 4):
+        c.call(items)
+        assert abs(c.p[1][200].item() - p0[200].item() * decay ** step) <= 4 * step * U * abs(p0[200].item())
+        assert all(torch.isfinite(x).all() for x in c.p)
+        assert torch.equal(c.p16[1], c.p[1].to(BF16)) and c.amax[1].item() == amax_of(c.p16[1])
+        assert torch.equal(c.p8[1], codes_of(c.p16[1], c.q[1:2], fp8.E4M3))
+        c.g[1][200] = 1e-3
+    if bits == 32:
+        assert c.v[1][200].item() == math.inf
+
+
 def test_adamw_random_rounding_is_unbiased_and_repeats():
     """Small changes of a large second moment: rounded to nearest they would be lost.  2^20 values between two codes: the mean
     of the stored values is within 5 deviations (step / 2 / 2^10 each) of the value, the two codes are the neighbours."""
