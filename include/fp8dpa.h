@@ -397,7 +397,9 @@ typedef struct {
  *   FP8_ROPE_NTK       base * factor^(rot / (rot - 2)) in place of base
  *   FP8_ROPE_BY_PARTS  (1 - w) f_i / factor + w f_i with w = (n_i - turns_low) / (turns_high - turns_low) clamped to [0, 1], n_i =
  *                      original_len f_i / 2 pi: the turns of the pair over the length that the model was trained with
- * Angles are formed in 64 bits; entries are good to 2 ulp of binary32 for every position.  rot % 16 == 0, rot <= 256. */
+ * Entries are good to 2 ulp of binary32 for every position, next to zeros too (with a magnitude other than 1, one more):
+ * frequencies and angles have over 90 bits.  No pair may make more than 2^31 turns in n_pos positions (base >= 1 and factor >= 1 never
+ * do).  rot % 16 == 0, rot <= 256, n_pos < 2^31. */
 enum { FP8_ROPE_PLAIN = 0, FP8_ROPE_LINEAR = 1, FP8_ROPE_NTK = 2, FP8_ROPE_BY_PARTS = 3 };
 FP8_API int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, double factor, double original_len, double turns_low,
                    double turns_high, double magnitude, float *cos_table, float *sin_table, void *stream);

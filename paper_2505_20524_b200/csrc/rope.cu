@@ -11,42 +11,55 @@ namespace fp8dpa {
 // ---------------------------------------------------------------- table
 constexpr int ROPE_MAX_PAIRS = 128;
 struct RopeTable {
-    double turns[ROPE_MAX_PAIRS];        // turns of each pair per position
+    double turns[ROPE_MAX_PAIRS];        // turns of each pair per position, and what its rounding to 64 bits left out
+    double rest[ROPE_MAX_PAIRS];
     float *cos_t, *sin_t;
     size_t rows;
     int pairs;
     float magnitude;
 };
 
-// sin and cos of two angles of at most pi / 4 in size: their Taylor series up to the powers 9 and 10, of which the next terms
-// are 1.8e-9 and 1.1e-10 there.
+// sin and cos of two angles of at most an eighth of a turn, in turns: their Taylor series up to the powers 9 and 10, of which the
+// next terms are 1.8e-9 and 1.1e-10 there, with the powers of 2 pi in the coefficients and the rounding of 2 pi itself in the sine's
+// second one.
 __device__ __forceinline__ void sincos2(uint64_t x, uint64_t &sn, uint64_t &cs)
 {
-    const auto k = [](float v) { return pack_f32x2(v, v); };
+    constexpr double T = 6.283185307179586, T2 = T * T, T4 = T2 * T2, T8 = T4 * T4;
+    constexpr float FULL = (float)T;
+    const auto k = [](double v) { return pack_f32x2((float)v, (float)v); };
     const uint64_t q = mul_f32x2(x, x);
-    uint64_t s = fma_f32x2(q, k(1.0f / 362880.0f), k(-1.0f / 5040.0f));
-    s = fma_f32x2(s, q, k(1.0f / 120.0f));
-    s = fma_f32x2(s, q, k(-1.0f / 6.0f));
-    sn = fma_f32x2(mul_f32x2(s, q), x, x);
-    uint64_t c = fma_f32x2(q, k(-1.0f / 3628800.0f), k(1.0f / 40320.0f));
-    c = fma_f32x2(c, q, k(-1.0f / 720.0f));
-    c = fma_f32x2(c, q, k(1.0f / 24.0f));
-    c = fma_f32x2(c, q, k(-0.5f));
-    cs = fma_f32x2(c, q, k(1.0f));
+    uint64_t s = fma_f32x2(q, k(T8 * T / 362880.0), k(-T4 * T2 * T / 5040.0));
+    s = fma_f32x2(s, q, k(T4 * T / 120.0));
+    s = fma_f32x2(s, q, k(-T2 * T / 6.0));
+    s = fma_f32x2(s, q, k(T - FULL));
+    sn = fma_f32x2(x, k(FULL), mul_f32x2(s, x));
+    uint64_t c = fma_f32x2(q, k(-T8 * T2 / 3628800.0), k(T8 / 40320.0));
+    c = fma_f32x2(c, q, k(-T4 * T2 / 720.0));
+    c = fma_f32x2(c, q, k(T4 / 24.0));
+    c = fma_f32x2(c, q, k(-T2 / 2.0));
+    cs = fma_f32x2(c, q, k(1.0));
 }
 
-// The angle in turns is a product in 64 bits, good to 2^-52 of itself; what is left of it next to the nearest quarter turn is
-// rounded to FP32, so that cos and sin are good to 2 ulp wherever the position lies, next to their zeros too.  Adding 1.5 * 2^52
-// leaves the nearest whole number of quarters in the low bits (2^31 turns at most).
-// A thread keeps four frequencies and walks over the positions (131072 x 64: 12.0 us in a graph, 67 MB at 5.6 TB/s; 34 us with the
-// frequencies read from the launch's parameters at every place, where lanes ask for different ones).
+// The angle in turns is the product of the position and a frequency kept as the sum of two doubles.  Adding 1.5 * 2^50 to the first's
+// product leaves the nearest whole number of quarters (2^31 turns at most), in the low bits of the sum too.  What is left of the angle
+// is the exact product less those, rounded once, and the second's product, so that nothing is lost next to a quarter turn: entries
+// are good to 2 ulp (1.3 seen) wherever the position lies, next to their zeros too.  (A product rounded to 64 bits is off by 2^-53 of
+// all turns: its cosine next to a zero by 2291 ulp below position 2^20, by 10^5 further out.)
+// A thread keeps four frequencies, which one thread each brings to shared memory (lanes that ask the launch's parameters for different
+// words wait for one another: 11.5 us for 131072 x 64 in a graph, 67 MB at 5.8 TB/s, and 15.3 without), and walks over the positions.
 __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__ RopeTable t)
 {
     const unsigned quads = t.pairs / 4, wide = 256 / quads, q = threadIdx.x % quads;
+    __shared__ double2 frequency[4][ROPE_MAX_PAIRS / 4];
+    if (threadIdx.x < t.pairs) frequency[threadIdx.x & 3][threadIdx.x >> 2] = make_double2(t.turns[threadIdx.x], t.rest[threadIdx.x]);
+    __syncthreads();
     if (threadIdx.x >= wide * quads) return;
-    double f[4];
+    double f[4], f_rest[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = t.turns[4 * q + e];
+    for (int e = 0; e < 4; ++e) {
+        f[e] = frequency[e][q].x;
+        f_rest[e] = frequency[e][q].y;
+    }
     const unsigned step = gridDim.x * wide;
 #pragma unroll 2
     for (unsigned pos = blockIdx.x * wide + threadIdx.x / quads; pos < t.rows; pos += step) {
@@ -55,9 +68,9 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const __grid_constant__
         int k[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const double turns = at * f[e], shifted = fma(4.0, turns, 6755399441055744.0);
+            const double shifted = fma(at, f[e], 1688849860263936.0), quarters = shifted - 1688849860263936.0;
             k[e] = __double2loint(shifted);
-            x[e] = (float)fma(-0.25, shifted - 6755399441055744.0, turns) * 6.2831853071795865f;
+            x[e] = (float)fma(at, f_rest[e], fma(at, f[e], -quarters));
         }
 #pragma unroll
         for (int e = 0; e < 4; e += 2) {
@@ -672,6 +685,50 @@ static int check_codes(const char *who, const void *scale, int fmt, bool any)
     return FP8_OK;
 }
 
+// A number as the sum of two doubles that do not overlap: about 2^-104 of itself.
+struct Wide {
+    double hi, lo;
+};
+static Wide wide(double a) { return {a, 0.0}; }
+static Wide wide_sum(double a, double b)
+{
+    const double s = a + b, t = s - a;
+    return {s, (a - (s - t)) + (b - t)};
+}
+static Wide negative(Wide a) { return {-a.hi, -a.lo}; }
+static Wide operator+(Wide a, Wide b)
+{
+    const Wide s = wide_sum(a.hi, b.hi);
+    return wide_sum(s.hi, s.lo + (a.lo + b.lo));
+}
+static Wide operator*(Wide a, Wide b)
+{
+    const double p = a.hi * b.hi;
+    return wide_sum(p, fma(a.hi, b.hi, -p) + (a.hi * b.lo + a.lo * b.hi));
+}
+static Wide operator/(Wide a, Wide b)
+{
+    const double q = a.hi / b.hi;
+    return wide_sum(q, (a + negative(wide(q) * b)).hi / b.hi);
+}
+// x^(-1 / n): Newton's iteration y + y (1 - x y^n) / n from the nearest doubles, whose error it squares.  Whole n-th powers of two
+// are taken out of x first, so that no power of y leaves the doubles' range.
+static Wide inverse_root(double x, int n)
+{
+    int e;
+    x = frexp(x, &e);
+    const int out = (e - (e < 0 ? n - 1 : 0)) / n;                // e / n, rounded down
+    x = ldexp(x, e - n * out);
+    Wide y = wide(pow(x, -1.0 / n));
+    for (int i = 0; i < 2; ++i) {
+        Wide product = wide(x), square = y;
+        for (int k = n; k > 0; k >>= 1, square = square * square)
+            if (k & 1) product = product * square;
+        y = y + y * ((wide(1.0) + negative(product)) / wide(n));
+    }
+    return {ldexp(y.hi, -out), ldexp(y.lo, -out)};
+}
+
 }  // namespace fp8dpa
 
 using namespace fp8dpa;
@@ -689,7 +746,7 @@ extern "C" int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, d
     }
     const bool scaled = scaling != FP8_ROPE_PLAIN, parts = scaling == FP8_ROPE_BY_PARTS;
     if (n_pos == 0 || n_pos > 0x7FFFFFFFull || rot <= 0 || rot % 16 || rot > 2 * ROPE_MAX_PAIRS || !(base > 0.0) || isinf(base) ||
-        !(magnitude > 0.0) || isinf(magnitude) || (scaled && (!(factor > 0.0) || isinf(factor))) ||
+        !(magnitude > 0.0) || isinf((float)magnitude) || (scaled && (!(factor > 0.0) || isinf(factor))) ||
         (parts && (!(original_len > 0.0) || isinf(original_len) || !(turns_high > turns_low) || isinf(turns_high) || isinf(turns_low)))) {
         set_error("fp8_rope_table: unsupported n_pos=%zu rot=%d (rot %% 16 == 0, rot <= 256) or a parameter that is not a positive "
                   "number", n_pos, rot);
@@ -699,24 +756,32 @@ extern "C" int fp8_rope_table(size_t n_pos, int rot, double base, int scaling, d
         set_error("fp8_rope_table: tables must be 16-byte aligned");
         return FP8_ERR_ALIGN;
     }
+    RopeTable t = {};
+    // Turns per position: powers of one ratio, of which 127 products in a row leave less than 2^-90 of error (positions below 2^31 need
+    // that next to zeros).
+    const Wide one = wide(1.0), share = scaling == FP8_ROPE_LINEAR || parts ? one / wide(factor) : one;
+    const Wide span = parts ? one / wide_sum(turns_high, -turns_low) : one;
+    Wide f = {0.15915494309189535, -9.839338337591243e-18}, ratio = inverse_root(base, rot / 2);             // 1 / 2 pi
+    if (scaling == FP8_ROPE_NTK) ratio = ratio * inverse_root(factor, (rot - 2) / 2);      // factor^(-2 / (rot - 2))
+    if (scaling == FP8_ROPE_LINEAR) f = f * share;
+    bool too_many = false;
+    for (int i = 0; i < rot / 2; ++i, f = f * ratio) {
+        Wide turns = f;
+        if (parts) {
+            const Wide w = (f * wide(original_len) + wide(-turns_low)) * span;
+            if (w.hi <= 0.0) turns = f * share;
+            else if (!(w.hi >= 1.0)) turns = (one + negative(w)) * f * share + w * f;
+        }
+        t.turns[i] = turns.hi;
+        t.rest[i] = turns.lo;
+        too_many |= !(turns.hi * (double)n_pos <= 2147483648.0);
+    }
+    if (too_many) {
+        set_error("fp8_rope_table: base=%g and factor=%g make more than 2^31 turns in %zu positions", base, factor, n_pos);
+        return FP8_ERR_SHAPE;
+    }
     int rc = check_arch();
     if (rc != FP8_OK) return rc;
-    RopeTable t = {};
-    // powers of one ratio in 80 bits: 127 products in a row leave less than 2^-56 of error, in the time of two calls of pow
-    const long double full_turn = 6.28318530717958647692529L;
-    long double power_of = base, f_i = 1.0L;
-    if (scaling == FP8_ROPE_NTK) power_of *= powl(factor, rot / (rot - 2.0L));
-    const long double ratio = powl(power_of, -2.0L / rot);
-    for (int i = 0; i < rot / 2; ++i, f_i *= ratio) {
-        long double f = f_i;
-        if (scaling == FP8_ROPE_LINEAR) f /= factor;
-        if (parts) {
-            long double w = (original_len * f / full_turn - turns_low) / (turns_high - turns_low);
-            w = w < 0.0L ? 0.0L : w > 1.0L ? 1.0L : w;
-            f = (1.0L - w) * f / factor + w * f;
-        }
-        t.turns[i] = (double)(f / full_turn);
-    }
     t.cos_t = cos_table;
     t.sin_t = sin_table;
     t.rows = n_pos;

@@ -242,3 +242,20 @@ def test_structures_have_the_header_layout(tmp_path):
     out = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split("\n")
     for st, line in zip(pairs.values(), out):
         assert [C.sizeof(st)] + [getattr(st, f[0]).offset for f in st._fields_] == [int(v) for v in line.split()]
+
+
+MANY_TURNS = [  # pairs that turn too often for the table's arithmetic, ones next to them that do not, a magnitude over FP32's range
+    (dict(kind=0, base=1e-12, n_pos=1000), SHAPE), (dict(kind=0, base=1e-12, n_pos=1, rot=16), SHAPE), (dict(kind=0, base=1e-300), SHAPE),
+    (dict(kind=0, base=1e-7, n_pos=1000), None), (dict(kind=0, base=1e300), None), (dict(kind=1, factor=1e-12, n_pos=10000), SHAPE),
+    (dict(kind=1, factor=1e-3, n_pos=10000), None), (dict(kind=2, factor=1e-30), SHAPE), (dict(kind=3, factor=1e-9, n_pos=1000), SHAPE),
+    (dict(kind=0, base=1.0, n_pos=(1 << 31) - 1), None), (dict(kind=0, base=5e-324), SHAPE), (dict(kind=1, factor=5e-324), SHAPE),
+    (dict(kind=2, factor=5e-324, base=1e308), SHAPE), (dict(kind=0, base=1.7e308, rot=256), None), (dict(kind=3, length=1e308, factor=1e308), None),
+    (dict(mag=1e39), SHAPE), (dict(mag=3e38), None),
+]
+
+
+@pytest.mark.parametrize("i", range(len(MANY_TURNS)))
+def test_rope_table_refuses_more_turns_than_it_counts(lib, i):
+    change, status = MANY_TURNS[i]
+    rc = lib.fp8_rope_table(*(TABLE | change).values())
+    assert rc in OK_ARGS_STATUS if status is None else rc == status, (change, rc, lib.fp8_last_error())

@@ -8,6 +8,7 @@ exponential of the sigmoid is off by 2^-22 of itself plus 2 u |gate| through its
 few products around them every FP32 value below is off by less than 64 u of the magnitudes that went into it, (64 + 2 |gate|) u with
 a sigmoid, on top of one rounding to the output's type.
 """
+import decimal
 import math
 
 import numpy as np
@@ -91,6 +92,64 @@ def test_rope_table(N, rot, kind, magnitude):
     for got, ref in ((cos, angle.cos()), (sin, angle.sin())):
         within(got, ref * magnitude, (6 * U * ref.abs() + 8 * 2.0 ** -53 * angle) * magnitude)
     assert (cos[0] == np.float32(magnitude)).all() and (sin[0] == 0).all()
+
+
+def exact_turns(rot, base, kind=fp8.ROPE_PLAIN, factor=1.0, length=1.0, low=0.0, high=1.0, bits=160):
+    """Turns per position of each pair, times 2^bits, as whole numbers: from decimals of 80 digits."""
+    with decimal.localcontext() as ctx:
+        ctx.prec = 80
+        D = decimal.Decimal
+        full_turn = 2 * D("3.1415926535897932384626433832795028841971693993751058209749445923078164062862090")
+        out = []
+        for i in range(rot // 2):
+            b = D(base) * D(factor) ** (D(rot) / (rot - 2)) if kind == fp8.ROPE_NTK else D(base)
+            f = b ** (D(-2 * i) / rot)
+            if kind == fp8.ROPE_LINEAR:
+                f /= D(factor)
+            if kind == fp8.ROPE_BY_PARTS:
+                w = min(D(1), max(D(0), (D(length) * f / full_turn - D(low)) / (D(high) - D(low))))
+                f = (1 - w) * f / D(factor) + w * f
+            out.append(int((f / full_turn * 2 ** bits).to_integral_value()))
+        return out
+
+
+def exact_cos_sin(turns, pos, bits=160):
+    """cos and sin of a position's angle: what is left of it next to the nearest quarter turn is exact before it becomes a float."""
+    quarter = 1 << (bits - 2)
+    k = (turns * pos + quarter // 2) // quarter
+    x = (turns * pos - k * quarter) / (1 << bits) * (2 * math.pi)
+    c, s = math.cos(x), math.sin(x)
+    return ((c, s), (-s, c), (-c, -s), (s, -c))[k % 4]
+
+
+# numerators of fractions next to pi and its half: a sine or a cosine next to 0 at frequency 1
+NEAR_ZEROS = [11, 22, 333, 344, 355, 51819, 52174, 103993, 104348, 208341, 312689, 573204, 833719, 1146408, 4272943, 5419351, 80143857]
+
+
+@pytest.mark.parametrize("N,rot,base,kind,factor", [
+    (131072, 128, 500000.0, fp8.ROPE_BY_PARTS, 16.0), (1 << 21, 64, 10000.0, fp8.ROPE_PLAIN, 1.0), (80143858, 16, 10000.0, fp8.ROPE_PLAIN, 1.0),
+    (1 << 20, 32, 10000.0, fp8.ROPE_NTK, 8.0), (1 << 19, 256, 10000.0, fp8.ROPE_LINEAR, 7.0),
+    (8192, 64, 2.0 ** -20, fp8.ROPE_PLAIN, 1.0), (1 << 20, 16, 1.0, fp8.ROPE_LINEAR, 2.0 ** -13)])   # many turns per position
+def test_rope_table_to_two_ulp(N, rot, base, kind, factor):
+    """Entries next to the zeros of both functions and far out, against angles in 160 bits."""
+    half = rot // 2
+    cos, sin = full((N, half), NAN, F32), full((N, half), NAN, F32)
+    fp8.fp8_rope_table(cos, sin, base, kind, factor, 8192.0, 1.0, 32.0)
+    turns = exact_turns(rot, base, kind, factor, 8192.0, 1.0, 32.0)
+    rng = np.random.default_rng(N + rot)
+    rows = sorted({x for x in NEAR_ZEROS if x < N} | {int(x) for x in rng.integers(0, N, 300)} | {0, N - 1})
+    # and where the table itself is smallest
+    for t in (cos, sin):
+        rows += t[1:].abs().amin(1).topk(min(100, N - 1), largest=False).indices.add(1).tolist()
+    at = torch.tensor(rows, device="cuda")
+    want = np.array([[exact_cos_sin(f, r) for f in turns] for r in rows])
+    for j, table in enumerate((cos, sin)):
+        ref, got = want[..., j], table[at].cpu().numpy().astype(np.float64)
+        ulp = np.ldexp(1.0, np.frexp(ref)[1] - 24)
+        ulp[ref == 0] = 0.0
+        off = np.abs(got - ref) - 2 * ulp
+        worst = np.unravel_index(off.argmax(), off.shape)
+        assert off.max() <= 0, (rows[worst[0]], worst[1], got[worst], ref[worst], (np.abs(got - ref) / np.maximum(ulp, 1e-300)).max())
 
 
 # ------------------------------------------------------------------------------------------------ rotary positions
