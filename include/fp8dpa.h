@@ -543,10 +543,10 @@ FP8_API int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *
  *
  * state_bits = 32: m, v: n binary32.  state_bits = 8: m: n E4M3 codes, v: n E4M3 codes of sqrt(v), in blocks of 128 consecutive
  * elements with a scale 2^(m_exp[i / 128] - 127), 2^(v_exp[i / 128] - 127): the smallest power of two (2^-126 at least) that leaves no
- * value above 448.  m, v and the root of v take one rounding per operation in the order written above (a sum below FP32's normal
- * numbers is 0), so that codes are the same wherever they are worked out.  The update uses the values before they are stored.  A
- * stored value is rounded towards zero or away from it
- * with the probability of the part cut off, from 16 random bits each: the lower (m) and upper (v) half of
+ * value above 448.  m, v and the root of v take one rounding per operation in the order written above, so that codes
+ * are the same wherever they are worked out; a term or a sum of m or v below FP32's normal numbers (2^-126) counts as 0, and the root
+ * of a v below 2^-102 may be the nearest value's neighbour.  The update uses the values before they are stored.  A stored value is
+ * rounded towards zero or away from it with the probability of the part cut off, from 16 random bits each: the lower (m) and upper (v) half of
  * mix(mix(mix(K + item) + (i >> 32)) + i) modulo 2^32, K = mix(mix(mix(seed) ^ (seed >> 32)) ^ t), with mix(x): x = (x ^ x >> 16) *
  * 0x9E3779B9; x = (x ^ x >> 15) * 0x6A09E667; x ^ x >> 16, item the number in the list; the same seed and step give the same
  * codes.  v above zero is stored as the smallest code at least.  New states: zeros (all bytes).

@@ -177,7 +177,7 @@ __device__ __forceinline__ void decode8(uint2 codes, float scale, uint64_t (&f)[
     }
 }
 // A sum that stays one: the compiler makes one rounding of a product and a sum of pairs, but not where they treat small numbers
-// differently (0.9 m + 0.1 g in one rounding moved 181 of 218 M codes).
+// differently (0.9 m + 0.1 g in one rounding moved 181 of 218 M codes).  Terms and sums below the normal numbers are 0.
 __device__ __forceinline__ uint64_t add_ftz2(uint64_t a, uint64_t b)
 {
     uint64_t r;
@@ -186,7 +186,8 @@ __device__ __forceinline__ uint64_t add_ftz2(uint64_t a, uint64_t b)
 }
 // Square roots of two values that are 0 or normal numbers: the hardware's reciprocal root and one step of Newton's iteration on
 // r^2 = v, r - (r^2 - v) / (2 r), with the difference exact: the correctly rounded root but where that lies within 2^-44 of the
-// middle of two values.
+// middle of two values (none of 8.4 M mantissas from 2^-102 on).  Below 2^-102 the difference has fewer bits, and the root may be the
+// next value (of 2^-126 to 2^-125 a tenth are).  NaN of infinity.
 __device__ __forceinline__ uint64_t root2(uint64_t v)
 {
     float a, b, qa, qb;
@@ -345,7 +346,7 @@ __device__ __forceinline__ void adamw_chunk(const AdamTable &t, int k, unsigned 
             const uint64_t rest = EIGHT ? m[e] : mul_f32x2(both(a.beta1), m[e]), new_m = mul_f32x2(both(a.rest1), g);
             const uint64_t old = mul_f32x2(both(a.beta2), v[e]), more = mul_f32x2(mul_f32x2(both(a.rest2), g), g);
             if constexpr (EIGHT) {
-                m[e] = add_ftz2(rest, new_m);                // below the normal numbers: 0
+                m[e] = add_ftz2(rest, new_m);
                 v[e] = add_ftz2(old, more);
                 r[e] = root2(v[e]);
             } else {

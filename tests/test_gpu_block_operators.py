@@ -987,6 +987,41 @@ def test_adamw_of_squares_that_overflow(bad, bits):
         assert c.v[1][200].item() == math.inf
 
 
+def test_adamw_8_bit_moments_next_to_the_smallest_numbers():
+    """Terms and sums below FP32's normal numbers (2^-126) count as 0 with moments of 8 bits, beside an old moment above them too.
+    The roots' values are FP32's next to the formula's: codes are compared away from the rounding's borders."""
+    n = 1280
+    c = AdamCase([n], 8, F32)
+    c.norm = None
+    tiny = 2.0 ** -126
+    c.v[0].fill_(0x3A), c.ve[0].fill_(64)                          # roots of 1.25 * 2^-63
+    c.m[0].fill_(0x38), c.me[0].fill_(6)                           # 2^-121
+    v_old, m_old = 1.5625 * tiny, 32.0 * tiny
+    small = torch.arange(n, device="cuda") % 2 == 0                # every other new term lies below the normal numbers
+    c.g[0].copy_(torch.where(small, math.sqrt(0.5 * tiny / 0.001), math.sqrt(4.0 * tiny / 0.001)))
+    g = c.g[0].to(F64)
+    c.call(c.items())
+    terms = (1 - c.b2) * g * g
+    v = c.b2 * v_old + torch.where(terms < tiny, 0.0, terms)
+    assert torch.equal(terms < tiny, small)
+    r = random_bits(c.seed, 5, 0, n)
+    check_codes(c.v[0], c.ve[0], v.sqrt(), v.sqrt(), r >> 16, True)
+    m = c.b1 * m_old + (1 - c.b1) * g
+    check_codes(c.m[0], c.me[0], m, m.abs(), r & 0xFFFF, False)
+    # first moments: new terms of half the smallest normal number beside an old one above it, and alone
+    c = AdamCase([n], 8, F32)
+    c.norm = None
+    c.v[0].fill_(0x38), c.ve[0].fill_(120)
+    c.m[0].copy_(torch.where(small, 0x40, 0).to(U8)), c.me[0].fill_(1)
+    c.g[0].fill_(5.0 * tiny)                                       # a tenth of it is tiny / 2
+    c.call(c.items())
+    got = decode(c.m[0], c.me[0], n)
+    kept = 0.9 * 2.0 * tiny
+    r = random_bits(c.seed, 5, 0, n)
+    assert (got[~small] == 0).all()
+    check_codes(c.m[0], c.me[0], torch.where(small, kept, 0.0).to(F64), torch.where(small, kept, 0.0).to(F64), r & 0xFFFF, False)
+
+
 def test_adamw_random_rounding_is_unbiased_and_repeats():
     """Small changes of a large second moment: rounded to nearest they would be lost.  2^20 values between two codes: the mean
     of the stored values is within 5 deviations (step / 2 / 2^10 each) of the value, the two codes are the neighbours."""
