@@ -465,7 +465,8 @@ FP8_API int fp8_block_norm_fwd_q(const void *x_bf16, const void *y_bf16, const v
  *   dgate = y_scale G z s',  dz = y_scale G s,  dgamma_post (+)= sum over rows of dz yh
  *   dy = r_post (f - yh mean(f yh)) with f = gamma_post dz  (FP8_NORM_LAYERSCALE: f;  FP8_NORM_NONE: dz)
  * dx, dy, dgate: [T,D] BF16; dx may be dh or dout itself, dy may be y, dgate may be gate; dgamma_*: D binary32, added to with
- * `accumulate`, sums over rows in FP32 in a fixed order.  y NULL: dx alone (dy, dgate NULL).  *amax_out (nullable): amax(dy), the
+ * `accumulate`, sums over rows in FP32 in a fixed order.  y NULL: dx alone (dy, dgate, amax_out NULL); gate NULL: dgate NULL;
+ * dgamma_* without its gamma is not touched.  *amax_out (nullable): amax(dy), the
  * operand of the block's last gradient products; _q: its codes dy8 (dy_bf16 may be NULL).  ws: scratch of
  * fp8_block_norm_bwd_workspace_bytes(T, D), 256-byte aligned; calls that share it must be ordered. */
 FP8_API size_t fp8_block_norm_bwd_workspace_bytes(size_t T, size_t D);

@@ -673,8 +673,8 @@ static int bn_bwd(const char *who, const void *dout, const void *dh, const void 
                   "and gate need)", who);
         return FP8_ERR_NULL;
     }
-    if ((!pre && dout) || (!y && (dy || dy8))) {
-        set_error("%s: dout goes with gamma_pre, and gradients of y with y", who);
+    if ((!pre && dout) || (!y && (dy || dy8 || amax_out)) || (!gate && dgate)) {
+        set_error("%s: dout goes with gamma_pre, gradients of y and their amax with y, and dgate with a gate", who);
         return FP8_ERR_SHAPE;
     }
     if (!aligned16(dout) || !aligned16(dh) || !aligned16(h) || !aligned16(y) || !aligned16(gate) || !aligned16(gamma_post) ||
@@ -712,7 +712,7 @@ static int bn_bwd(const char *who, const void *dout, const void *dh, const void 
     p.dy = static_cast<uint16_t *>(dy);
     p.dgate = static_cast<uint16_t *>(dgate);
     p.partial = pre || scaled ? static_cast<float *>(ws) : nullptr;
-    unsigned int *const amax = reinterpret_cast<unsigned int *>(y ? amax_out : nullptr);
+    unsigned int *const amax = reinterpret_cast<unsigned int *>(amax_out);
     p.maxima = p.partial && amax ? reinterpret_cast<unsigned int *>(p.partial + (size_t)s.grid * 2 * D) : nullptr;
     p.amax_bits = p.maxima ? nullptr : amax;
     p.q_scale = q_scale;

@@ -259,3 +259,18 @@ def test_rope_table_refuses_more_turns_than_it_counts(lib, i):
     change, status = MANY_TURNS[i]
     rc = lib.fp8_rope_table(*(TABLE | change).values())
     assert rc in OK_ARGS_STATUS if status is None else rc == status, (change, rc, lib.fp8_last_error())
+
+
+OUTPUTS_OF_NOTHING = [  # outputs that nothing would be written to
+    (dict(y=None, gate=None, dy=None, dgate=None, amax=A), SHAPE), (dict(gate=None), SHAPE), (dict(gate=None, dgate=None), None),
+    (dict(gate=None, amax=A), SHAPE), (dict(gate=None, dgate=None, amax=A), None), (dict(y=None, gate=None, dy=None), SHAPE),
+]
+
+
+@pytest.mark.parametrize("i", range(len(OUTPUTS_OF_NOTHING)))
+def test_joint_gradient_refuses_outputs_of_what_is_not_there(lib, i):
+    change, status = OUTPUTS_OF_NOTHING[i]
+    args = GRAD | change
+    args["cfg"] = C.byref(binding.BlockNorm(*CFG.values()))
+    rc = lib.fp8_block_norm_bwd(*args.values())
+    assert rc in OK_ARGS_STATUS if status is None else rc == status, (change, rc, lib.fp8_last_error())
