@@ -417,7 +417,8 @@ FP8_API int fp8_rope_qkv_fwd_q(const void *qkv_bf16, size_t pitch, size_t T, int
 /* Backward: dq, dk, dv (BF16, shapes of q, k, v; dk, dv may be NULL with Hkv = 0) and the forward's qkv (NULL allowed with
  * FP8_QK_NONE) -> dqkv BF16, rows dqkv_pitch elements apart.  With u the gradient turned back and xh = x / rms(x): FP8_QK_RMS
  * (u - xh mean(u xh)) / rms(x), FP8_QK_TANH alpha u (1 - tanh(alpha x)^2).  *amax_out (nullable): amax(dqkv).  _q: the codes
- * dqkv8 [T, (Hq + 2 Hkv) d] (contiguous rows: the dY8 of the projection's gradient products); dqkv_bf16 may be NULL. */
+ * dqkv8 [T, (Hq + 2 Hkv) d] (contiguous rows: the dY8 of the projection's gradient products); dqkv_bf16 may be NULL.  Outputs must not
+ * overlap inputs here either. */
 FP8_API int fp8_rope_qkv_bwd(const void *dq_bf16, const void *dk_bf16, const void *dv_bf16, const void *qkv_bf16, size_t pitch, size_t T,
                      int Hq, int Hkv, int d, const fp8_rope *rope, void *dqkv_bf16, size_t dqkv_pitch, float *amax_out,
                      void *stream);
@@ -450,7 +451,7 @@ typedef struct {
  * backward pass reads.  y NULL: no block in front (h = x_scale x; h may then be NULL where x_scale is 1).  gate NULL: no gate.
  * gamma_pre NULL: no norm in front of the next block; out is then NULL, and codes and amax are those of h.  *amax_out (nullable) is
  * overwritten with amax(out).  _q: also out8 = FP8cast(*scale * out) of the BF16-rounded values (bit-identical to fp8_cast); out_bf16
- * may be NULL.  h may be x or y itself.  D % 8 == 0, D <= 16384, 1 <= T < 2^31. */
+ * may be NULL.  h may be x or y itself; r_* of a norm that is not there is not touched.  D % 8 == 0, D <= 16384, 1 <= T < 2^31. */
 FP8_API int fp8_block_norm_fwd(const void *x_bf16, const void *y_bf16, const void *gate_bf16, const float *gamma_post,
                        const float *gamma_pre, size_t T, size_t D, const fp8_block_norm *cfg, void *h_bf16, void *out_bf16,
                        float *r_post, float *r_pre, float *amax_out, void *stream);
@@ -550,7 +551,8 @@ FP8_API int fp8_grad_clip(const fp8_grad_item *items, int n_items, const float *
  * rounded towards zero or away from it with the probability of the part cut off, from 16 random bits each: the lower (m) and upper (v) half of
  * mix(mix(mix(K + item) + (i >> 32)) + i) modulo 2^32, K = mix(mix(mix(seed) ^ (seed >> 32)) ^ t), with mix(x): x = (x ^ x >> 16) *
  * 0x9E3779B9; x = (x ^ x >> 15) * 0x6A09E667; x ^ x >> 16, item the number in the list; the same seed and step give the same
- * codes.  v above zero is stored as the smallest code at least.  New states: zeros (all bytes).
+ * codes.  v above zero is stored as the smallest code at least.  The rounding keeps the mean of m and of the root of v; v's own lies 2 to
+ * 4 % above (gradients that do not change in kind), and single roots scatter by a quarter.  New states: zeros (all bytes).
  *
  * `items` is a HOST array, read during the call; its pointers are device pointers, 16-byte aligned (m_exp, v_exp, q_scale, amax to
  * their own type); items of n = 0 are skipped.  A tensor is listed once.  lr, step (int32), norm (nullable): device scalars, so that the

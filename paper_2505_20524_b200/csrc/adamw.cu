@@ -3,8 +3,8 @@
 //
 // The tensors are cut into chunks, numbered through all of them, and a short CTA takes one, found through a table that travels with
 // the launch.  With FP32 moments bytes bind (218 M weights, BF16 gradients and both copies: 924 us, 6.3 GB at 6.8 TB/s).  With 8
-// bits 17 bytes are left per weight and the arithmetic comes up to them: 102 instructions per weight took 916 us, 59 take 565 to
-// 610 (3.7 GB at 6.1 to 6.6 TB/s; the longer it runs the lower the clocks that power allows).
+// bits 17 bytes are left per weight and the arithmetic comes up to them: 102 instructions per weight took 916 us, 60 take 562 to
+// 566 in a graph (3.7 GB at 6.6 TB/s), 580 to 620 back to back (the longer it runs the lower the clocks that power allows).
 #include <math.h>
 
 #include "common.cuh"
@@ -15,7 +15,7 @@ namespace fp8dpa {
 
 constexpr int AW_THREADS = 256;
 // Elements of a thread in a launch: 16 where moments have 8 bits, whose arithmetic hides the second eight's loads (218 M weights:
-// 593 us, 686 with 8), and 8 where all have 32 (930 us, 948 with 16).
+// 563 us, 635 with 8), and 8 where all have 32 (921 us, 943 with 16).
 constexpr int AW_PER_THREAD_8BIT = 16, AW_PER_THREAD = 8;
 constexpr int AW_ITEMS = 304;                             // tensors per launch (31 KB of kernel parameters)
 constexpr int AW_BUCKETS = 512;

@@ -62,8 +62,8 @@ struct BnFwd {
 // Rows and columns on threads as in the layer norm: a thread holds KG groups of eight columns of its unit's rows, both gammas of
 // them in registers, and the next rows travel through its private ring.  NT tensors are read (x; y; gate); the sum of squares of
 // y, the joint, its rounding to BF16, the sum of squares of that and the result follow in one pass: every tensor is read once and
-// written once (8192 x 4096 with both norms and codes: 39.8 us in a graph, 235 MB at 5.9 TB/s; 43 with two CTAs per SM for three;
-// with a gate 49.5 us, 6.1 TB/s).  The reciprocal roots by rsqrtf, off by 2 ulp of FP32 at most.
+// written once (8192 x 4096 with both norms and codes: 40.6 us in a graph, 235 MB at 5.8 TB/s; 43 with two CTAs per SM for three;
+// with a gate 50.2 us, 6.0 TB/s).  The reciprocal roots by rsqrtf, off by 2 ulp of FP32 at most.
 template <int KG, RowUnit UNIT, int NT, bool PRE, int STAGES, int MAXT, int MINB>
 __global__ void __launch_bounds__(MAXT, MINB) block_norm_fwd_kernel(const BnFwd p, int lanes_log2)
 {
@@ -223,12 +223,12 @@ struct BnBwd {
 // dgamma_post = sum dz yh, which a thread keeps in registers for its columns.  The two means are two sums over the row's
 // threads, the second from what the first gives.  Every tensor is read once and written once.  The reciprocal roots go into
 // scalars of the row: the loop forms e r_pre, dz r_post and f r_post and adds multiples of h and y to them, and the gammas lie in
-// shared memory (8192 x 4096 with gate and codes: 106 -> 87 us in a graph, 503 MB at 5.8 TB/s; without a gate 70 us for 369 MB).
+// shared memory (8192 x 4096 with gate and codes: 106 -> 88 us in a graph, 503 MB at 5.7 TB/s; without a gate 67 us for 369 MB).
 // Two barriers per row on 16 warps leave 0.55 instructions per cycle and scheduler; 512 threads with one group each, two CTAs
 // per SM, have to do with 64 registers and spill (120 us).
 // STAGES = 1: the ring holds one row, and a thread asks for the next row's piece as soon as it has read its own: above 8192
-// columns, where two rows find no room (3000 x 10000: 84 us without a gate, memory's 55; 2048 x 16384 102, memory's 62: 64 of 128
-// registers are the gammas' sums there, and one CTA fills an SM).
+// columns, where two rows find no room (BF16 results without a gate, norm behind: 3000 x 10000 83 us, memory's 55; 2048 x 16384 114,
+// memory's 62: 64 of 128 registers are the gammas' sums there, and one CTA fills an SM).
 __host__ __device__ constexpr int bn_bwd_tensors(bool pre, bool gate) { return 2 + 2 * pre + gate; }
 __host__ __device__ constexpr int bn_bwd_near(int kg, bool pre) { return kg <= 3 && pre ? 2 : 1; }
 template <int KG, RowUnit UNIT, bool PRE, bool GATE, int STAGES, int MAXT, int MINB>
