@@ -627,8 +627,9 @@ static int bn_fwd(const char *who, const void *x, const void *y, const void *gat
         return FP8_ERR_SHAPE;
     }
     if (!aligned16(x) || !aligned16(y) || !aligned16(gate) || !aligned16(gamma_post) || !aligned16(gamma_pre) || !aligned16(h) ||
-        !aligned16(out) || !aligned16(out8)) {
-        set_error("%s: pointers must be 16-byte aligned", who);
+        !aligned16(out) || !aligned16(out8) || !aligned_to(q_scale, 4) || !aligned_to(r_post, 4) || !aligned_to(r_pre, 4) ||
+        !aligned_to(amax_out, 4)) {
+        set_error("%s: pointers must be 16-byte aligned, the scale, r_post, r_pre and amax_out to their type", who);
         return FP8_ERR_ALIGN;
     }
     rc = check_arch();
@@ -678,8 +679,9 @@ static int bn_bwd(const char *who, const void *dout, const void *dh, const void 
         return FP8_ERR_SHAPE;
     }
     if (!aligned16(dout) || !aligned16(dh) || !aligned16(h) || !aligned16(y) || !aligned16(gate) || !aligned16(gamma_post) ||
-        !aligned16(gamma_pre) || !aligned16(dx) || !aligned16(dy) || !aligned16(dy8) || !aligned16(dgate)) {
-        set_error("%s: pointers must be 16-byte aligned", who);
+        !aligned16(gamma_pre) || !aligned16(dx) || !aligned16(dy) || !aligned16(dy8) || !aligned16(dgate) || !aligned_to(q_scale, 4) ||
+        !aligned_to(r_post, 4) || !aligned_to(r_pre, 4) || !aligned_to(dgamma_post, 4) || !aligned_to(dgamma_pre, 4) || !aligned_to(amax_out, 4)) {
+        set_error("%s: pointers must be 16-byte aligned, the scale, r_post, r_pre, dgamma_* and amax_out to their type", who);
         return FP8_ERR_ALIGN;
     }
     const size_t need = fp8_block_norm_bwd_workspace_bytes(T, D);

@@ -615,8 +615,9 @@ static int rope_fwd(const char *who, const void *qkv, size_t pitch, size_t T, in
         set_error("%s: outputs of K or V without heads of them", who);
         return FP8_ERR_SHAPE;
     }
-    if (!aligned16(qkv) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q8) || !aligned16(k8) || !aligned16(v8)) {
-        set_error("%s: tensor pointers must be 16-byte aligned", who);
+    if (!aligned16(qkv) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q8) || !aligned16(k8) || !aligned16(v8) ||
+        !aligned_to(scales, 4) || !aligned_to(amax_out, 4)) {
+        set_error("%s: tensor pointers must be 16-byte aligned, scales and amax_out to their type", who);
         return FP8_ERR_ALIGN;
     }
     rc = check_arch();
@@ -652,8 +653,9 @@ static int rope_bwd(const char *who, const void *dq, const void *dk, const void 
         set_error("%s: pitches of %zu and %zu elements (rows of %zu, multiples of 8)", who, pitch, out_pitch, row);
         return FP8_ERR_SHAPE;
     }
-    if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(qkv) || !aligned16(dqkv) || !aligned16(dqkv8)) {
-        set_error("%s: tensor pointers must be 16-byte aligned", who);
+    if (!aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(qkv) || !aligned16(dqkv) || !aligned16(dqkv8) ||
+        !aligned_to(scale, 4) || !aligned_to(amax_out, 4)) {
+        set_error("%s: tensor pointers must be 16-byte aligned, scale and amax_out to their type", who);
         return FP8_ERR_ALIGN;
     }
     rc = check_arch();

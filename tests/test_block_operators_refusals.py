@@ -274,3 +274,27 @@ def test_joint_gradient_refuses_outputs_of_what_is_not_there(lib, i):
     args["cfg"] = C.byref(binding.BlockNorm(*CFG.values()))
     rc = lib.fp8_block_norm_bwd(*args.values())
     assert rc in OK_ARGS_STATUS if status is None else rc == status, (change, rc, lib.fp8_last_error())
+
+
+WORDS_OFF_THEIR_TYPE = [
+    ("fp8_rope_qkv_fwd", FWD, dict(amax=A + 2)), ("fp8_rope_qkv_fwd_q", FWD_Q, dict(scales=A + 1)), ("fp8_rope_qkv_fwd_q", FWD_Q, dict(amax=A + 3)),
+    ("fp8_rope_qkv_bwd", BWD, dict(amax=A + 2)), ("fp8_rope_qkv_bwd_q", BWD_Q, dict(scale=A + 2)),
+    ("fp8_block_norm_fwd", NORM, dict(rq=A + 2)), ("fp8_block_norm_fwd", NORM, dict(rp=A + 1)), ("fp8_block_norm_fwd", NORM, dict(amax=A + 2)),
+    ("fp8_block_norm_fwd_q", NORM_Q, dict(scale=A + 2)),
+    ("fp8_block_norm_bwd", GRAD, dict(rq=A + 2)), ("fp8_block_norm_bwd", GRAD, dict(rp=A + 2)), ("fp8_block_norm_bwd", GRAD, dict(dgq=A + 2)),
+    ("fp8_block_norm_bwd", GRAD, dict(dgp=A + 1)), ("fp8_block_norm_bwd", GRAD, dict(amax=A + 2)), ("fp8_block_norm_bwd_q", GRAD_Q, dict(scale=A + 2)),
+]
+
+
+@pytest.mark.parametrize("i", range(len(WORDS_OFF_THEIR_TYPE)))
+def test_refuses_words_that_are_not_aligned(lib, i):
+    """Scales, maxima, statistics and sums are binary32 words: at 4-byte addresses they are taken, at others refused."""
+    name, base, change = WORDS_OFF_THEIR_TYPE[i]
+    for args, status in ((base | change, ALIGN), (base | {k: v // 4 * 4 + 4 for k, v in change.items()}, None)):
+        args = dict(args)
+        if "rope" in args:
+            args["rope"] = C.byref(binding.Rope(*args["rope"].values()))
+        if "cfg" in args:
+            args["cfg"] = C.byref(binding.BlockNorm(*args["cfg"].values()))
+        rc = getattr(lib, name)(*args.values())
+        assert rc in OK_ARGS_STATUS if status is None else rc == status, (name, change, rc, lib.fp8_last_error())
